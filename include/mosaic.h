@@ -448,6 +448,84 @@ mosaic_status mosaic_op_rope(void* stream, int32_t quota, int32_t dtype, int32_t
                              int32_t H, int32_t d, int32_t direction, void* qkv,
                              const void* table);
 
+/* Rotary positions with several axes (time, height, width of images and video).  A head of d
+ * elements (even, at most 256) has d/2 pairs, each with an axis and a frequency; at token t pair i
+ * turns by pos[axis(i)*T + t] * frequency(i).  pos: device int32 [n_axes, T], any values; the angle is formed
+ * in double.  mosaic_op_rope_axes_table fills `table`, a 16-byte aligned device buffer of
+ * mosaic_op_rope_axes_table_bytes(d), for n_axes (1 to MOSAIC_MAX_AXES) axes with
+ * sections[a] >= 0 pairs each (a HOST array, read before the call returns; their sum is
+ * at most d/2, and the pairs past it stay as they are):
+ *   MOSAIC_AXES_SPLIT  runs of pairs in the order of the axes; frequency(i) = base^(-2i/d)
+ *   MOSAIC_AXES_OWN    the same runs, each axis with a spectrum of its own: its j-th pair has base^(-j/sections[a])
+ *   MOSAIC_AXES_DEALT  pairs go to the axes in turn, one each, while an axis has room; frequency(i) = base^(-2i/d)
+ * Pair i is elements (2i, 2i+1) of the head (MOSAIC_PAIR_ADJACENT) or (i, i+d/2) (MOSAIC_PAIR_HALVES). */
+#define MOSAIC_MAX_AXES 4
+enum { MOSAIC_AXES_SPLIT = 0, MOSAIC_AXES_OWN = 1, MOSAIC_AXES_DEALT = 2 };
+enum { MOSAIC_PAIR_ADJACENT = 0, MOSAIC_PAIR_HALVES = 1 };
+size_t        mosaic_op_rope_axes_table_bytes(int32_t d);
+mosaic_status mosaic_op_rope_axes_table(void* stream, int32_t quota, int32_t d, int32_t n_axes,
+                                        const int32_t* sections, int32_t order, float base, void* table);
+/* x, y [T, (H + 2*Hkv)*d], row = [q (H heads) | k (Hkv heads) | v (Hkv heads)], Hkv divides H: the q
+ * and k heads of x rotated (direction = +1) or turned back (-1: gradients of rotated q, k), v as it is.
+ * y may be x; it must not overlap it otherwise.  A pair whose axis is n_axes or more (a
+ * table made for more axes) stays as it is.  The tokens may be any set: a batch, packed sequences, the
+ * single tokens of a serving step. */
+mosaic_status mosaic_op_rope_axes(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t H,
+                                  int32_t Hkv, int32_t d, int32_t pairing, int32_t direction,
+                                  int32_t n_axes, const int32_t* pos, const void* table, const void* x,
+                                  void* y);
+/* A norm over the d elements of every query and key head, and the rotation of the result, in one
+ * pass: norm = MOSAIC_RMSNORM (x * rstd * gamma; beta_q, beta_k unused) or MOSAIC_LAYERNORM
+ * ((x - mean) * rstd * gamma + beta), eps > 0.  gamma_q, beta_q [d] are shared by the query heads, gamma_k, beta_k [d]
+ * by the key heads.  table == NULL (then pos may be NULL and n_axes 0): no rotation. */
+mosaic_status mosaic_op_qk_norm_rope_fwd(void* stream, int32_t quota, int32_t dtype, int32_t norm,
+                                         int64_t T, int32_t H, int32_t Hkv, int32_t d, float eps,
+                                         int32_t pairing, int32_t n_axes, const int32_t* pos,
+                                         const void* table, const void* x, const void* gamma_q,
+                                         const void* beta_q, const void* gamma_k, const void* beta_k,
+                                         void* y);
+/* Its backward pass: x, the rows before the norm; dy, the gradient of y ([dq | dk | dv], as
+ * mosaic_op_attention_gqa_bwd gives it); dx, the gradient of x (dx may be dy and must not
+ * overlap x or dy otherwise; v's part is dy's); dgamma_q, dgamma_k, and for LayerNorm dbeta_q, dbeta_k, [d] each, sums over tokens and heads
+ * in a fixed order (overwritten; zero for T = 0).  scratch: 16-byte aligned device buffer of
+ * mosaic_op_qk_norm_rope_bwd_scratch_bytes(d), not shared by calls that overlap in time. */
+mosaic_status mosaic_op_qk_norm_rope_bwd(void* stream, int32_t quota, int32_t dtype, int32_t norm,
+                                         int64_t T, int32_t H, int32_t Hkv, int32_t d, float eps,
+                                         int32_t pairing, int32_t n_axes, const int32_t* pos,
+                                         const void* table, const void* x, const void* gamma_q,
+                                         const void* gamma_k, const void* dy, void* dx, void* dgamma_q,
+                                         void* dbeta_q, void* dgamma_k, void* dbeta_k, void* scratch);
+size_t        mosaic_op_qk_norm_rope_bwd_scratch_bytes(int32_t d);
+
+/* Activation checkpoints in 8 bits.  n consecutive elements are kept as q, n whole numbers (int8), and scale,
+ * one byte for each 32 of them (mosaic_op_pack8_scale_bytes(n)): with e the smallest exponent from -127 on
+ * for which max |x| <= 127.5 * 2^e, the byte e + 127 and q = x / 2^e rounded to nearest (ties to even), at most 127
+ * in size.  An element comes back as q * 2^e, off by 2^e / 2 at most, and exactly so in either dtype.  A block that holds a
+ * NaN or an infinity has the byte 255 and comes back as NaN.  q and scale need no alignment (16-byte aligned
+ * buffers are faster).  No output may overlap an input or another output, but dz may be da where it says so. */
+size_t        mosaic_op_pack8_scale_bytes(int64_t n);
+mosaic_status mosaic_op_pack8(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* x,
+                              void* q, void* scale);
+mosaic_status mosaic_op_unpack8(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* q,
+                                const void* scale, void* x);
+/* The activation of an MLP that keeps its input z in 8 bits instead of z and a: a = act(z) (of z as given) and z
+ * packed, in one pass; act = MOSAIC_GELU, MOSAIC_GELU_TANH (z [T,f]) or MOSAIC_SWIGLU (z [T,2f] = [gate | up]); a [T,f].
+ * The backward pass takes z from its 8 bits: dz = act'(z) da (dz laid out like z; for the GELU forms it may be da) and, where a is not NULL, a = act(z)
+ * again, the input of the next layer's weight gradient. */
+mosaic_status mosaic_op_act_fwd_pack8(void* stream, int32_t quota, int32_t dtype, int32_t act, int64_t T,
+                                      int64_t f, const void* z, void* a, void* zq, void* zscale);
+mosaic_status mosaic_op_act_bwd_pack8(void* stream, int32_t quota, int32_t dtype, int32_t act, int64_t T,
+                                      int64_t f, const void* zq, const void* zscale, const void* da,
+                                      void* dz, void* a);
+/* mosaic_op_linear_wgrad for an input X [T,k] that was kept in 8 bits (Xq, Xscale): dW[k,n] = X^T dY, db[n] = column
+ * sums of dY (may be NULL); dY, dW, db of `dtype`, T > 0; with db, n must be a multiple of 8
+ * (bf16) or 4 (fp32).  scratch: 16-byte aligned device buffer of
+ * mosaic_op_linear_wgrad_pack8_scratch_bytes(dtype, T, k, n), not shared by calls that overlap in time. */
+mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t dtype, int64_t T,
+                                           int64_t k, int64_t n, const void* Xq, const void* Xscale,
+                                           const void* dY, void* dW, void* db, void* scratch);
+size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t T, int64_t k, int64_t n);
+
 /* AdamW over n elements: m = b1 m + (1-b1) g; v = b2 v + (1-b2) g^2;
  * p -= lr * ( (m / (1-b1^step)) / (sqrt(v / (1-b2^step)) + eps) + weight_decay * p ).
  * params, grads in `dtype`; m, v and master (may be NULL) fp32; master, when given, is the

@@ -30,6 +30,11 @@ _NORM = {"none": NORM_NONE, "layernorm": LAYERNORM, "rmsnorm": RMSNORM}
 GELU_TANH = 2
 _ACT = {"gelu": GELU, "swiglu": SWIGLU, "gelu_tanh": GELU_TANH}
 _DTYPE = {"f32": F32, "bf16": BF16}
+AXES_SPLIT, AXES_OWN, AXES_DEALT = 0, 1, 2
+PAIR_ADJACENT, PAIR_HALVES = 0, 1
+MAX_AXES = 4
+_ORDER = {"split": AXES_SPLIT, "own": AXES_OWN, "dealt": AXES_DEALT}
+_PAIRING = {"adjacent": PAIR_ADJACENT, "halves": PAIR_HALVES}
 
 
 class MosaicError(RuntimeError):
@@ -130,6 +135,20 @@ SIGNATURES = {
     "mosaic_op_rope_table_bytes": (C.c_size_t, [_i32, _i32]),
     "mosaic_op_rope_table": (_i32, [_vp, _i32, _i32, _i32, _f32, _vp]),
     "mosaic_op_rope": (_i32, [_vp, _i32, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "mosaic_op_rope_axes_table_bytes": (_sz, [_i32]),
+    "mosaic_op_rope_axes_table": (_i32, [_vp, _i32, _i32, _i32, C.POINTER(_i32), _i32, _f32, _vp]),
+    "mosaic_op_rope_axes": (_i32, [_vp, _i32, _i32, _i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp]),
+    "mosaic_op_qk_norm_rope_fwd": (_i32, [_vp, _i32, _i32, _i32, _i64, _i32, _i32, _i32, _f32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mosaic_op_qk_norm_rope_bwd": (_i32, [_vp, _i32, _i32, _i32, _i64, _i32, _i32, _i32, _f32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                          _vp, _vp, _vp, _vp]),
+    "mosaic_op_qk_norm_rope_bwd_scratch_bytes": (_sz, [_i32]),
+    "mosaic_op_pack8_scale_bytes": (_sz, [_i64]),
+    "mosaic_op_pack8": (_i32, [_vp, _i32, _i32, _i64, _vp, _vp, _vp]),
+    "mosaic_op_unpack8": (_i32, [_vp, _i32, _i32, _i64, _vp, _vp, _vp]),
+    "mosaic_op_act_fwd_pack8": (_i32, [_vp, _i32, _i32, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "mosaic_op_act_bwd_pack8": (_i32, [_vp, _i32, _i32, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "mosaic_op_linear_wgrad_pack8": (_i32, [_vp, _i32, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mosaic_op_linear_wgrad_pack8_scratch_bytes": (_sz, [_i32, _i64, _i64, _i64]),
     "mosaic_op_adamw": (_i32, [_vp, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _f32, _i64]),
     "mosaic_op_swiglu_fwd": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp]),
     "mosaic_op_swiglu_bwd": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp, _vp]),
@@ -555,6 +574,65 @@ def op_rope_table(stream, quota, N, d, base, table):
 
 def op_rope(stream, quota, dtype, B, N, H, d, direction, qkv, table):
     check(lib().mosaic_op_rope(stream, quota, _dt(dtype), B, N, H, d, direction, _ptr(qkv), _ptr(table)))
+
+
+def rope_axes_table_bytes(d: int) -> int:
+    return int(lib().mosaic_op_rope_axes_table_bytes(d))
+
+
+def op_rope_axes_table(stream, quota, d, sections: Sequence[int], order: str, base, table):
+    """sections: pairs of each axis; order: "split", "own" or "dealt"."""
+    host = (C.c_int32 * max(1, len(sections)))(*[int(v) for v in sections])
+    check(lib().mosaic_op_rope_axes_table(stream, quota, d, len(sections), host, _ORDER[order], base, _ptr(table)))
+
+
+def op_rope_axes(stream, quota, dtype, T, H, Hkv, d, pairing: str, direction, n_axes, pos, table, x, y):
+    """pos: int32 [n_axes, T]; pairing: "adjacent" or "halves"."""
+    check(lib().mosaic_op_rope_axes(stream, quota, _dt(dtype), T, H, Hkv, d, _PAIRING[pairing], direction, n_axes, _ptr(pos), _ptr(table), _ptr(x), _ptr(y)))
+
+
+def op_qk_norm_rope_fwd(stream, quota, dtype, norm, T, H, Hkv, d, eps, pairing, n_axes, pos, table, x, gamma_q, beta_q, gamma_k, beta_k, y):
+    check(lib().mosaic_op_qk_norm_rope_fwd(stream, quota, _dt(dtype), _NORM[norm], T, H, Hkv, d, eps, _PAIRING[pairing], n_axes, _ptr(pos), _ptr(table),
+                                           _ptr(x), _ptr(gamma_q), _ptr(beta_q), _ptr(gamma_k), _ptr(beta_k), _ptr(y)))
+
+
+def op_qk_norm_rope_bwd(stream, quota, dtype, norm, T, H, Hkv, d, eps, pairing, n_axes, pos, table, x, gamma_q, gamma_k, dy, dx, dgamma_q, dbeta_q,
+                        dgamma_k, dbeta_k, scratch):
+    check(lib().mosaic_op_qk_norm_rope_bwd(stream, quota, _dt(dtype), _NORM[norm], T, H, Hkv, d, eps, _PAIRING[pairing], n_axes, _ptr(pos), _ptr(table),
+                                           _ptr(x), _ptr(gamma_q), _ptr(gamma_k), _ptr(dy), _ptr(dx), _ptr(dgamma_q), _ptr(dbeta_q), _ptr(dgamma_k),
+                                           _ptr(dbeta_k), _ptr(scratch)))
+
+
+def qk_norm_rope_bwd_scratch_bytes(d: int) -> int:
+    return int(lib().mosaic_op_qk_norm_rope_bwd_scratch_bytes(d))
+
+
+def pack8_scale_bytes(n: int) -> int:
+    return int(lib().mosaic_op_pack8_scale_bytes(n))
+
+
+def op_pack8(stream, quota, dtype, n, x, q, scale):
+    check(lib().mosaic_op_pack8(stream, quota, _dt(dtype), n, _ptr(x), _ptr(q), _ptr(scale)))
+
+
+def op_unpack8(stream, quota, dtype, n, q, scale, x):
+    check(lib().mosaic_op_unpack8(stream, quota, _dt(dtype), n, _ptr(q), _ptr(scale), _ptr(x)))
+
+
+def op_act_fwd_pack8(stream, quota, dtype, act, T, f, z, a, zq, zscale):
+    check(lib().mosaic_op_act_fwd_pack8(stream, quota, _dt(dtype), _ACT[act], T, f, _ptr(z), _ptr(a), _ptr(zq), _ptr(zscale)))
+
+
+def op_act_bwd_pack8(stream, quota, dtype, act, T, f, zq, zscale, da, dz, a=None):
+    check(lib().mosaic_op_act_bwd_pack8(stream, quota, _dt(dtype), _ACT[act], T, f, _ptr(zq), _ptr(zscale), _ptr(da), _ptr(dz), _ptr(a)))
+
+
+def op_linear_wgrad_pack8(stream, quota, dtype, T, k, n, Xq, Xscale, dY, dW, db, scratch):
+    check(lib().mosaic_op_linear_wgrad_pack8(stream, quota, _dt(dtype), T, k, n, _ptr(Xq), _ptr(Xscale), _ptr(dY), _ptr(dW), _ptr(db), _ptr(scratch)))
+
+
+def linear_wgrad_pack8_scratch_bytes(dtype: str, T: int, k: int, n: int) -> int:
+    return int(lib().mosaic_op_linear_wgrad_pack8_scratch_bytes(_dt(dtype), T, k, n))
 
 
 def op_adamw(stream, quota, dtype, n, params, grads, m, v, master, lr, beta1, beta2, eps, weight_decay, step):

@@ -261,6 +261,169 @@ mosaic_status mosaic_op_adamw(void* stream, int32_t quota, int32_t dtype, int64_
   return launch_adamw((hipStream_t)stream, quota, dtype, n, params, grads, m, v, master, lr, beta1, beta2, eps, weight_decay, step);
 }
 
+size_t mosaic_op_rope_axes_table_bytes(int32_t d) { return d > 0 ? rope_axes_table_bytes(d) : 0; }
+
+mosaic_status mosaic_op_rope_axes_table(void* stream, int32_t quota, int32_t d, int32_t n_axes, const int32_t* sections, int32_t order, float base,
+                                        void* table) {
+  NONNULL(sections); NONNULL(table);
+  if (d <= 0 || d % 2) MOSAIC_FAIL(MOSAIC_EINVAL, "head size %d is not positive and even", d);
+  if (d > 256) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "head size %d > 256", d);
+  if (n_axes < 1 || n_axes > MOSAIC_MAX_AXES) MOSAIC_FAIL(MOSAIC_EINVAL, "%d position axes; 1 to %d", n_axes, MOSAIC_MAX_AXES);
+  if (order < MOSAIC_AXES_SPLIT || order > MOSAIC_AXES_DEALT) MOSAIC_FAIL(MOSAIC_EINVAL, "bad order of axes %d", order);
+  if (!(base > 0.f) || base > 3.4028234e38f) MOSAIC_FAIL(MOSAIC_EINVAL, "rotary base must be positive and finite");
+  int64_t sum = 0;
+  for (int a = 0; a < n_axes; ++a) {
+    if (sections[a] < 0) MOSAIC_FAIL(MOSAIC_EINVAL, "axis %d has %d pairs", a, sections[a]);
+    sum += sections[a];
+  }
+  if (sum > d / 2) MOSAIC_FAIL(MOSAIC_EINVAL, "the axes have %lld pairs, a head %d", (long long)sum, d / 2);
+  if ((uintptr_t)table % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "the table must be 16-byte aligned");
+  MOSAIC_TRY(check_common(quota, MOSAIC_F32));
+  return launch_rope_axes_table((hipStream_t)stream, quota, d, n_axes, sections, order, base, table);
+}
+
+// what the calls on packed rows share; `rotates`: there is a table
+static mosaic_status check_heads(int32_t dtype, int64_t T, int32_t H, int32_t Hkv, int32_t d, int32_t pairing, int32_t n_axes, const int32_t* pos,
+                                 const void* table) {
+  if (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) MOSAIC_FAIL(MOSAIC_EINVAL, "bad dtype %d", dtype);
+  if (T < 0 || H <= 0 || Hkv <= 0) MOSAIC_FAIL(MOSAIC_EINVAL, "bad sizes T=%lld H=%d Hkv=%d", (long long)T, H, Hkv);
+  if (H % Hkv) MOSAIC_FAIL(MOSAIC_EINVAL, "key/value heads (%d) must divide the query heads (%d)", Hkv, H);
+  if (d <= 0 || d % 2) MOSAIC_FAIL(MOSAIC_EINVAL, "head size %d is not positive and even", d);
+  if (d > 256) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "head size %d > 256", d);
+  if (((int64_t)H + 2 * (int64_t)Hkv) * d > INT32_MAX) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "rows of more than 2^31 - 1 elements");
+  if (T > ((int64_t)1 << 62) / (((int64_t)H + 2 * Hkv) * d)) MOSAIC_FAIL(MOSAIC_EINVAL, "%lld tokens", (long long)T);
+  if (pairing != MOSAIC_PAIR_ADJACENT && pairing != MOSAIC_PAIR_HALVES) MOSAIC_FAIL(MOSAIC_EINVAL, "bad pairing %d", pairing);
+  if (table) {
+    NONNULL(pos);
+    if (n_axes < 1 || n_axes > MOSAIC_MAX_AXES) MOSAIC_FAIL(MOSAIC_EINVAL, "%d position axes; 1 to %d", n_axes, MOSAIC_MAX_AXES);
+    if ((uintptr_t)table % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "the table must be 16-byte aligned");
+  }
+  return MOSAIC_OK;
+}
+static mosaic_status check_qk_norm(int32_t norm, float eps) {
+  if (norm != MOSAIC_LAYERNORM && norm != MOSAIC_RMSNORM) MOSAIC_FAIL(MOSAIC_EINVAL, "bad norm kind %d", norm);
+  if (!(eps > 0.f)) MOSAIC_FAIL(MOSAIC_EINVAL, "eps must be positive");
+  return MOSAIC_OK;
+}
+#define APART(p, pn, q, qn) if (overlap(p, pn, q, qn)) MOSAIC_FAIL(MOSAIC_EINVAL, #p " overlaps " #q)
+
+mosaic_status mosaic_op_rope_axes(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t H, int32_t Hkv, int32_t d, int32_t pairing,
+                                  int32_t direction, int32_t n_axes, const int32_t* pos, const void* table, const void* x, void* y) {
+  NONNULL(table); NONNULL(x); NONNULL(y);
+  MOSAIC_TRY(check_heads(dtype, T, H, Hkv, d, pairing, n_axes, pos, table));
+  if (direction != 1 && direction != -1) MOSAIC_FAIL(MOSAIC_EINVAL, "direction must be +1 or -1");
+  const int64_t bytes = T * (H + 2 * Hkv) * d * (int64_t)dtype_size(dtype);
+  if (x != y) APART(x, bytes, y, bytes);
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_qk_norm_rope_fwd((hipStream_t)stream, quota, dtype, MOSAIC_NORM_NONE, T, H, Hkv, d, 0.f, pairing, direction, n_axes, pos, table, x,
+                                 nullptr, nullptr, nullptr, nullptr, y);
+}
+
+mosaic_status mosaic_op_qk_norm_rope_fwd(void* stream, int32_t quota, int32_t dtype, int32_t norm, int64_t T, int32_t H, int32_t Hkv, int32_t d,
+                                         float eps, int32_t pairing, int32_t n_axes, const int32_t* pos, const void* table, const void* x,
+                                         const void* gamma_q, const void* beta_q, const void* gamma_k, const void* beta_k, void* y) {
+  NONNULL(x); NONNULL(gamma_q); NONNULL(gamma_k); NONNULL(y);
+  MOSAIC_TRY(check_qk_norm(norm, eps));
+  if (norm == MOSAIC_LAYERNORM) { NONNULL(beta_q); NONNULL(beta_k); }
+  MOSAIC_TRY(check_heads(dtype, T, H, Hkv, d, pairing, n_axes, pos, table));
+  const int64_t bytes = T * (H + 2 * Hkv) * d * (int64_t)dtype_size(dtype);
+  if (x != y) APART(x, bytes, y, bytes);
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_qk_norm_rope_fwd((hipStream_t)stream, quota, dtype, norm, T, H, Hkv, d, eps, pairing, +1, n_axes, pos, table, x, gamma_q, beta_q,
+                                 gamma_k, beta_k, y);
+}
+
+size_t mosaic_op_qk_norm_rope_bwd_scratch_bytes(int32_t d) { return d > 0 ? qk_norm_rope_bwd_scratch_bytes(d) : 0; }
+
+mosaic_status mosaic_op_qk_norm_rope_bwd(void* stream, int32_t quota, int32_t dtype, int32_t norm, int64_t T, int32_t H, int32_t Hkv, int32_t d,
+                                         float eps, int32_t pairing, int32_t n_axes, const int32_t* pos, const void* table, const void* x,
+                                         const void* gamma_q, const void* gamma_k, const void* dy, void* dx, void* dgamma_q, void* dbeta_q,
+                                         void* dgamma_k, void* dbeta_k, void* scratch) {
+  NONNULL(x); NONNULL(gamma_q); NONNULL(gamma_k); NONNULL(dy); NONNULL(dx); NONNULL(dgamma_q); NONNULL(dgamma_k); NONNULL(scratch);
+  MOSAIC_TRY(check_qk_norm(norm, eps));
+  if (norm == MOSAIC_LAYERNORM) { NONNULL(dbeta_q); NONNULL(dbeta_k); }
+  MOSAIC_TRY(check_heads(dtype, T, H, Hkv, d, pairing, n_axes, pos, table));
+  const int64_t bytes = T * (H + 2 * Hkv) * d * (int64_t)dtype_size(dtype);
+  APART(x, bytes, dx, bytes);
+  if (dy != dx) APART(dy, bytes, dx, bytes);
+  if ((uintptr_t)scratch % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 16-byte aligned");
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_qk_norm_rope_bwd((hipStream_t)stream, quota, dtype, norm, T, H, Hkv, d, eps, pairing, n_axes, pos, table, x, gamma_q, gamma_k, dy, dx,
+                                 dgamma_q, dbeta_q, dgamma_k, dbeta_k, scratch);
+}
+
+size_t mosaic_op_pack8_scale_bytes(int64_t n) { return n > 0 ? pack8_scale_bytes(n) : 0; }
+
+// sizes that the packed calls take: their products fit 64 bits with room for the element size
+static mosaic_status check_packed(int32_t dtype, int64_t rows, int64_t cols) {
+  if (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) MOSAIC_FAIL(MOSAIC_EINVAL, "bad dtype %d", dtype);
+  if (rows < 0 || cols < 0 || (cols > 0 && rows > ((int64_t)1 << 58) / cols)) MOSAIC_FAIL(MOSAIC_EINVAL, "bad size %lld x %lld", (long long)rows, (long long)cols);
+  return MOSAIC_OK;
+}
+
+mosaic_status mosaic_op_pack8(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* x, void* q, void* scale) {
+  NONNULL(x); NONNULL(q); NONNULL(scale);
+  MOSAIC_TRY(check_packed(dtype, n, 1));
+  const int64_t bytes = n * (int64_t)dtype_size(dtype), scales = (int64_t)mosaic_op_pack8_scale_bytes(n);
+  APART(x, bytes, q, n); APART(x, bytes, scale, scales); APART(q, n, scale, scales);
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_pack8((hipStream_t)stream, quota, dtype, n, x, q, scale);
+}
+
+mosaic_status mosaic_op_unpack8(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* q, const void* scale, void* x) {
+  NONNULL(q); NONNULL(scale); NONNULL(x);
+  MOSAIC_TRY(check_packed(dtype, n, 1));
+  const int64_t bytes = n * (int64_t)dtype_size(dtype);
+  APART(x, bytes, q, n); APART(x, bytes, scale, (int64_t)mosaic_op_pack8_scale_bytes(n));
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_unpack8((hipStream_t)stream, quota, dtype, n, q, scale, x);
+}
+
+static mosaic_status check_act(int32_t dtype, int32_t act, int64_t T, int64_t f) {
+  if (act != MOSAIC_GELU && act != MOSAIC_SWIGLU && act != MOSAIC_GELU_TANH) MOSAIC_FAIL(MOSAIC_EINVAL, "bad activation %d", act);
+  return check_packed(dtype, T, f);
+}
+
+mosaic_status mosaic_op_act_fwd_pack8(void* stream, int32_t quota, int32_t dtype, int32_t act, int64_t T, int64_t f, const void* z, void* a, void* zq,
+                                      void* zscale) {
+  NONNULL(z); NONNULL(a); NONNULL(zq); NONNULL(zscale);
+  MOSAIC_TRY(check_act(dtype, act, T, f));
+  const int64_t es = (int64_t)dtype_size(dtype), m = T * f, n = act == MOSAIC_SWIGLU ? 2 * m : m, scales = (int64_t)mosaic_op_pack8_scale_bytes(n);
+  APART(z, n * es, a, m * es); APART(z, n * es, zq, n); APART(z, n * es, zscale, scales);
+  APART(a, m * es, zq, n); APART(a, m * es, zscale, scales); APART(zq, n, zscale, scales);
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_act_fwd_pack8((hipStream_t)stream, quota, dtype, act, T, f, z, a, zq, zscale);
+}
+
+mosaic_status mosaic_op_act_bwd_pack8(void* stream, int32_t quota, int32_t dtype, int32_t act, int64_t T, int64_t f, const void* zq, const void* zscale,
+                                      const void* da, void* dz, void* a) {
+  NONNULL(zq); NONNULL(zscale); NONNULL(da); NONNULL(dz);
+  MOSAIC_TRY(check_act(dtype, act, T, f));
+  const int64_t es = (int64_t)dtype_size(dtype), m = T * f, n = act == MOSAIC_SWIGLU ? 2 * m : m, scales = (int64_t)mosaic_op_pack8_scale_bytes(n);
+  if (da != dz || act == MOSAIC_SWIGLU) APART(da, m * es, dz, n * es);
+  APART(dz, n * es, zq, n); APART(dz, n * es, zscale, scales);
+  if (a) { APART(a, m * es, da, m * es); APART(a, m * es, dz, n * es); APART(a, m * es, zq, n); APART(a, m * es, zscale, scales); }
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_act_bwd_pack8((hipStream_t)stream, quota, dtype, act, T, f, zq, zscale, da, dz, a);
+}
+
+size_t mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t T, int64_t k, int64_t n) {
+  return T > 0 && k > 0 && n > 0 ? linear_wgrad_pack8_scratch_bytes(dtype, T, k, n) : 0;
+}
+
+mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t k, int64_t n, const void* Xq, const void* Xscale,
+                                           const void* dY, void* dW, void* db, void* scratch) {
+  NONNULL(Xq); NONNULL(Xscale); NONNULL(dY); NONNULL(dW); NONNULL(scratch);
+  if (T < 0 || k <= 0 || n <= 0) MOSAIC_FAIL(MOSAIC_EINVAL, "bad linear sizes");
+  if (T == 0) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "weight gradient over zero tokens");
+  MOSAIC_TRY(check_packed(dtype, T, k)); MOSAIC_TRY(check_packed(dtype, T, n)); MOSAIC_TRY(check_packed(dtype, k, n));
+  const int vn = dtype == MOSAIC_BF16 ? 8 : 4;
+  if (db && n % vn) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "column sums of rows of %lld elements, not a multiple of %d", (long long)n, vn);
+  if ((uintptr_t)scratch % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 16-byte aligned");
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_linear_wgrad_pack8((hipStream_t)stream, quota, dtype, T, k, n, Xq, Xscale, dY, dW, db, scratch);
+}
+
 size_t mosaic_op_mse_scratch_bytes(void) { return mse_scratch_bytes(); }
 
 mosaic_status mosaic_op_mse(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* y, const void* target,

@@ -134,6 +134,29 @@ mosaic_status launch_rope(hipStream_t s, int quota, int dtype, int B, int N, int
 mosaic_status launch_adamw(hipStream_t s, int quota, int dtype, int64_t n, void* p, const void* g,
                            float* m, float* v, float* master, float lr, float beta1, float beta2,
                            float eps, float weight_decay, int64_t step);
+// A norm (NONE: without) over every head of the q and k parts of packed rows, and a rotation by positions with several axes ([n_axes, T]; table null: none);
+// x -> y, which may be x.  direction -1 turns back (NONE).  The backward pass reads the rows before the norm; dx may be dy.
+size_t rope_axes_table_bytes(int d);
+mosaic_status launch_rope_axes_table(hipStream_t s, int quota, int d, int n_axes, const int32_t* sections, int order, float base, void* table);
+mosaic_status launch_qk_norm_rope_fwd(hipStream_t s, int quota, int dtype, int norm, int64_t T, int H, int Hkv, int d, float eps, int pairing, int direction,
+                                      int n_axes, const int32_t* pos, const void* table, const void* x, const void* gq, const void* bq,
+                                      const void* gk, const void* bk, void* y);
+size_t qk_norm_rope_bwd_scratch_bytes(int d);
+mosaic_status launch_qk_norm_rope_bwd(hipStream_t s, int quota, int dtype, int norm, int64_t T, int H, int Hkv, int d, float eps, int pairing, int n_axes,
+                                      const int32_t* pos, const void* table, const void* x, const void* gq, const void* gk, const void* dy, void* dx,
+                                      void* dgq, void* dbq, void* dgk, void* dbk, void* scratch);
+// activations in 8 bits: whole numbers q[n] and an exponent byte for 32 of them
+size_t pack8_scale_bytes(int64_t n);
+mosaic_status launch_pack8(hipStream_t s, int quota, int dtype, int64_t n, const void* x, void* q, void* scale);
+mosaic_status launch_unpack8(hipStream_t s, int quota, int dtype, int64_t n, const void* q, const void* scale, void* x);
+// a = act(z) with z kept in 8 bits; dz and, not null, a again from there
+mosaic_status launch_act_fwd_pack8(hipStream_t s, int quota, int dtype, int act, int64_t T, int64_t f, const void* z, void* a, void* q, void* scale);
+mosaic_status launch_act_bwd_pack8(hipStream_t s, int quota, int dtype, int act, int64_t T, int64_t f, const void* q, const void* scale, const void* da,
+                                   void* dz, void* a);
+// dW[k,n] = X^T dY and, not null, db = column sums of dY, with X[T,k] in 8 bits
+size_t linear_wgrad_pack8_scratch_bytes(int dtype, int64_t T, int64_t k, int64_t n);
+mosaic_status launch_linear_wgrad_pack8(hipStream_t s, int quota, int dtype, int64_t T, int64_t k, int64_t n, const void* q, const void* scale, const void* dY,
+                                        void* dW, void* db, void* scratch);
 // k=3, pad=1 convolution over frames-major [B, L, C] as gather + GEMM: out [B*Lo, 3*C] with
 // column index tap*C + channel; col2im1d is the transposed gather at stride 1 (one owner per element)
 mosaic_status launch_im2col1d(hipStream_t s, int quota, int dtype, int64_t B, int L, int Lo, int C,

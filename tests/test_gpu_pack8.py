@@ -1,0 +1,241 @@
+"""GPU parity of the activation checkpoints in 8 bits: the packed bytes and what they stand for, bit for bit, against the plain
+definition; the activations' and the weight gradient's backward passes from them against 64 bits.
+
+Bounds, u = 2^-24; a bf16 result is off by 2^-8 of its size besides.  GELU: the error function is off by 2 u, so the result by at most 8 u |z|, its
+derivative by 8 u (1 + |z|).  Tanh form: 1 - t^2 is off by 13 u and meets z^3, at most 8.7 before t is 1: 128 u (1 + |z|).
+SwiGLU: an exponential, a sum, a quotient and products, 16 u of the result's size (and 1e-36 where exp overflows); the gate's derivative
+is a sum of two such terms, at most 1 + |gate| in size.  Weight gradient: T additions and products, T u of the sum of magnitudes."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as P
+from paper_2605_18710_amd import synth
+from helpers import from_dev, quantize, to_dev
+from test_gpu_qk_rope import Framed, bits, last, within
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def mb():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2605_18710_amd import binding
+    binding.lib()
+    return binding
+
+
+class Bytes:
+    """n bytes `shift` behind a 16-byte boundary with a frame that must stay."""
+
+    def __init__(self, n, shift=0):
+        self.flat = torch.full((n + 128,), 77, dtype=torch.uint8, device="cuda")
+        self.at = slice(64 + shift, 64 + shift + n)
+        self.t = self.flat[self.at]
+
+    def framed(self):
+        f = self.flat.clone()
+        f[self.at] = 77
+        return bool((f == 77).all())
+
+    def host(self, kind):
+        return self.t.cpu().numpy().view(kind).copy()
+
+
+def values(dtype, n, seed=7000):
+    """Wide in size, with ties, zeros, blocks of tiny numbers, of the type's largest, and of NaN and infinities."""
+    x = synth.normal(seed, (n,)) * np.exp(np.repeat(synth.normal(seed + 1, (n // 32 + 1,), 0.0, 8.0), 32)[:n])
+    x[::7] = np.round(x[::7] * 2) / 2
+    for b, v in ((3, 0.0), (5, 1e-39), (6, 1e-45), (7, 127.5), (8, 255.0), (9, 3.3e38), (10, 2.0 ** -120)):
+        x[32 * b:32 * b + 32] *= 0
+        x[32 * b:32 * b + 32] += v * np.linspace(-1, 1, 32)[:max(0, min(32, n - 32 * b))]
+    for i, v in ((32 * 12 + 3, np.nan), (32 * 13, np.inf), (32 * 14 + 31, -np.inf)):
+        if i < n:
+            x[i] = v
+    with np.errstate(over="ignore"):
+        return quantize(x, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [0, 1, 31, 32, 33, 1000, 4096, 8 * 1031, 65536 + 17])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_pack_and_unpack(mb, dtype, n, shift):
+    x = values(dtype, n) if n else np.zeros(0)
+    q_ref, byte_ref = P.pack8(x)
+    back_ref = P.unpack8(q_ref, byte_ref)
+    for quota in (256, 24):
+        x_ = Framed(x, dtype, shift)
+        q, scale = Bytes(n, shift), Bytes(mb.pack8_scale_bytes(n), shift)
+        mb.op_pack8(None, quota, dtype, n, x_.at_, q.t if n else q.flat, scale.t if n else scale.flat)
+        torch.cuda.synchronize()
+        assert q.framed() and scale.framed() and x_.framed()
+        assert np.array_equal(scale.host(np.uint8), byte_ref)
+        assert np.array_equal(q.host(np.int8), q_ref)
+        for to in ("bf16", "f32"):
+            back = Framed(None, to, shift, (n,))
+            mb.op_unpack8(None, quota, to, n, q.t if n else q.flat, scale.t if n else scale.flat, back.at_)
+            torch.cuda.synchronize()
+            assert back.framed()
+            assert np.array_equal(from_dev(back.t), back_ref, equal_nan=True)          # exact in either type
+
+
+def act_ref(act, z, da):
+    """a, dz, and the sizes that their bounds count."""
+    if act == "swiglu":
+        f = z.shape[1] // 2
+        gate, up = z[:, :f], z[:, f:]
+        with np.errstate(over="ignore"):
+            s = 1.0 / (1.0 + np.exp(-gate))
+        a = gate * s * up
+        dz = np.concatenate([da * up * s * (1 + gate * (1 - s)), da * gate * s], axis=1)
+        size = np.concatenate([np.abs(da * up) * s * (1 + np.abs(gate) * (1 - s)), np.abs(da * gate) * s], axis=1)
+        return a, dz, 16 * U * np.abs(a) + 1e-36 * (1 + np.abs(gate * up)), 16 * U * size + 1e-36 * (1 + np.abs(np.concatenate([up * da * gate, da * gate], axis=1)))
+    if act == "gelu":
+        p = 0.5 * np.vectorize(math.erfc)(-z * math.sqrt(0.5)) if z.size else z
+        return z * p, da * (p + z * np.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)), 8 * U * np.abs(z), 8 * U * (1 + np.abs(z)) * np.abs(da)
+    c = math.sqrt(2 / math.pi)
+    t = np.tanh(c * (z + 0.044715 * z ** 3))
+    dz = da * (0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z))
+    return 0.5 * z * (1 + t), dz, 8 * U * np.abs(z), 128 * U * (1 + np.abs(z)) * np.abs(da)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "swiglu"])
+@pytest.mark.parametrize("T,f", [(1, 1), (1, 32), (3, 40), (5, 64), (17, 24), (2, 1000), (7, 33), (0, 64), (65, 1056)])
+def test_activation(mb, dtype, act, T, f):
+    width = 2 * f if act == "swiglu" else f
+    z = quantize(synth.normal(7100, (T, width), 0.0, 2.0) * np.exp(synth.normal(7101, (width,))), dtype)
+    if T > 2:
+        z[1] = 0.0
+        z[2, : width // 2] = quantize(synth.normal(7102, (width // 2,), 0.0, 60.0), dtype)
+    da = quantize(synth.normal(7103, (T, f)), dtype)
+    q_ref, byte_ref = P.pack8(z)
+    kept = P.unpack8(q_ref, byte_ref).reshape(z.shape)
+    a_ref, _, a_tol, _ = act_ref(act, z, da)
+    again_ref, dz_ref, again_tol, dz_tol = act_ref(act, kept, da)
+    n = T * width
+    outs = []
+    for quota, shift in ((256, 0), (24, 0), (256, 1)):
+        z_, da_ = Framed(z, dtype, shift), Framed(da, dtype, shift)
+        a, again, dz = Framed(None, dtype, shift, (T, f)), Framed(None, dtype, shift, (T, f)), Framed(None, dtype, shift, (T, width))
+        alone = Framed(None, dtype, shift, (T, width))
+        q, scale = Bytes(n, shift), Bytes(mb.pack8_scale_bytes(n), shift)
+        pq, ps = (q.t, scale.t) if n else (q.flat, scale.flat)
+        at = lambda framed: framed.at_
+        mb.op_act_fwd_pack8(None, quota, dtype, act, T, f, at(z_), at(a), pq, ps)
+        mb.op_act_bwd_pack8(None, quota, dtype, act, T, f, pq, ps, at(da_), at(dz), at(again))
+        mb.op_act_bwd_pack8(None, quota, dtype, act, T, f, pq, ps, at(da_), at(alone))
+        torch.cuda.synchronize()
+        if act != "swiglu":
+            mb.op_act_bwd_pack8(None, quota, dtype, act, T, f, pq, ps, at(da_), at(da_))      # over the gradient that it reads
+            torch.cuda.synchronize()
+            assert np.array_equal(bits(da_.t), bits(dz.t))
+        assert all(b.framed() for b in (z_, da_, a, again, dz, alone, q, scale))
+        assert np.array_equal(q.host(np.int8), q_ref) and np.array_equal(scale.host(np.uint8), byte_ref)
+        assert np.array_equal(bits(alone.t), bits(dz.t))
+        if n:
+            within(from_dev(a.t), a_ref, last(dtype, a_ref) + a_tol, ("a", shift))
+            within(from_dev(again.t), again_ref, last(dtype, again_ref) + again_tol, ("again", shift))
+            within(from_dev(dz.t), dz_ref, last(dtype, dz_ref) + dz_tol, ("dz", shift))
+        outs.append([bits(a.t), bits(again.t), bits(dz.t)])
+    assert all(np.array_equal(x, y) for x, y in zip(outs[0], outs[1]))
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "swiglu"])
+def test_activation_of_a_block_with_nan(mb, act):
+    """The forward result of what is finite stays; the block comes back as NaN, in the gradient and in the activation formed again."""
+    T, f = 4, 64
+    width = 2 * f if act == "swiglu" else f
+    z = quantize(synth.normal(7200, (T, width)), "bf16")
+    z[2, 40] = np.inf
+    z_, da = to_dev(z, "bf16"), torch.ones((T, f), dtype=torch.bfloat16, device="cuda")
+    a, again, dz = torch.empty_like(da), torch.empty_like(da), torch.empty_like(z_)
+    q, scale = torch.empty(T * width, dtype=torch.int8, device="cuda"), torch.empty(T * width // 32, dtype=torch.uint8, device="cuda")
+    mb.op_act_fwd_pack8(None, 256, "bf16", act, T, f, z_, a, q, scale)
+    mb.op_act_bwd_pack8(None, 256, "bf16", act, T, f, q, scale, da, dz, again)
+    bad = np.isnan(from_dev(again))
+    assert bad[2, 32:64].all() and bad.sum() == 32
+    bad = np.isnan(from_dev(dz))
+    assert bad[2, 32:64].all() and bad.sum() == (64 if act == "swiglu" else 32)
+    fine = np.isfinite(from_dev(a))
+    fine[2, 40] = True
+    assert fine.all()
+
+
+@pytest.mark.parametrize("dtype,T,k,n,db", [("bf16", 1, 8, 8, True), ("bf16", 37, 64, 72, True), ("bf16", 300, 136, 256, False), ("bf16", 1500, 320, 264, True),
+                                            ("bf16", 5, 33, 7, True), ("bf16", 513, 256, 512, True), ("f32", 1, 1, 1, True), ("f32", 70, 20, 12, True),
+                                            ("f32", 257, 128, 64, False), ("bf16", 64, 128, 128, True), ("bf16", 2100, 512, 512, False)])
+def test_weight_gradient(mb, dtype, T, k, n, db):
+    x = quantize(synth.normal(7300, (T, k)) * np.exp(synth.normal(7301, (k,))), dtype)
+    if T > 4:
+        x[T - 3:] = 0.0
+    dy = quantize(synth.normal(7302, (T, n)), dtype)
+    q, byte = P.pack8(x)
+    kept = P.unpack8(q, byte).reshape(T, k)
+    outs = []
+    for quota in (256, 24):
+        q_, s_ = Bytes(T * k), Bytes(byte.size)
+        q_.t.copy_(torch.from_numpy(q.view(np.uint8))); s_.t.copy_(torch.from_numpy(byte))
+        dw, bias = Framed(None, dtype, 0, (k, n)), Framed(None, dtype, 0, (n,))
+        scratch = Bytes(mb.linear_wgrad_pack8_scratch_bytes(dtype, T, k, n))
+        if db and n % (8 if dtype == "bf16" else 4):         # column sums of such rows are refused, before anything is launched
+            with pytest.raises(mb.MosaicError) as e:
+                mb.op_linear_wgrad_pack8(None, quota, dtype, T, k, n, q_.t, s_.t, to_dev(dy, dtype), dw.t, bias.t, scratch.t)
+            assert e.value.status == mb.EUNSUPPORTED
+            torch.cuda.synchronize()
+            assert (dw.t == 7.0).all() and (bias.t == 7.0).all()
+            db = False
+        mb.op_linear_wgrad_pack8(None, quota, dtype, T, k, n, q_.t, s_.t, to_dev(dy, dtype), dw.t, bias.t if db else None, scratch.t)
+        torch.cuda.synchronize()
+        assert dw.framed() and bias.framed() and scratch.framed() and q_.framed() and s_.framed()
+        outs.append((bits(dw.t), bits(bias.t)))
+    assert all(np.array_equal(a, b) for a, b in zip(outs[0], outs[1]))
+    ref = kept.T @ dy
+    within(from_dev(dw.t), ref, last(dtype, ref) + (T + 8) * U * (np.abs(kept).T @ np.abs(dy)), "dw")
+    if db:
+        within(from_dev(bias.t), dy.sum(0), last(dtype, dy.sum(0)) + (T + 8) * U * np.abs(dy).sum(0), "db")
+    else:
+        assert (bias.t == 7.0).all()
+
+
+def test_captured_and_replayed(mb):
+    T, k, n, f = 200, 64, 72, 96
+    x, dy = to_dev(quantize(synth.normal(7400, (T, k)), "bf16"), "bf16"), to_dev(quantize(synth.normal(7401, (T, n)), "bf16"), "bf16")
+    z, da = to_dev(quantize(synth.normal(7402, (T, 2 * f)), "bf16"), "bf16"), to_dev(quantize(synth.normal(7403, (T, f)), "bf16"), "bf16")
+    byte = lambda size: torch.empty(size, dtype=torch.uint8, device="cuda")
+    xq, xs, zq, zs = byte(T * k), byte(T * k // 32), byte(T * 2 * f), byte(T * 2 * f // 32)
+    out = dict(a=torch.empty_like(da), dz=torch.empty_like(z), again=torch.empty_like(da), dw=torch.empty((k, n), dtype=torch.bfloat16, device="cuda"),
+               db=torch.empty(n, dtype=torch.bfloat16, device="cuda"))
+    scratch = byte(mb.linear_wgrad_pack8_scratch_bytes("bf16", T, k, n))
+
+    def step(stream):
+        mb.op_act_fwd_pack8(stream, 256, "bf16", "swiglu", T, f, z, out["a"], zq, zs)
+        mb.op_pack8(stream, 256, "bf16", T * k, x, xq, xs)
+        mb.op_act_bwd_pack8(stream, 256, "bf16", "swiglu", T, f, zq, zs, da, out["dz"], out["again"])
+        mb.op_linear_wgrad_pack8(stream, 256, "bf16", T, k, n, xq, xs, dy, out["dw"], out["db"], scratch)
+
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        step(s.cuda_stream)
+        s.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            step(torch.cuda.current_stream().cuda_stream)
+    for turn in range(3):
+        for t, seed in ((x, 0), (z, 1), (dy, 2)):
+            t.copy_(to_dev(quantize(synth.normal(7500 + 3 * turn + seed, tuple(t.shape)), "bf16"), "bf16"))
+        torch.cuda.synchronize()
+        step(None)
+        torch.cuda.synchronize()
+        want = {name: bits(t) for name, t in out.items()}
+        for t in (*out.values(), xq, xs, zq, zs):
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, t in out.items():
+            assert np.array_equal(want[name], bits(t)), name
