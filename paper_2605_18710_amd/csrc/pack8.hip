@@ -4,6 +4,8 @@
 // whole numbers q nearest to x / 2^e (ties to even, at most 127 in size): an element is off by half of 2^e at most, and
 // q * 2^e is a bf16 number, so that unpacking rounds nothing.  x / 2^e is exact too: the bits do not depend on how it is computed.  A block
 // with a NaN or an infinity has the byte 255 and comes back as NaN.
+#include <initializer_list>
+#include <type_traits>
 #include "kernels.h"
 #include "activations.h"
 
@@ -27,6 +29,120 @@ __device__ __forceinline__ float inverse_step(int byte) {     // 2^-e; e is 122 
 __device__ __forceinline__ int packed(float x, float inverse) {
   const float v = rintf(x * inverse);
   return v != v ? 0 : (int)fminf(fmaxf(v, -127.f), 127.f);
+}
+
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive elements in fp32: 16 bytes of bf16, 32 of fp32.
+template <bool PAST> __device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
+  Vec16<bf16> x;
+  x.load<PAST>(p);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = x.get(k);
+}
+template <bool PAST> __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+  Vec16<float> x, y;
+  x.load<PAST>(p);
+  y.load<PAST>(p + 4);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { v[k] = x.get(k); v[4 + k] = y.get(k); }
+}
+template <bool PAST> __device__ __forceinline__ void store8(bf16* p, const float (&v)[8]) {
+  Vec16<bf16> x;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x.set(k, v[k]);
+  x.store<PAST>(p);
+}
+template <bool PAST> __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+  Vec16<float> x, y;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { x.set(k, v[k]); y.set(k, v[4 + k]); }
+  x.store<PAST>(p);
+  y.store<PAST>(p + 4);
+}
+// the same, of an array that ends within the eight
+template <bool PAST, typename T> __device__ __forceinline__ void load8(const T* p, int64_t left, float (&v)[8]) {
+  if (left >= 8) return load8<PAST>(p, v);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = k < left ? to_f32(p[k]) : 0.f;
+}
+template <bool PAST, typename T> __device__ __forceinline__ void store8(T* p, int64_t left, const float (&v)[8]) {
+  if (left >= 8) return store8<PAST>(p, v);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < left) p[k] = from_f32<T>(v[k]);
+}
+
+// Packs the eight elements of each of a block's four lanes (a quad): its exponent byte, and the numbers in two words.  Within 127 the number added to
+// 1.5 * 2^23 is rounded to a whole one, ties to even, and stands in the sum's low byte.
+__device__ __forceinline__ int pack_quad(const float (&v)[8], u32x2* q) {
+  unsigned top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+  top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, true));
+  top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, true));
+  const int byte = scale_byte(top);
+  const float inverse = inverse_step(byte);
+  unsigned w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(__builtin_amdgcn_fmed3f(v[4 * h + k] * inverse, -127.f, 127.f) + 12582912.f);
+    const unsigned lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
+    w[h] = byte == 255 ? 0u : lo | hi;
+  }
+  *q = u32x2{w[0], w[1]};
+  return byte;
+}
+// the eight values of two words; (number + 128) * step - 128 * step in one operation would overflow in blocks of the largest numbers
+__device__ __forceinline__ void unpack8_of(u32x2 q, int byte, float (&v)[8]) {
+  const float step = step_of(byte);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const unsigned w = (h ? q.y : q.x) ^ 0x80808080u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[4 * h + k] = ((float)(w >> (8 * k) & 0xffu) - 128.f) * step;
+  }
+}
+__device__ __forceinline__ void put_tail(int8_t* p, int64_t left, u32x2 q) {
+  for (int k = 0; k < 8; ++k)
+    if (k < left) p[k] = (int8_t)((k < 4 ? q.x : q.y) >> (8 * (k & 3)));
+}
+__device__ __forceinline__ u32x2 get_tail(const int8_t* p, int64_t left) {
+  u32x2 q = {0u, 0u};
+  for (int k = 0; k < 8; ++k)
+    if (k < left) { if (k < 4) q.x |= (unsigned)(uint8_t)p[k] << (8 * k); else q.y |= (unsigned)(uint8_t)p[k] << (8 * (k - 4)); }
+  return q;
+}
+
+// 16-byte aligned arrays of any size: a lane takes eight elements, a quad of lanes a block.  `vectors`: eights, rounded up to whole blocks, so that a
+// quad's lanes take part together.
+template <typename T, bool PAST>
+__global__ __launch_bounds__(kThreads) void pack8_kernel(const T* __restrict__ x, int8_t* __restrict__ q, uint8_t* __restrict__ scale, int64_t n, int64_t vectors) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t left = n - i * 8;
+    float v[8];
+    load8<PAST>(x + i * 8, left, v);
+    u32x2 w;
+    const int byte = pack_quad(v, &w);
+    if (left >= 8) store_to<PAST>((u32x2*)(q + i * 8), w);
+    else put_tail(q + i * 8, left, w);
+    if (i % 4 == 0) scale[i / 4] = (uint8_t)byte;
+  }
+}
+
+template <typename T, bool PAST>
+__global__ __launch_bounds__(kThreads) void unpack8_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ scale, T* __restrict__ x, int64_t n, int64_t vectors) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t left = n - i * 8;
+    if (left <= 0) continue;
+    const u32x2 w = left >= 8 ? load_from<PAST>((const u32x2*)(q + i * 8)) : get_tail(q + i * 8, left);
+    float v[8];
+    unpack8_of(w, scale[i / 4], v);
+    store8<PAST>(x + i * 8, left, v);
+  }
 }
 
 // any size and alignment: a thread takes an element, 32 lanes a block
@@ -94,6 +210,112 @@ __global__ __launch_bounds__(kThreads) void act_bwd_any_kernel(const int8_t* __r
   }
 }
 
+// (row, column) of the i-th eight of rows of fv eights
+__device__ __forceinline__ void place(int64_t i, int64_t fv, int64_t* r, int64_t* c) {
+  if ((uint64_t)(i | fv) >> 32 == 0) {                    // the same for all lanes but where an array passes 2^32 eights
+    const uint32_t q = (uint32_t)i / (uint32_t)fv;
+    *r = q;
+    *c = (uint32_t)i - q * (uint32_t)fv;
+  } else {
+    *r = i / fv;
+    *c = i - *r * fv;
+  }
+}
+
+// a = act(z) and z in 8 bits.  GELU forms: flat, any size.  SwiGLU: rows of f = 8 fv, f a multiple of 32, so that no block has elements of both halves.
+template <typename T, int ACT, bool PAST>
+__global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__ z, T* __restrict__ a, int8_t* __restrict__ q, uint8_t* __restrict__ scale,
+                                                           int64_t n, int64_t vectors, int64_t fv) {
+  constexpr bool TAB = ACT == MOSAIC_GELU && sizeof(T) == 2;
+  __shared__ float table[TAB ? ErfTable::kEntries : 1];
+  if constexpr (TAB) { ErfTable::fill(table, threadIdx.x, kThreads); __syncthreads(); }
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
+    float v[8], o[8];
+    u32x2 w;
+    if constexpr (ACT == MOSAIC_SWIGLU) {
+      int64_t r, c;
+      place(i, fv, &r, &c);
+      const int64_t at = (r * 2 * fv + c) * 8, up = at + fv * 8;
+      float u[8];
+      load8<PAST>(z + at, v);
+      load8<PAST>(z + up, u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = swiglu_f(v[k], u[k]);
+      store8<PAST>(a + i * 8, o);
+      u32x2 wu;
+      const int bg = pack_quad(v, &w), bu = pack_quad(u, &wu);
+      store_to<PAST>((u32x2*)(q + at), w);
+      store_to<PAST>((u32x2*)(q + up), wu);
+      if (c % 4 == 0) { scale[at / kBlock] = (uint8_t)bg; scale[up / kBlock] = (uint8_t)bu; }
+    } else {
+      const int64_t left = n - i * 8;
+      load8<PAST>(z + i * 8, left, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if constexpr (TAB) o[k] = ErfTable::gelu(table, v[k]);
+        else o[k] = act_of<ACT>(v[k]);
+      }
+      store8<PAST>(a + i * 8, left, o);
+      const int byte = pack_quad(v, &w);
+      if (left >= 8) store_to<PAST>((u32x2*)(q + i * 8), w);
+      else put_tail(q + i * 8, left, w);
+      if (i % 4 == 0) scale[i / 4] = (uint8_t)byte;
+    }
+  }
+}
+
+// dz = act'(z) da and, where asked for, a = act(z), with z from its 8 bits; SwiGLU: rows of f = 8 fv
+template <typename T, int ACT, bool PAST, bool AGAIN>
+__global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ scale, const T* da, T* dz, T* __restrict__ a,
+                                                           int64_t n, int64_t vectors, int64_t fv) {
+  constexpr bool TAB = ACT == MOSAIC_GELU && sizeof(T) == 2;      // unpacked numbers are bf16 numbers
+  __shared__ float table[TAB ? ErfTable::kEntries : 1];
+  if constexpr (TAB) { ErfTable::fill(table, threadIdx.x, kThreads); __syncthreads(); }
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
+    float z[8], d[8], o[8];
+    if constexpr (ACT == MOSAIC_SWIGLU) {
+      int64_t r, c;
+      place(i, fv, &r, &c);
+      const int64_t at = (r * 2 * fv + c) * 8, up = at + fv * 8;
+      float u[8], og[8], ou[8];
+      const u32x2 wg = load_from<PAST>((const u32x2*)(q + at)), wu = load_from<PAST>((const u32x2*)(q + up));
+      const int bg = scale[at / kBlock], bu = scale[up / kBlock];
+      load8<PAST>(da + i * 8, d);
+      unpack8_of(wg, bg, z);
+      unpack8_of(wu, bu, u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        swiglu_grad_f(z[k], u[k], d[k], &og[k], &ou[k]);
+        if constexpr (AGAIN) o[k] = swiglu_f(z[k], u[k]);
+      }
+      store8<PAST>(dz + at, og);
+      store8<PAST>(dz + up, ou);
+      if constexpr (AGAIN) store8<PAST>(a + i * 8, o);
+    } else {
+      const int64_t left = n - i * 8;
+      if (left <= 0) continue;
+      const u32x2 w = left >= 8 ? load_from<PAST>((const u32x2*)(q + i * 8)) : get_tail(q + i * 8, left);
+      const int byte = scale[i / 4];
+      load8<PAST>(da + i * 8, left, d);
+      unpack8_of(w, byte, z);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if constexpr (TAB) d[k] *= ErfTable::gelu_grad(table, z[k]);
+        else d[k] *= act_grad_of<ACT>(z[k]);
+        if constexpr (AGAIN) o[k] = TAB ? ErfTable::gelu(table, z[k]) : act_of<ACT>(z[k]);
+      }
+      store8<PAST>(dz + i * 8, left, d);
+      if constexpr (AGAIN) store8<PAST>(a + i * 8, left, o);
+    }
+  }
+}
+
+bool on16(std::initializer_list<const void*> pointers) {
+  uintptr_t bits = 0;
+  for (const void* p : pointers) bits |= (uintptr_t)p;
+  return bits % 16 == 0;
+}
+
 }  // namespace
 
 size_t pack8_scale_bytes(int64_t n) { return (size_t)ceil_div(n, kBlock); }
@@ -101,18 +323,36 @@ size_t pack8_scale_bytes(int64_t n) { return (size_t)ceil_div(n, kBlock); }
 mosaic_status launch_pack8(hipStream_t s, int quota, int dtype, int64_t n, const void* x, void* q, void* scale) {
   if (n == 0) return MOSAIC_OK;
   const int64_t blocks = ceil_div(n, kBlock);
-  const int grid = grid_for(quota, 8, ceil_div(n, kThreads));
-  if (dtype == MOSAIC_BF16) pack8_any_kernel<bf16><<<grid, kThreads, 0, s>>>((const bf16*)x, (int8_t*)q, (uint8_t*)scale, n, blocks);
-  else pack8_any_kernel<float><<<grid, kThreads, 0, s>>>((const float*)x, (int8_t*)q, (uint8_t*)scale, n, blocks);
+  auto launch = [&](auto type) {
+    typedef decltype(type) E;
+    if (!on16({x, q})) {
+      pack8_any_kernel<E><<<grid_for(quota, 8, ceil_div(n, kThreads)), kThreads, 0, s>>>((const E*)x, (int8_t*)q, (uint8_t*)scale, n, blocks);
+      return;
+    }
+    const int64_t vectors = blocks * (kBlock / 8), bytes = n * (int64_t)(sizeof(E) + 1);
+    const Sweep sw = sweep_grid(s, quota, ceil_div(vectors, kThreads), bytes);
+    if (sw.in_order && bytes > kPastCacheBytes) pack8_kernel<E, true><<<sw.grid, kThreads, 0, s>>>((const E*)x, (int8_t*)q, (uint8_t*)scale, n, vectors);
+    else pack8_kernel<E, false><<<sw.grid, kThreads, 0, s>>>((const E*)x, (int8_t*)q, (uint8_t*)scale, n, vectors);
+  };
+  if (dtype == MOSAIC_BF16) launch(bf16{}); else launch(float{});
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
 
 mosaic_status launch_unpack8(hipStream_t s, int quota, int dtype, int64_t n, const void* q, const void* scale, void* x) {
   if (n == 0) return MOSAIC_OK;
-  const int grid = grid_for(quota, 8, ceil_div(n, kThreads));
-  if (dtype == MOSAIC_BF16) unpack8_any_kernel<bf16><<<grid, kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (bf16*)x, n);
-  else unpack8_any_kernel<float><<<grid, kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (float*)x, n);
+  auto launch = [&](auto type) {
+    typedef decltype(type) E;
+    if (!on16({x, q})) {
+      unpack8_any_kernel<E><<<grid_for(quota, 8, ceil_div(n, kThreads)), kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (E*)x, n);
+      return;
+    }
+    const int64_t vectors = ceil_div(n, 8), bytes = n * (int64_t)(sizeof(E) + 1);
+    const Sweep sw = sweep_grid(s, quota, ceil_div(vectors, kThreads), bytes);
+    if (sw.in_order && bytes > kPastCacheBytes) unpack8_kernel<E, true><<<sw.grid, kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (E*)x, n, vectors);
+    else unpack8_kernel<E, false><<<sw.grid, kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (E*)x, n, vectors);
+  };
+  if (dtype == MOSAIC_BF16) launch(bf16{}); else launch(float{});
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -131,22 +371,57 @@ template <typename F> void of_type_and_act(int dtype, int act, F launch) {
 
 mosaic_status launch_act_fwd_pack8(hipStream_t s, int quota, int dtype, int act, int64_t T, int64_t f, const void* z, void* a, void* q, void* scale) {
   if (T * f == 0) return MOSAIC_OK;
-  const int grid = grid_for(quota, 8, ceil_div(T * f, kThreads));
-  of_type_and_act(dtype, act, [&](auto type, auto kind) {
-    typedef decltype(type) E;
-    act_fwd_any_kernel<E, decltype(kind)::value><<<grid, kThreads, 0, s>>>((const E*)z, (E*)a, T, f);
-  });
-  MOSAIC_LAUNCH_CHECK();
-  return launch_pack8(s, quota, dtype, act == MOSAIC_SWIGLU ? 2 * T * f : T * f, z, q, scale);
+  const bool glu = act == MOSAIC_SWIGLU, whole = !glu || f % kBlock == 0;
+  const int64_t m = T * f, n = glu ? 2 * m : m;
+  if (whole && on16({z, a, q})) {
+    of_type_and_act(dtype, act, [&](auto type, auto kind) {
+      typedef decltype(type) E;
+      constexpr int ACT = decltype(kind)::value;
+      const int64_t vectors = glu ? m / 8 : ceil_div(n, kBlock) * (kBlock / 8), blocks = ceil_div(vectors, kThreads), bytes = (n + m) * (int64_t)sizeof(E) + n;
+      const bool table = ACT == MOSAIC_GELU && sizeof(E) == 2;          // filled by every workgroup: few of them
+      const Sweep sw = table ? Sweep{grid_for(quota, 8, blocks), false} : sweep_grid(s, quota, blocks, bytes);
+      auto with = [&](auto past) {
+        act_fwd_kernel<E, ACT, decltype(past)::value><<<sw.grid, kThreads, 0, s>>>((const E*)z, (E*)a, (int8_t*)q, (uint8_t*)scale, n, vectors, f / 8);
+      };
+      if (sw.in_order && bytes > kPastCacheBytes) with(std::true_type{}); else with(std::false_type{});
+    });
+    MOSAIC_LAUNCH_CHECK();
+    return MOSAIC_OK;
+  }
+  const int64_t vn = 16 / (int64_t)dtype_size(dtype);
+  if (glu && f % vn == 0 && on16({z, a})) MOSAIC_TRY(launch_swiglu_fwd(s, quota, dtype, T, f, z, a));
+  else {
+    const int grid = grid_for(quota, 8, ceil_div(m, kThreads));
+    of_type_and_act(dtype, act, [&](auto type, auto kind) {
+      typedef decltype(type) E;
+      act_fwd_any_kernel<E, decltype(kind)::value><<<grid, kThreads, 0, s>>>((const E*)z, (E*)a, T, f);
+    });
+    MOSAIC_LAUNCH_CHECK();
+  }
+  return launch_pack8(s, quota, dtype, n, z, q, scale);
 }
 
 mosaic_status launch_act_bwd_pack8(hipStream_t s, int quota, int dtype, int act, int64_t T, int64_t f, const void* q, const void* scale, const void* da,
                                    void* dz, void* a) {
   if (T * f == 0) return MOSAIC_OK;
-  const int grid = grid_for(quota, 8, ceil_div(T * f, kThreads));
+  const bool glu = act == MOSAIC_SWIGLU, whole = !glu || f % 8 == 0;
+  const int64_t m = T * f, n = glu ? 2 * m : m;
   of_type_and_act(dtype, act, [&](auto type, auto kind) {
     typedef decltype(type) E;
-    act_bwd_any_kernel<E, decltype(kind)::value><<<grid, kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (const E*)da, (E*)dz, (E*)a, T, f);
+    constexpr int ACT = decltype(kind)::value;
+    if (!whole || !on16({q, da, dz, a})) {
+      act_bwd_any_kernel<E, ACT><<<grid_for(quota, 8, ceil_div(m, kThreads)), kThreads, 0, s>>>((const int8_t*)q, (const uint8_t*)scale, (const E*)da, (E*)dz, (E*)a, T, f);
+      return;
+    }
+    const int64_t vectors = ceil_div(m, 8), blocks = ceil_div(vectors, kThreads), bytes = n + (n + (a ? 2 : 1) * m) * (int64_t)sizeof(E);
+    const bool table = ACT == MOSAIC_GELU && sizeof(E) == 2;
+    const Sweep sw = table ? Sweep{grid_for(quota, 8, blocks), false} : sweep_grid(s, quota, blocks, bytes);
+    auto with = [&](auto past, auto again) {
+      act_bwd_kernel<E, ACT, decltype(past)::value, decltype(again)::value><<<sw.grid, kThreads, 0, s>>>(
+          (const int8_t*)q, (const uint8_t*)scale, (const E*)da, (E*)dz, (E*)a, n, vectors, f / 8);
+    };
+    auto of_past = [&](auto past) { if (a) with(past, std::true_type{}); else with(past, std::false_type{}); };
+    if (sw.in_order && bytes > kPastCacheBytes) of_past(std::true_type{}); else of_past(std::false_type{});
   });
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
