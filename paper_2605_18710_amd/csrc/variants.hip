@@ -4,11 +4,20 @@
 // every output element has one owner, so results do not depend on the grid.
 #include <type_traits>
 #include "kernels.h"
-#include "activations.h"
 
 namespace {
 
 constexpr int kThreads = 256;
+
+__device__ __forceinline__ float tanh_gelu_f(float z) {
+  const float u = 0.7978845608028654f * (z + 0.044715f * z * z * z);
+  return 0.5f * z * (1.0f + tanhf(u));
+}
+__device__ __forceinline__ float tanh_gelu_grad_f(float z) {
+  const float u = 0.7978845608028654f * (z + 0.044715f * z * z * z);
+  const float t = tanhf(u);
+  return 0.5f * (1.0f + t) + 0.5f * z * (1.0f - t * t) * 0.7978845608028654f * (1.0f + 3.0f * 0.044715f * z * z);
+}
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void gelu_tanh_fwd_kernel(const T* __restrict__ z, T* __restrict__ a, int64_t nvec) {
