@@ -10,16 +10,6 @@
 #include <initializer_list>
 #include <math.h>
 #include "kernels.h"
-#ifndef BOCC
-#define BOCC 1
-#endif
-#ifndef FW
-#define FW 16
-#endif
-#ifndef BW
-#define BW 8
-#endif
-
 namespace {
 
 constexpr int kThreads = 256;
@@ -35,6 +25,7 @@ struct PairTurn {
   double turns;
   int axis, unused;
 };
+static_assert(kMaxAxes == 4, "positions are chosen from four");
 static_assert(sizeof(PairTurn) == 16, "an entry of the table");
 
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -136,13 +127,17 @@ template <typename T, int VE, int LPH, bool HALVES> struct Share {
   }
   // The token's turns: each pair's by one lane, through LDS that only this wave uses.
   __device__ __forceinline__ void turns(const Positions& at, const PairTurn (&mine)[2], int64_t t, Turn* lds, float (&c)[VE], float (&s)[VE]) const {
+    int pos[kMaxAxes];                                   // wave-wide, and asked for without waiting for the table
+#pragma unroll
+    for (int a = 0; a < kMaxAxes; ++a) pos[a] = at.pos[min(a, at.n_axes - 1) * at.T + t];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int i = (threadIdx.x & 63) + 64 * u;
       if (i < half) {
         Turn r = {1.f, 0.f};
         if (mine[u].axis >= 0) {
-          double turns = (double)at.pos[mine[u].axis * at.T + t] * mine[u].turns;
+          const int axis = mine[u].axis;
+          double turns = (double)(axis == 0 ? pos[0] : axis == 1 ? pos[1] : axis == 2 ? pos[2] : pos[3]) * mine[u].turns;
           turns -= rint(turns);
           sincospif(2.f * (float)turns, &r.s, &r.c);
         }
@@ -546,7 +541,13 @@ __global__ __launch_bounds__(kThreads) void qk_bwd_any_kernel(const T* __restric
   }
 }
 
-// launch(elements of a vector, lanes of a head) where heads are whole vectors of 16 bytes in each half (bf16 also 8) and all addresses lie on them
+// Past the caches what they do not hold, where a half of a head is whole lines of 128 bytes: a lane's two vectors lie half a head apart, and parts of lines go
+// past the caches one by one.  bf16, 32768 tokens of 48 heads of 128: forward 150 -> 139 us, backward 251 -> 237; 36864 tokens of 48 heads of 64 85 -> 94.
+template <typename T> bool past_caches(int d, int64_t bytes) { return bytes > kPastCacheBytes && d / 2 * (int)sizeof(T) % 128 == 0; }
+
+// launch(elements of a vector, lanes of a head) where each half of a head is whole vectors and all addresses lie on them.  kBytes: of a vector of bf16; 8 where
+// d is no multiple of 16.  The backward pass takes 8 everywhere: with 16 a lane's sums and values leave room for half the waves (12000 tokens, 20 heads
+// of 64, LayerNorm 83 us, with 8 62; 32768 tokens of 32 + 8 heads of 128 232 and 237, on 64 CUs 574 and 505).  Forward 16 / 8: 139 / 146 us.
 template <typename T, int kBytes, typename F> bool with_vectors(int64_t width, int d, std::initializer_list<const void*> pointers, F launch) {
   constexpr int kWide = (kBytes < 16 && sizeof(T) == 2 ? 8 : 16) / (int)sizeof(T);
   uintptr_t bits = 0;
@@ -587,7 +588,7 @@ mosaic_status launch_qk_norm_rope_fwd(hipStream_t s, int quota, int dtype, int n
   if (T > 0) {
     auto launch = [&](auto type, auto kind, auto halves) {
       typedef decltype(type) E;
-      const bool vectors = with_vectors<E, FW>((int64_t)(H + 2 * Hkv) * d, d, {x, y, gq, gk, bq, bk}, [&](auto ve, auto lph) {
+      const bool vectors = with_vectors<E, 16>((int64_t)(H + 2 * Hkv) * d, d, {x, y, gq, gk, bq, bk}, [&](auto ve, auto lph) {
         constexpr int VE = decltype(ve)::value, LPH = decltype(lph)::value;
         const int groups = (int)ceil_div(heads, 64 / LPH);
         // few tokens: their groups of heads apart, as far as there are waves for them
@@ -599,7 +600,7 @@ mosaic_status launch_qk_norm_rope_fwd(hipStream_t s, int quota, int dtype, int n
               (const E*)x, (E*)y, at, H, Hkv, d, heads, per_chunk, (int)ceil_div(groups, per_chunk), eps, (float)direction,
               (const E*)gq, (const E*)bq, (const E*)gk, (const E*)bk);
         };
-        if (sw.in_order && bytes > kPastCacheBytes) with(std::true_type{}); else with(std::false_type{});
+        if (sw.in_order && past_caches<E>(d, bytes)) with(std::true_type{}); else with(std::false_type{});
       });
       if (vectors) return;
       const int grid = grid_for(quota, 8, ceil_div(T * heads, kWaves));
@@ -628,17 +629,18 @@ mosaic_status launch_qk_norm_rope_bwd(hipStream_t s, int quota, int dtype, int n
   if (T > 0) {
     auto launch = [&](auto type, auto kind, auto halves) {
       typedef decltype(type) E;
-      const bool vectors = with_vectors<E, BW>((int64_t)(H + 2 * Hkv) * d, d, {x, dy, dx, gq, gk}, [&](auto ve, auto lph) {
+      const bool vectors = with_vectors<E, 8>((int64_t)(H + 2 * Hkv) * d, d, {x, dy, dx, gq, gk}, [&](auto ve, auto lph) {
         constexpr int VE = decltype(ve)::value, LPH = decltype(lph)::value;
         const int64_t bytes = T * (2 * heads + H + Hkv) * d * (int64_t)sizeof(E);
         const int parts = dx == dy ? 2 : 3;            // in place, v lies where it should
-        np = (int)std::min<int64_t>(kMaxParts, ceil_div(T, kWavesBwd));
+        const int64_t each = ceil_div(T, (int64_t)kMaxParts * kWavesBwd);      // tokens of a wave: as many for all
+        np = (int)ceil_div(T, each * kWavesBwd);
         const int grid = grid_for(quota, 4, (int64_t)parts * np);
         auto with = [&](auto past) {
           qk_bwd_kernel<E, VE, LPH, decltype(kind)::value, decltype(halves)::value, decltype(past)::value><<<grid, kThreadsBwd, 0, s>>>(
               (const E*)x, (const E*)dy, (E*)dx, at, H, Hkv, d, parts, eps, (const E*)gq, (const E*)gk, (float*)scratch, np);
         };
-        if (bytes > kPastCacheBytes) with(std::true_type{}); else with(std::false_type{});
+        if (past_caches<E>(d, bytes)) with(std::true_type{}); else with(std::false_type{});
       });
       if (vectors) return;
       const int rp = (int)std::max<int64_t>(kWaves, ceil_div(T, kMaxParts));
