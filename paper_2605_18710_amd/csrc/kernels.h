@@ -157,6 +157,9 @@ mosaic_status launch_act_bwd_pack8(hipStream_t s, int quota, int dtype, int act,
 size_t linear_wgrad_pack8_scratch_bytes(int dtype, int64_t T, int64_t k, int64_t n);
 mosaic_status launch_linear_wgrad_pack8(hipStream_t s, int quota, int dtype, int64_t T, int64_t k, int64_t n, const void* q, const void* scale, const void* dY,
                                         void* dW, void* db, void* scratch);
+// the same in one launch, for bf16 and small outputs (wgrad_pack8.hip)
+bool wgrad_pack8_small(int64_t T, int64_t k, int64_t n, const void* q, const void* dY, const void* dW);
+mosaic_status launch_wgrad_pack8_small(hipStream_t s, int quota, int64_t T, int64_t k, int64_t n, const void* q, const void* scale, const void* dY, void* dW, void* db);
 // k=3, pad=1 convolution over frames-major [B, L, C] as gather + GEMM: out [B*Lo, 3*C] with
 // column index tap*C + channel; col2im1d is the transposed gather at stride 1 (one owner per element)
 mosaic_status launch_im2col1d(hipStream_t s, int quota, int dtype, int64_t B, int L, int Lo, int C,

@@ -8,6 +8,7 @@
 #include <type_traits>
 #include "kernels.h"
 #include "activations.h"
+#include "pack8.h"
 
 namespace {
 
@@ -20,9 +21,6 @@ __device__ __forceinline__ int scale_byte(unsigned top) {
   const int e = (int)(top >> 23) - 6 + ((top & 0x7fffffu) > 0x7f0000u);     // exponent byte of e; 127.5 = 1.9921875 * 2^6
   return e < 0 ? 0 : e;
 }
-__device__ __forceinline__ float step_of(int byte) {          // 2^e
-  return __uint_as_float(byte == 255 ? 0x7fc00000u : byte == 0 ? 0x400000u : (unsigned)byte << 23);
-}
 __device__ __forceinline__ float inverse_step(int byte) {     // 2^-e; e is 122 at most (a NaN's numbers are 0)
   return __uint_as_float(byte == 255 ? 0u : (unsigned)(254 - byte) << 23);
 }
@@ -30,9 +28,6 @@ __device__ __forceinline__ int packed(float x, float inverse) {
   const float v = rintf(x * inverse);
   return v != v ? 0 : (int)fminf(fmaxf(v, -127.f), 127.f);
 }
-
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 // Eight consecutive elements in fp32: 16 bytes of bf16, 32 of fp32.
 template <bool PAST> __device__ __forceinline__ void load8(const bf16* p, float (&v)[8]) {
@@ -95,16 +90,6 @@ __device__ __forceinline__ int pack_quad(const float (&v)[8], u32x2* q) {
   }
   *q = u32x2{w[0], w[1]};
   return byte;
-}
-// the eight values of two words; (number + 128) * step - 128 * step in one operation would overflow in blocks of the largest numbers
-__device__ __forceinline__ void unpack8_of(u32x2 q, int byte, float (&v)[8]) {
-  const float step = step_of(byte);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const unsigned w = (h ? q.y : q.x) ^ 0x80808080u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[4 * h + k] = ((float)(w >> (8 * k) & 0xffu) - 128.f) * step;
-  }
 }
 __device__ __forceinline__ void put_tail(int8_t* p, int64_t left, u32x2 q) {
   for (int k = 0; k < 8; ++k)
@@ -443,6 +428,7 @@ size_t linear_wgrad_pack8_scratch_bytes(int dtype, int64_t T, int64_t k, int64_t
 
 mosaic_status launch_linear_wgrad_pack8(hipStream_t s, int quota, int dtype, int64_t T, int64_t k, int64_t n, const void* q, const void* scale, const void* dY,
                                         void* dW, void* db, void* scratch) {
+  if (dtype == MOSAIC_BF16 && wgrad_pack8_small(T, k, n, q, dY, dW)) return launch_wgrad_pack8_small(s, quota, T, k, n, q, scale, dY, dW, db);
   char* x = (char*)scratch;
   char* splitk = x + align_up((size_t)T * k * dtype_size(dtype), 256);
   MOSAIC_TRY(launch_unpack8(s, quota, dtype, T * k, q, scale, x));
