@@ -291,7 +291,7 @@ static mosaic_status check_heads(int32_t dtype, int64_t T, int32_t H, int32_t Hk
   if (d <= 0 || d % 2) MOSAIC_FAIL(MOSAIC_EINVAL, "head size %d is not positive and even", d);
   if (d > 256) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "head size %d > 256", d);
   if (((int64_t)H + 2 * (int64_t)Hkv) * d > INT32_MAX) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "rows of more than 2^31 - 1 elements");
-  if (T > ((int64_t)1 << 62) / (((int64_t)H + 2 * Hkv) * d)) MOSAIC_FAIL(MOSAIC_EINVAL, "%lld tokens", (long long)T);
+  if (T > ((int64_t)1 << 58) / (((int64_t)H + 2 * Hkv) * d)) MOSAIC_FAIL(MOSAIC_EINVAL, "%lld tokens", (long long)T);
   if (pairing != MOSAIC_PAIR_ADJACENT && pairing != MOSAIC_PAIR_HALVES) MOSAIC_FAIL(MOSAIC_EINVAL, "bad pairing %d", pairing);
   if (table) {
     NONNULL(pos);

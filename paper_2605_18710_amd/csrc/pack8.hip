@@ -165,12 +165,36 @@ template <int ACT> __device__ __forceinline__ float act_grad_of(float z) {
   }
 }
 
+// e = exp(-z) and s = 1 / (1 + e) of SwiGLU's gate for results in bf16: the exponential of 2 with the rounding of its argument put right to first
+// order, and the approximate reciprocal, 4 * 2^-24 off in all where expf and the divide are 2 (and three times the instructions).
+// 1 - s is e s, which keeps its digits.  Past +-126 both are what they are in the limit; a NaN reaches the results through the gate itself.
+struct Gate { float e, s; };
+__device__ __forceinline__ Gate gate_of(float z) {
+  const float x = -__builtin_amdgcn_fmed3f(z, -126.f, 126.f), hi = x * 1.44269504088896341f;
+  const float lo = fmaf(x, 1.92596299112661746e-8f, fmaf(x, 1.44269504088896341f, -hi));       // log2(e) in two pieces
+  const float p = __builtin_amdgcn_exp2f(hi), e = fminf(fmaf(p, lo * 0.693147180559945309f, p), 3e38f);
+  return {e, __builtin_amdgcn_rcpf(1.f + e)};
+}
+template <typename T> __device__ __forceinline__ float glu_of(float gate, float up) {
+  if constexpr (sizeof(T) == 2) return gate * gate_of(gate).s * up;
+  else return swiglu_f(gate, up);
+}
+template <typename T> __device__ __forceinline__ void glu_grad_of(float gate, float up, float d, float* dgate, float* dup) {
+  if constexpr (sizeof(T) == 2) {
+    const Gate g = gate_of(gate);
+    *dgate = d * up * (g.s * fmaf(gate, g.e * g.s, 1.f));
+    *dup = d * (gate * g.s);
+  } else {
+    swiglu_grad_f(gate, up, d, dgate, dup);
+  }
+}
+
 template <typename T, int ACT>
 __global__ __launch_bounds__(kThreads) void act_fwd_any_kernel(const T* __restrict__ z, T* __restrict__ a, int64_t rows, int64_t f) {
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < rows * f; i += (int64_t)gridDim.x * kThreads) {
     if constexpr (ACT == MOSAIC_SWIGLU) {
       const int64_t r = i / f, at = i + r * f;              // row r starts at 2 r f
-      a[i] = from_f32<T>(swiglu_f(to_f32(z[at]), to_f32(z[at + f])));
+      a[i] = from_f32<T>(glu_of<T>(to_f32(z[at]), to_f32(z[at + f])));
     } else {
       a[i] = from_f32<T>(act_of<ACT>(to_f32(z[i])));
     }
@@ -188,10 +212,10 @@ __global__ __launch_bounds__(kThreads) void act_bwd_any_kernel(const int8_t* __r
       const int64_t r = i / f, at = i + r * f;
       const float gate = value(at), up = value(at + f);
       float dg, du;
-      swiglu_grad_f(gate, up, d, &dg, &du);
+      glu_grad_of<T>(gate, up, d, &dg, &du);
       dz[at] = from_f32<T>(dg);
       dz[at + f] = from_f32<T>(du);
-      if (a) a[i] = from_f32<T>(swiglu_f(gate, up));
+      if (a) a[i] = from_f32<T>(glu_of<T>(gate, up));
     } else {
       const float z = value(i);
       dz[i] = from_f32<T>(d * act_grad_of<ACT>(z));
@@ -230,7 +254,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__
       load8<PAST>(z + at, v);
       load8<PAST>(z + up, u);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = swiglu_f(v[k], u[k]);
+      for (int k = 0; k < 8; ++k) o[k] = glu_of<T>(v[k], u[k]);
       store8<PAST>(a + i * 8, o);
       u32x2 wu;
       const int bg = pack_quad(v, &w), bu = pack_quad(u, &wu);
@@ -275,8 +299,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restr
       unpack8_of(wu, bu, u);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        swiglu_grad_f(z[k], u[k], d[k], &og[k], &ou[k]);
-        if constexpr (AGAIN) o[k] = swiglu_f(z[k], u[k]);
+        glu_grad_of<T>(z[k], u[k], d[k], &og[k], &ou[k]);
+        if constexpr (AGAIN) o[k] = glu_of<T>(z[k], u[k]);
       }
       store8<PAST>(dz + at, og);
       store8<PAST>(dz + up, ou);
