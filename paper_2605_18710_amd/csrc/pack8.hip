@@ -151,21 +151,7 @@ __global__ __launch_bounds__(kThreads) void unpack8_any_kernel(const int8_t* __r
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) x[i] = from_f32<T>((float)q[i] * step_of(scale[i / kBlock]));
 }
 
-// The tanh form as a logistic function: (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), which keeps its digits where tanh is near -1 and takes one exponential.
-__device__ __forceinline__ float tanh_gelu_gate(float z) { return sigmoid_f(1.5957691216057308f * (z + 0.044715f * z * z * z)); }
-template <int ACT> __device__ __forceinline__ float act_of(float z) {
-  if constexpr (ACT == MOSAIC_GELU) return gelu_f(z);
-  else return z * tanh_gelu_gate(z);
-}
-template <int ACT> __device__ __forceinline__ float act_grad_of(float z) {
-  if constexpr (ACT == MOSAIC_GELU) return gelu_grad_f(z);
-  else {
-    const float s = tanh_gelu_gate(z);
-    return s + z * s * (1.0f - s) * 1.5957691216057308f * (1.0f + 0.134145f * z * z);
-  }
-}
-
-// e = exp(-z) and s = 1 / (1 + e) of SwiGLU's gate for results in bf16: the exponential of 2 with the rounding of its argument put right to first
+// e = exp(-z) and s = 1 / (1 + e) of a gate z for results in bf16: the exponential of 2 with the rounding of its argument put right to first
 // order, and the approximate reciprocal, 4 * 2^-24 off in all where expf and the divide are 2 (and three times the instructions).
 // 1 - s is e s, which keeps its digits.  Past +-126 both are what they are in the limit; a NaN reaches the results through the gate itself.
 struct Gate { float e, s; };
@@ -174,6 +160,33 @@ __device__ __forceinline__ Gate gate_of(float z) {
   const float lo = fmaf(x, 1.92596299112661746e-8f, fmaf(x, 1.44269504088896341f, -hi));       // log2(e) in two pieces
   const float p = __builtin_amdgcn_exp2f(hi), e = fminf(fmaf(p, lo * 0.693147180559945309f, p), 3e38f);
   return {e, __builtin_amdgcn_rcpf(1.f + e)};
+}
+// The tanh form as a logistic function: (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), which keeps its digits where tanh is near -1 and takes one exponential.
+__device__ __forceinline__ float tanh_gelu_arg(float z) { return 1.5957691216057308f * (z + 0.044715f * z * z * z); }
+// act(z) and its derivative; TAB: with erf of bf16 numbers from a table in LDS (GELU in bf16)
+template <typename T, int ACT, bool TAB> __device__ __forceinline__ float act_of(const float* table, float z) {
+  if constexpr (ACT == MOSAIC_GELU_TANH) return z * (sizeof(T) == 2 ? gate_of(tanh_gelu_arg(z)).s : sigmoid_f(tanh_gelu_arg(z)));
+  else if constexpr (TAB) return ErfTable::gelu(table, z);
+  else return gelu_f(z);
+}
+template <typename T, int ACT, bool TAB> __device__ __forceinline__ float act_grad_of(const float* table, float z) {
+  if constexpr (ACT == MOSAIC_GELU_TANH) {
+    const float v = tanh_gelu_arg(z), w = z * 1.5957691216057308f * (1.0f + 0.134145f * z * z);
+    if constexpr (sizeof(T) == 2) {
+      const Gate g = gate_of(v);
+      return g.s * fmaf(w, g.e * g.s, 1.f);
+    } else {
+      const float s = sigmoid_f(v);
+      return s + s * (1.0f - s) * w;
+    }
+  } else if constexpr (TAB) {
+    // ErfTable::gelu_grad with the exponential of 2: its argument w is rounded, but w exp(-w) never passes 0.37
+    const float series = z * fmaf(z * z, -0.13298076013381091f, 0.79788456080286536f), far = ErfTable::erf_of(table, z);
+    const float e = fabsf(z) < 0x1p-10f ? series : far;
+    return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z), 0.5f * (1.0f + e));
+  } else {
+    return gelu_grad_f(z);
+  }
 }
 template <typename T> __device__ __forceinline__ float glu_of(float gate, float up) {
   if constexpr (sizeof(T) == 2) return gate * gate_of(gate).s * up;
@@ -196,7 +209,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_any_kernel(const T* __restri
       const int64_t r = i / f, at = i + r * f;              // row r starts at 2 r f
       a[i] = from_f32<T>(glu_of<T>(to_f32(z[at]), to_f32(z[at + f])));
     } else {
-      a[i] = from_f32<T>(act_of<ACT>(to_f32(z[i])));
+      a[i] = from_f32<T>(act_of<T, ACT, false>(nullptr, to_f32(z[i])));
     }
   }
 }
@@ -218,8 +231,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_any_kernel(const int8_t* __r
       if (a) a[i] = from_f32<T>(glu_of<T>(gate, up));
     } else {
       const float z = value(i);
-      dz[i] = from_f32<T>(d * act_grad_of<ACT>(z));
-      if (a) a[i] = from_f32<T>(act_of<ACT>(z));
+      dz[i] = from_f32<T>(d * act_grad_of<T, ACT, false>(nullptr, z));
+      if (a) a[i] = from_f32<T>(act_of<T, ACT, false>(nullptr, z));
     }
   }
 }
@@ -265,10 +278,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__
       const int64_t left = n - i * 8;
       load8<PAST>(z + i * 8, left, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if constexpr (TAB) o[k] = ErfTable::gelu(table, v[k]);
-        else o[k] = act_of<ACT>(v[k]);
-      }
+      for (int k = 0; k < 8; ++k) o[k] = act_of<T, ACT, TAB>(table, v[k]);
       store8<PAST>(a + i * 8, left, o);
       const int byte = pack_quad(v, &w);
       if (left >= 8) store_to<PAST>((u32x2*)(q + i * 8), w);
@@ -314,9 +324,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restr
       unpack8_of(w, byte, z);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        if constexpr (TAB) d[k] *= ErfTable::gelu_grad(table, z[k]);
-        else d[k] *= act_grad_of<ACT>(z[k]);
-        if constexpr (AGAIN) o[k] = TAB ? ErfTable::gelu(table, z[k]) : act_of<ACT>(z[k]);
+        d[k] *= act_grad_of<T, ACT, TAB>(table, z[k]);
+        if constexpr (AGAIN) o[k] = act_of<T, ACT, TAB>(table, z[k]);
       }
       store8<PAST>(dz + i * 8, left, d);
       if constexpr (AGAIN) store8<PAST>(a + i * 8, left, o);
