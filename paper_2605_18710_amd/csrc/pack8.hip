@@ -163,13 +163,24 @@ __device__ __forceinline__ Gate gate_of(float z) {
 }
 // The tanh form as a logistic function: (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), which keeps its digits where tanh is near -1 and takes one exponential.
 __device__ __forceinline__ float tanh_gelu_arg(float z) { return 1.5957691216057308f * (z + 0.044715f * z * z * z); }
-// act(z) and its derivative; TAB: with erf of bf16 numbers from a table in LDS (GELU in bf16)
-template <typename T, int ACT, bool TAB> __device__ __forceinline__ float act_of(const float* table, float z) {
+// e = exp(-z^2 / 2) and the normal distribution's phi = (1 + erf(z / sqrt 2)) / 2 for results in bf16.  erf by Hastings' approximation (Abramowitz and Stegun,
+// Handbook of Mathematical Functions, 7.1.26: 1 - (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), off by 1.5e-7), whose exponential GELU's derivative needs anyway:
+// phi is off by 1.3 * 2^-24 for it and 2 * 2^-24 for roundings.  e's rounded argument w costs w exp(-w) * 2^-24, which never passes 0.37.
+struct Normal { float e, phi; };
+__device__ __forceinline__ Normal normal_of(float z) {
+  const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.f));
+  const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float tail = 0.5f * poly * e;                       // phi(-|z|)
+  return {e, z < 0.f ? tail : 1.f - tail};
+}
+// act(z) and its derivative
+template <typename T, int ACT> __device__ __forceinline__ float act_of(float z) {
   if constexpr (ACT == MOSAIC_GELU_TANH) return z * (sizeof(T) == 2 ? gate_of(tanh_gelu_arg(z)).s : sigmoid_f(tanh_gelu_arg(z)));
-  else if constexpr (TAB) return ErfTable::gelu(table, z);
+  else if constexpr (sizeof(T) == 2) return z * normal_of(z).phi;
   else return gelu_f(z);
 }
-template <typename T, int ACT, bool TAB> __device__ __forceinline__ float act_grad_of(const float* table, float z) {
+template <typename T, int ACT> __device__ __forceinline__ float act_grad_of(float z) {
   if constexpr (ACT == MOSAIC_GELU_TANH) {
     const float v = tanh_gelu_arg(z), w = z * 1.5957691216057308f * (1.0f + 0.134145f * z * z);
     if constexpr (sizeof(T) == 2) {
@@ -179,11 +190,9 @@ template <typename T, int ACT, bool TAB> __device__ __forceinline__ float act_gr
       const float s = sigmoid_f(v);
       return s + s * (1.0f - s) * w;
     }
-  } else if constexpr (TAB) {
-    // ErfTable::gelu_grad with the exponential of 2: its argument w is rounded, but w exp(-w) never passes 0.37
-    const float series = z * fmaf(z * z, -0.13298076013381091f, 0.79788456080286536f), far = ErfTable::erf_of(table, z);
-    const float e = fabsf(z) < 0x1p-10f ? series : far;
-    return fmaf(z * 0.39894228040143268f, __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z), 0.5f * (1.0f + e));
+  } else if constexpr (sizeof(T) == 2) {
+    const Normal n = normal_of(z);
+    return fmaf(z * 0.39894228040143268f, n.e, n.phi);
   } else {
     return gelu_grad_f(z);
   }
@@ -209,7 +218,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_any_kernel(const T* __restri
       const int64_t r = i / f, at = i + r * f;              // row r starts at 2 r f
       a[i] = from_f32<T>(glu_of<T>(to_f32(z[at]), to_f32(z[at + f])));
     } else {
-      a[i] = from_f32<T>(act_of<T, ACT, false>(nullptr, to_f32(z[i])));
+      a[i] = from_f32<T>(act_of<T, ACT>(to_f32(z[i])));
     }
   }
 }
@@ -231,8 +240,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_any_kernel(const int8_t* __r
       if (a) a[i] = from_f32<T>(glu_of<T>(gate, up));
     } else {
       const float z = value(i);
-      dz[i] = from_f32<T>(d * act_grad_of<T, ACT, false>(nullptr, z));
-      if (a) a[i] = from_f32<T>(act_of<T, ACT, false>(nullptr, z));
+      dz[i] = from_f32<T>(d * act_grad_of<T, ACT>(z));
+      if (a) a[i] = from_f32<T>(act_of<T, ACT>(z));
     }
   }
 }
@@ -249,13 +258,13 @@ __device__ __forceinline__ void place(int64_t i, int64_t fv, int64_t* r, int64_t
   }
 }
 
+// Bound by memory: 16384 x 11008 SwiGLU 240 us forward (6.1 TB/s; 281 with expf and a divide for the gate) and 295 backward (6.2), 32768 x 5120 GELU 138 (6.1) and
+// 185 (6.4; 236 with erf from a table in LDS, which keeps workgroups from starting in order).  f no multiple of 32: the activation and the packing
+// in a pass each, 8192 x 5608 102 us where 8192 x 5632 takes 61.
 // a = act(z) and z in 8 bits.  GELU forms: flat, any size.  SwiGLU: rows of f = 8 fv, f a multiple of 32, so that no block has elements of both halves.
 template <typename T, int ACT, bool PAST>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__ z, T* __restrict__ a, int8_t* __restrict__ q, uint8_t* __restrict__ scale,
                                                            int64_t n, int64_t vectors, int64_t fv) {
-  constexpr bool TAB = ACT == MOSAIC_GELU && sizeof(T) == 2;
-  __shared__ float table[TAB ? ErfTable::kEntries : 1];
-  if constexpr (TAB) { ErfTable::fill(table, threadIdx.x, kThreads); __syncthreads(); }
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
     float v[8], o[8];
     u32x2 w;
@@ -278,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__
       const int64_t left = n - i * 8;
       load8<PAST>(z + i * 8, left, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = act_of<T, ACT, TAB>(table, v[k]);
+      for (int k = 0; k < 8; ++k) o[k] = act_of<T, ACT>(v[k]);
       store8<PAST>(a + i * 8, left, o);
       const int byte = pack_quad(v, &w);
       if (left >= 8) store_to<PAST>((u32x2*)(q + i * 8), w);
@@ -292,9 +301,6 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__
 template <typename T, int ACT, bool PAST, bool AGAIN>
 __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restrict__ q, const uint8_t* __restrict__ scale, const T* da, T* dz, T* __restrict__ a,
                                                            int64_t n, int64_t vectors, int64_t fv) {
-  constexpr bool TAB = ACT == MOSAIC_GELU && sizeof(T) == 2;      // unpacked numbers are bf16 numbers
-  __shared__ float table[TAB ? ErfTable::kEntries : 1];
-  if constexpr (TAB) { ErfTable::fill(table, threadIdx.x, kThreads); __syncthreads(); }
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
     float z[8], d[8], o[8];
     if constexpr (ACT == MOSAIC_SWIGLU) {
@@ -324,8 +330,8 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restr
       unpack8_of(w, byte, z);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        d[k] *= act_grad_of<T, ACT, TAB>(table, z[k]);
-        if constexpr (AGAIN) o[k] = act_of<T, ACT, TAB>(table, z[k]);
+        d[k] *= act_grad_of<T, ACT>(z[k]);
+        if constexpr (AGAIN) o[k] = act_of<T, ACT>(z[k]);
       }
       store8<PAST>(dz + i * 8, left, d);
       if constexpr (AGAIN) store8<PAST>(a + i * 8, left, o);
@@ -333,6 +339,9 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restr
   }
 }
 
+// Workgroups in order from 64 MB on (sweep_grid), striding / in order, us: 2^27 bf16 elements packed 76 / 72, unpacked 75 / 67; GELU of 12000 x 5120, forward 62 / 51
+// and backward 85 / 69, on 64 CUs 182 / 154 and 208 / 168; SwiGLU of 8192 x 5632 71 / 61 and 89 / 75, of 2048 x 5632 (93 and 116 MB) 19.5 / 20.3 and
+// 23.6 / 23.7, on 64 CUs 44.7 / 44.3 and 54.9 / 51.2.
 // Past the caches what they do not hold, of bf16: 16384 x 11008 SwiGLU 292 / 309 us -> 282 / 297, unpacking 2^27 elements 70 -> 67.  An fp32 lane's 32 bytes
 // are two instructions' halves of a line, which past the caches are written one by one: unpacking 2^26 elements 61 us, past them 91.
 template <typename T> bool past_caches(const Sweep& sw, int64_t bytes) { return sizeof(T) == 2 && sw.in_order && bytes > kPastCacheBytes; }
@@ -405,8 +414,7 @@ mosaic_status launch_act_fwd_pack8(hipStream_t s, int quota, int dtype, int act,
       typedef decltype(type) E;
       constexpr int ACT = decltype(kind)::value;
       const int64_t vectors = glu ? m / 8 : ceil_div(n, kBlock) * (kBlock / 8), blocks = ceil_div(vectors, kThreads), bytes = (n + m) * (int64_t)sizeof(E) + n;
-      const bool table = ACT == MOSAIC_GELU && sizeof(E) == 2;          // filled by every workgroup: few of them
-      const Sweep sw = table ? Sweep{grid_for(quota, 8, blocks), false} : sweep_grid(s, quota, blocks, bytes);
+      const Sweep sw = sweep_grid(s, quota, blocks, bytes);
       auto with = [&](auto past) {
         act_fwd_kernel<E, ACT, decltype(past)::value><<<sw.grid, kThreads, 0, s>>>((const E*)z, (E*)a, (int8_t*)q, (uint8_t*)scale, n, vectors, f / 8);
       };
@@ -441,8 +449,7 @@ mosaic_status launch_act_bwd_pack8(hipStream_t s, int quota, int dtype, int act,
       return;
     }
     const int64_t vectors = ceil_div(m, 8), blocks = ceil_div(vectors, kThreads), bytes = n + (n + (a ? 2 : 1) * m) * (int64_t)sizeof(E);
-    const bool table = ACT == MOSAIC_GELU && sizeof(E) == 2;
-    const Sweep sw = table ? Sweep{grid_for(quota, 8, blocks), false} : sweep_grid(s, quota, blocks, bytes);
+    const Sweep sw = sweep_grid(s, quota, blocks, bytes);
     auto with = [&](auto past, auto again) {
       act_bwd_kernel<E, ACT, decltype(past)::value, decltype(again)::value><<<sw.grid, kThreads, 0, s>>>(
           (const int8_t*)q, (const uint8_t*)scale, (const E*)da, (E*)dz, (E*)a, n, vectors, f / 8);
