@@ -259,8 +259,7 @@ __device__ __forceinline__ void place(int64_t i, int64_t fv, int64_t* r, int64_t
 }
 
 // Bound by memory: 16384 x 11008 SwiGLU 240 us forward (6.1 TB/s; 281 with expf and a divide for the gate) and 295 backward (6.2), 32768 x 5120 GELU 138 (6.1) and
-// 185 (6.4; 236 with erf from a table in LDS, which keeps workgroups from starting in order).  f no multiple of 32: the activation and the packing
-// in a pass each, 8192 x 5608 102 us where 8192 x 5632 takes 61.
+// 185 (6.4; 236 with erf from a table in LDS, which keeps workgroups from starting in order).
 // a = act(z) and z in 8 bits.  GELU forms: flat, any size.  SwiGLU: rows of f = 8 fv, f a multiple of 32, so that no block has elements of both halves.
 template <typename T, int ACT, bool PAST>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__ z, T* __restrict__ a, int8_t* __restrict__ q, uint8_t* __restrict__ scale,
@@ -294,6 +293,31 @@ __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__
       else put_tail(q + i * 8, left, w);
       if (i % 4 == 0) scale[i / 4] = (uint8_t)byte;
     }
+  }
+}
+
+// SwiGLU whose halves are no whole blocks (f = 8 fv): lanes walk z as it lies, and those of gate numbers ask for their up numbers too, which another
+// workgroup packs and the caches hold.  8192 x 5608 75 us (activation and packing in a pass each 101; halves of whole blocks, 8192 x 5632, 61), 16384 x 11000 280 (373),
+// 333 x 1000 4.2 (8.4); fp32 4096 x 5624 62 (82), but on 64 CUs 176 (168).
+template <typename T, bool PAST>
+__global__ __launch_bounds__(kThreads) void swiglu_fwd_flat_kernel(const T* __restrict__ z, T* __restrict__ a, int8_t* __restrict__ q, uint8_t* __restrict__ scale,
+                                                                   int64_t n, int64_t vectors, int64_t fv) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < vectors; i += (int64_t)gridDim.x * kThreads) {
+    const bool any = i * 8 < n;                            // the last block's lanes take part together
+    int64_t r, c;
+    place(i, 2 * fv, &r, &c);
+    float v[8] = {}, u[8], o[8];
+    if (any) load8<false>(z + i * 8, v);
+    if (any && c < fv) {
+      load8<false>(z + (i + fv) * 8, u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = glu_of<T>(v[k], u[k]);
+      store8<PAST>(a + (r * fv + c) * 8, o);
+    }
+    u32x2 w;
+    const int byte = pack_quad(v, &w);
+    if (any) store_to<PAST>((u32x2*)(q + i * 8), w);
+    if (i % 4 == 0) scale[i / 4] = (uint8_t)byte;
   }
 }
 
@@ -423,16 +447,26 @@ mosaic_status launch_act_fwd_pack8(hipStream_t s, int quota, int dtype, int act,
     MOSAIC_LAUNCH_CHECK();
     return MOSAIC_OK;
   }
-  const int64_t vn = 16 / (int64_t)dtype_size(dtype);
-  if (glu && f % vn == 0 && on16({z, a})) MOSAIC_TRY(launch_swiglu_fwd(s, quota, dtype, T, f, z, a));
-  else {
-    const int grid = grid_for(quota, 8, ceil_div(m, kThreads));
-    of_type_and_act(dtype, act, [&](auto type, auto kind) {
+  if (glu && f % 8 == 0 && on16({z, a, q})) {
+    auto launch = [&](auto type) {
       typedef decltype(type) E;
-      act_fwd_any_kernel<E, decltype(kind)::value><<<grid, kThreads, 0, s>>>((const E*)z, (E*)a, T, f);
-    });
+      const int64_t vectors = ceil_div(n, kBlock) * (kBlock / 8), bytes = (n + m) * (int64_t)sizeof(E) + n;
+      const Sweep sw = sweep_grid(s, quota, ceil_div(vectors, kThreads), bytes);
+      auto with = [&](auto past) {
+        swiglu_fwd_flat_kernel<E, decltype(past)::value><<<sw.grid, kThreads, 0, s>>>((const E*)z, (E*)a, (int8_t*)q, (uint8_t*)scale, n, vectors, f / 8);
+      };
+      if (past_caches<E>(sw, bytes)) with(std::true_type{}); else with(std::false_type{});
+    };
+    if (dtype == MOSAIC_BF16) launch(bf16{}); else launch(float{});
     MOSAIC_LAUNCH_CHECK();
+    return MOSAIC_OK;
   }
+  const int grid = grid_for(quota, 8, ceil_div(m, kThreads));
+  of_type_and_act(dtype, act, [&](auto type, auto kind) {
+    typedef decltype(type) E;
+    act_fwd_any_kernel<E, decltype(kind)::value><<<grid, kThreads, 0, s>>>((const E*)z, (E*)a, T, f);
+  });
+  MOSAIC_LAUNCH_CHECK();
   return launch_pack8(s, quota, dtype, n, z, q, scale);
 }
 
