@@ -468,7 +468,7 @@ mosaic_status mosaic_op_rope_axes_table(void* stream, int32_t quota, int32_t d, 
 /* x, y [T, (H + 2*Hkv)*d], row = [q (H heads) | k (Hkv heads) | v (Hkv heads)], Hkv divides H: the q
  * and k heads of x rotated (direction = +1) or turned back (-1: gradients of rotated q, k), v as it is.
  * y may be x; it must not overlap it otherwise.  A pair whose axis is n_axes or more (a
- * table made for more axes) stays as it is.  The tokens may be any set: a batch, packed sequences, the
+ * table made for more axes) stays as it is.  A NaN or an infinity makes its pair NaN (with a norm, its head).  The tokens may be any set: a batch, packed sequences, the
  * single tokens of a serving step. */
 mosaic_status mosaic_op_rope_axes(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t H,
                                   int32_t Hkv, int32_t d, int32_t pairing, int32_t direction,
@@ -509,7 +509,8 @@ mosaic_status mosaic_op_pack8(void* stream, int32_t quota, int32_t dtype, int64_
 mosaic_status mosaic_op_unpack8(void* stream, int32_t quota, int32_t dtype, int64_t n, const void* q,
                                 const void* scale, void* x);
 /* The activation of an MLP that keeps its input z in 8 bits instead of z and a: a = act(z) (of z as given) and z
- * packed, in one pass; act = MOSAIC_GELU, MOSAIC_GELU_TANH (z [T,f]) or MOSAIC_SWIGLU (z [T,2f] = [gate | up]); a [T,f].
+ * packed, in one pass where the buffers are 16-byte aligned (SwiGLU: and f is a multiple of 8), in two otherwise; any T, f >= 0;
+ * act = MOSAIC_GELU, MOSAIC_GELU_TANH (z [T,f]) or MOSAIC_SWIGLU (z [T,2f] = [gate | up]); a [T,f].
  * The backward pass takes z from its 8 bits: dz = act'(z) da (dz laid out like z; for the GELU forms it may be da) and, where a is not NULL, a = act(z)
  * again, the input of the next layer's weight gradient. */
 mosaic_status mosaic_op_act_fwd_pack8(void* stream, int32_t quota, int32_t dtype, int32_t act, int64_t T,

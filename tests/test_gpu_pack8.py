@@ -1,10 +1,11 @@
 """GPU parity of the activation checkpoints in 8 bits: the packed bytes and what they stand for, bit for bit, against the plain
 definition; the activations' and the weight gradient's backward passes from them against 64 bits.
 
-Bounds, u = 2^-24; a bf16 result is off by 2^-8 of its size besides.  GELU: the error function is off by 2 u, so the result by at most 8 u |z|, its
-derivative by 8 u (1 + |z|).  Tanh form: 1 - t^2 is off by 13 u and meets z^3, at most 8.7 before t is 1: 128 u (1 + |z|).
-SwiGLU: an exponential, a sum, a quotient and products, 16 u of the result's size (and 1e-36 where exp overflows); the gate's derivative
-is a sum of two such terms, at most 1 + |gate| in size.  Weight gradient: T additions and products, T u of the sum of magnitudes."""
+Bounds, u = 2^-24; a bf16 result is off by 2^-8 of its size besides.  GELU: the distribution is off by 4 u (erf by 1.5e-7 = 2.5 u, halved, and roundings), so the
+result by at most 8 u |z|, its derivative by 8 u (1 + |z|).  A logistic function is off by 6 u (exponential 2 u, its correction 1 u, sum 1 u, reciprocal
+2 u).  Tanh form: with its argument's 4 u, at most 0.28 of them in the result, 12 u |z|; its derivative meets z^3, at most 8.7 before the function is 1: 128 u (1 + |z|).
+SwiGLU: two more products, 16 u of the result's size (and 1e-36 where exp overflows); the gate's derivative is s (1 + gate e s), where e s is off by
+13 u and the rest by 9 u: 24 u of the sum of both terms' sizes.  Weight gradient: T additions and products, T u of the sum of magnitudes."""
 import math
 
 import numpy as np
@@ -93,14 +94,14 @@ def act_ref(act, z, da):
         a = gate * s * up
         dz = np.concatenate([da * up * s * (1 + gate * (1 - s)), da * gate * s], axis=1)
         size = np.concatenate([np.abs(da * up) * s * (1 + np.abs(gate) * (1 - s)), np.abs(da * gate) * s], axis=1)
-        return a, dz, 16 * U * np.abs(a) + 1e-36 * (1 + np.abs(gate * up)), 16 * U * size + 1e-36 * (1 + np.abs(np.concatenate([up * da * gate, da * gate], axis=1)))
+        return a, dz, 16 * U * np.abs(a) + 1e-36 * (1 + np.abs(gate * up)), 24 * U * size + 1e-36 * (1 + np.abs(np.concatenate([up * da * gate, da * gate], axis=1)))
     if act == "gelu":
         p = 0.5 * np.vectorize(math.erfc)(-z * math.sqrt(0.5)) if z.size else z
         return z * p, da * (p + z * np.exp(-0.5 * z * z) / math.sqrt(2 * math.pi)), 8 * U * np.abs(z), 8 * U * (1 + np.abs(z)) * np.abs(da)
     c = math.sqrt(2 / math.pi)
     t = np.tanh(c * (z + 0.044715 * z ** 3))
     dz = da * (0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z))
-    return 0.5 * z * (1 + t), dz, 8 * U * np.abs(z), 128 * U * (1 + np.abs(z)) * np.abs(da)
+    return 0.5 * z * (1 + t), dz, 12 * U * np.abs(z), 128 * U * (1 + np.abs(z)) * np.abs(da)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -168,7 +169,8 @@ def test_activation_of_a_block_with_nan(mb, act):
 
 @pytest.mark.parametrize("dtype,T,k,n,db", [("bf16", 1, 8, 8, True), ("bf16", 37, 64, 72, True), ("bf16", 300, 136, 256, False), ("bf16", 1500, 320, 264, True),
                                             ("bf16", 5, 33, 7, True), ("bf16", 513, 256, 512, True), ("f32", 1, 1, 1, True), ("f32", 70, 20, 12, True),
-                                            ("f32", 257, 128, 64, False), ("bf16", 64, 128, 128, True), ("bf16", 2100, 512, 512, False)])
+                                            ("f32", 257, 128, 64, False), ("bf16", 64, 128, 128, True), ("bf16", 2100, 512, 512, False), ("bf16", 200, 1040, 1048, True),
+                                            ("bf16", 5000, 256, 512, True)])
 def test_weight_gradient(mb, dtype, T, k, n, db):
     x = quantize(synth.normal(7300, (T, k)) * np.exp(synth.normal(7301, (k,))), dtype)
     if T > 4:
@@ -200,6 +202,30 @@ def test_weight_gradient(mb, dtype, T, k, n, db):
         within(from_dev(bias.t), dy.sum(0), last(dtype, dy.sum(0)) + (T + 8) * U * np.abs(dy).sum(0), "db")
     else:
         assert (bias.t == 7.0).all()
+
+
+@pytest.mark.parametrize("T", [100, 4500])
+def test_weight_gradient_of_extreme_blocks(mb, T):
+    """Blocks of the largest and of the smallest numbers, and one with a NaN, which stays in its columns; in one launch and in several."""
+    k, n = 160, 64
+    x = quantize(synth.normal(7800, (T, k)), "bf16")
+    x[:, 32:64] = quantize(np.clip(x[:, 32:64], -3, 3) * 1.1e38, "bf16")
+    x[:, 64:96] = quantize(x[:, 64:96] * 2.0 ** -121, "bf16")            # steps of 2^-127
+    x[T // 2, 100] = np.inf
+    dy = quantize(synth.normal(7801, (T, n)), "bf16")
+    q, byte = P.pack8(x)
+    assert byte.max() == 255 and (byte == 248).any() and (byte < 2).any()      # 248: the largest step of bf16 numbers
+    kept = P.unpack8(q, byte).reshape(T, k)
+    scaled = [(slice(0, 32), 1.0), (slice(32, 64), 2.0 ** -40), (slice(64, 96), 2.0 ** 120), (slice(128, 160), 1.0)]
+    for cols, by in scaled:
+        dy_ = dy if by == 1.0 else quantize(dy * by, "bf16")
+        dw = torch.empty((k, n), dtype=torch.bfloat16, device="cuda")
+        scratch = torch.empty(mb.linear_wgrad_pack8_scratch_bytes("bf16", T, k, n), dtype=torch.uint8, device="cuda")
+        mb.op_linear_wgrad_pack8(None, 256, "bf16", T, k, n, torch.from_numpy(q).cuda(), torch.from_numpy(byte).cuda(), to_dev(dy_, "bf16"), dw, None, scratch)
+        got = from_dev(dw)
+        assert np.isnan(got[96:128]).all()
+        ref = kept[:, cols].T @ dy_
+        within(got[cols], ref, last("bf16", ref) + (T + 8) * U * (np.abs(kept[:, cols]).T @ np.abs(dy_)), (cols, by))
 
 
 def test_captured_and_replayed(mb):
