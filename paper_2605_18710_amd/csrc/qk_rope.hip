@@ -564,7 +564,7 @@ template <typename T, int kBytes, typename F> bool with_vectors(int64_t width, i
     else if (lanes <= 4) launch(ve, std::integral_constant<int, 4>{});
     else if (lanes <= 8) launch(ve, std::integral_constant<int, 8>{});
     else if (lanes <= 16) launch(ve, std::integral_constant<int, 16>{});
-    else launch(ve, std::integral_constant<int, 32>{});
+    else if constexpr (decltype(ve)::value * 2 * 16 < kMaxD) launch(ve, std::integral_constant<int, 32>{});
   };
   if (d % (2 * kWide) == 0 && bits % (kWide * sizeof(T)) == 0) { of_lanes(std::integral_constant<int, kWide>{}); return true; }
   if (kWide > 4 && d % 8 == 0 && bits % 8 == 0) { of_lanes(std::integral_constant<int, 4>{}); return true; }
@@ -606,7 +606,10 @@ mosaic_status launch_qk_norm_rope_fwd(hipStream_t s, int quota, int dtype, int n
               (const E*)x, (E*)y, at, H, Hkv, d, heads, per_chunk, (int)ceil_div(groups, per_chunk), eps, (float)direction,
               (const E*)gq, (const E*)bq, (const E*)gk, (const E*)bk);
         };
-        if (sw.in_order && past_caches<E>(d, bytes)) with(std::true_type{}); else with(std::false_type{});
+        if constexpr (VE * LPH * sizeof(E) >= 128) {       // a half of a head may be whole lines
+          if (sw.in_order && past_caches<E>(d, bytes)) return with(std::true_type{});
+        }
+        with(std::false_type{});
       });
       if (vectors) return;
       const int grid = grid_for(quota, 8, ceil_div(T * heads, kWaves));
@@ -646,7 +649,10 @@ mosaic_status launch_qk_norm_rope_bwd(hipStream_t s, int quota, int dtype, int n
           qk_bwd_kernel<E, VE, LPH, decltype(kind)::value, decltype(halves)::value, decltype(past)::value><<<grid, kThreadsBwd, 0, s>>>(
               (const E*)x, (const E*)dy, (E*)dx, at, H, Hkv, d, parts, eps, (const E*)gq, (const E*)gk, (float*)scratch, np);
         };
-        if (past_caches<E>(d, bytes)) with(std::true_type{}); else with(std::false_type{});
+        if constexpr (VE * LPH * sizeof(E) >= 128) {
+          if (past_caches<E>(d, bytes)) return with(std::true_type{});
+        }
+        with(std::false_type{});
       });
       if (vectors) return;
       const int rp = (int)std::max<int64_t>(kWaves, ceil_div(T, kMaxParts));
