@@ -153,12 +153,16 @@ __global__ __launch_bounds__(kThreads) void unpack8_any_kernel(const int8_t* __r
 
 // e = exp(-z) and s = 1 / (1 + e) of a gate z for results in bf16: the exponential of 2 with the rounding of its argument put right to first
 // order, and the approximate reciprocal, 4 * 2^-24 off in all where expf and the divide are 2 (and three times the instructions).
-// 1 - s is e s, which keeps its digits.  Past +-126 both are what they are in the limit; a NaN reaches the results through the gate itself.
-struct Gate { float e, s; };
+// 1 - s is e s (`rest`), which keeps its digits.  Past +-126 both are what they are in the limit (s is 0 there, so that no size of z brings it back); a NaN reaches
+// the results through the gate itself.
+struct Gate {
+  float e, s;
+  __device__ __forceinline__ float rest() const { return fminf(e, 3e38f) * s; }
+};
 __device__ __forceinline__ Gate gate_of(float z) {
   const float x = -__builtin_amdgcn_fmed3f(z, -126.f, 126.f), hi = x * 1.44269504088896341f;
   const float lo = fmaf(x, 1.92596299112661746e-8f, fmaf(x, 1.44269504088896341f, -hi));       // log2(e) in two pieces
-  const float p = __builtin_amdgcn_exp2f(hi), e = fminf(fmaf(p, lo * 0.693147180559945309f, p), 3e38f);
+  const float e = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147180559945309f, 1.f);
   return {e, __builtin_amdgcn_rcpf(1.f + e)};
 }
 // The tanh form as a logistic function: (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), which keeps its digits where tanh is near -1 and takes one exponential.
@@ -182,13 +186,14 @@ template <typename T, int ACT> __device__ __forceinline__ float act_of(float z) 
 }
 template <typename T, int ACT> __device__ __forceinline__ float act_grad_of(float z) {
   if constexpr (ACT == MOSAIC_GELU_TANH) {
-    const float v = tanh_gelu_arg(z), w = z * 1.5957691216057308f * (1.0f + 0.134145f * z * z);
+    // the argument's derivative; far out the logistic function's is 0, whatever size z has
+    const float v = tanh_gelu_arg(z), near = __builtin_amdgcn_fmed3f(z, -1e6f, 1e6f), w = 1.5957691216057308f * (1.0f + 0.134145f * near * near);
     if constexpr (sizeof(T) == 2) {
       const Gate g = gate_of(v);
-      return g.s * fmaf(w, g.e * g.s, 1.f);
+      return g.s * fmaf(z * g.rest(), w, 1.f);
     } else {
       const float s = sigmoid_f(v);
-      return s + s * (1.0f - s) * w;
+      return s + z * (s * (1.0f - s)) * w;
     }
   } else if constexpr (sizeof(T) == 2) {
     const Normal n = normal_of(z);
@@ -204,7 +209,7 @@ template <typename T> __device__ __forceinline__ float glu_of(float gate, float 
 template <typename T> __device__ __forceinline__ void glu_grad_of(float gate, float up, float d, float* dgate, float* dup) {
   if constexpr (sizeof(T) == 2) {
     const Gate g = gate_of(gate);
-    *dgate = d * up * (g.s * fmaf(gate, g.e * g.s, 1.f));
+    *dgate = d * up * (g.s * fmaf(gate, g.rest(), 1.f));
     *dup = d * (gate * g.s);
   } else {
     swiglu_grad_f(gate, up, d, dgate, dup);

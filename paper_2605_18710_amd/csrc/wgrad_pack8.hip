@@ -60,7 +60,7 @@ struct Args {
 // in order at the end.  A step is a chain (barrier, 16 reads from LDS, conversion of 16 numbers, writes, four products that wait for each other) of 0.39 us
 // where a CU has one workgroup of four waves; the second group fills its gaps (0.57 us for both steps).
 // Steps are requested kAhead rounds ahead, in registers; a group's two tiles in LDS take turns, and the next round's numbers are converted while
-// this round's operands are on their way from LDS.
+// these operands are on their way from LDS.
 template <int G>
 __global__ __launch_bounds__(256 * G) void wgrad_pack8_kernel(Args p) {
   constexpr int kAhead = 4, kSteps = kTokens / 16;
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256 * G) void wgrad_pack8_kernel(Args p) {
     auto work = [&](auto slot) {
       constexpr int a = decltype(slot)::value;
       const lds_byte* const ta = lds + (a & 1) * kStage;
-      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // this round's numbers are written, the last round's read; loads stay in flight
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");        // this turn's numbers are written, the last turn's read; loads stay in flight
       bf16x8 fa[kSteps], fb[kSteps];
 #pragma unroll
       for (int ks = 0; ks < kSteps; ++ks) {

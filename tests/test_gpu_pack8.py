@@ -146,6 +146,32 @@ def test_activation(mb, dtype, act, T, f):
     assert all(np.array_equal(x, y) for x, y in zip(outs[0], outs[1]))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "swiglu"])
+def test_activation_far_out(mb, act, dtype):
+    """Sizes from 20 to 10^30, where an exponential overflows and z^3 does: the limits, and zeros where the result is one."""
+    sizes = (20.0, 85.0, 89.0, 120.0, 130.0, 200.0, 1e4, 1e15, 1e18, 1e30)
+    T, f = 2 * len(sizes), 64
+    row = np.linspace(0.6, 1.0, f)
+    gate = quantize(np.concatenate([[m * row, -m * row] for m in sizes]), dtype)
+    up = quantize(synth.normal(7900, (T, f)) + 3.0, dtype)
+    z = np.concatenate([gate, up], axis=1) if act == "swiglu" else gate
+    da = quantize(synth.normal(7901, (T, f)) + 2.0, dtype)
+    kept = P.unpack8(*P.pack8(z)).reshape(z.shape)
+    z_, da_ = to_dev(z, dtype), to_dev(da, dtype)
+    a, again, dz = torch.empty_like(da_), torch.empty_like(da_), torch.empty_like(z_)
+    q, scale = torch.empty(z.size, dtype=torch.int8, device="cuda"), torch.empty(z.size // 32, dtype=torch.uint8, device="cuda")
+    mb.op_act_fwd_pack8(None, 256, dtype, act, T, f, z_, a, q, scale)
+    mb.op_act_bwd_pack8(None, 256, dtype, act, T, f, q, scale, da_, dz, again)
+    for got, ref, tol in ((a, act_ref(act, z, da)[0], act_ref(act, z, da)[2]), (again, act_ref(act, kept, da)[0], act_ref(act, kept, da)[2]),
+                          (dz, act_ref(act, kept, da)[1], act_ref(act, kept, da)[3])):
+        got = from_dev(got)
+        if act != "swiglu":          # the bounds grow with |z|, and so do the results on the one side alone
+            tol = np.minimum(tol, 32 * U * (np.abs(ref) + 300))
+        within(got, ref, last(dtype, ref) + tol, act)
+        assert (np.abs(got[np.abs(ref) < 1e-45]) < 1e-36).all()
+
+
 @pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "swiglu"])
 def test_activation_of_a_block_with_nan(mb, act):
     """The forward result of what is finite stays; the block comes back as NaN, in the gradient and in the activation formed again."""
