@@ -151,19 +151,21 @@ __global__ __launch_bounds__(kThreads) void unpack8_any_kernel(const int8_t* __r
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) x[i] = from_f32<T>((float)q[i] * step_of(scale[i / kBlock]));
 }
 
-// e = exp(-z) and s = 1 / (1 + e) of a gate z for results in bf16: the exponential of 2 with the rounding of its argument put right to first
-// order, and the approximate reciprocal, 4 * 2^-24 off in all where expf and the divide are 2 (and three times the instructions).
-// 1 - s is e s (`rest`), which keeps its digits.  Past +-126 both are what they are in the limit (s is 0 there, so that no size of z brings it back); a NaN reaches
-// the results through the gate itself.
+// e = exp(-z) and s = 1 / (1 + e) of a gate z for results in bf16.  u = 2^-24, of the numbers' own size: the exponential of 2 is off by 2 u, the rest of its rounded
+// argument, put right to first order, by 1 u and (for ln 2 in one piece) 1.9e-9 of the argument, 4 u at most: e 7 u, and s 2 u and (1 - s) times that.  A
+// third of the instructions of expf and a divide.  s is the approximate reciprocal after one step of Newton's, which makes it the number that the divide gives: its
+// last bits decide results that lie near a tie between two bf16 numbers, and of numbers from 8 bits, which repeat, those are many (16384 x 11008 SwiGLU formed
+// again: without the step 2.4e-5 of the results were not the nearest number, with it and in the plain form 2.4e-6).
+// 1 - s is e s (`rest`), which keeps its digits.  From -88.7 down s is 0, an infinitesimal that the reciprocal drops, so that no size of z brings it back, and
+// e stays finite for the step; a NaN reaches the results through the gate itself.
 struct Gate {
   float e, s;
-  __device__ __forceinline__ float rest() const { return fminf(e, 3e38f) * s; }
+  __device__ __forceinline__ float rest() const { return e * s; }
 };
 __device__ __forceinline__ Gate gate_of(float z) {
-  const float x = -__builtin_amdgcn_fmed3f(z, -126.f, 126.f), hi = x * 1.44269504088896341f;
-  const float lo = fmaf(x, 1.92596299112661746e-8f, fmaf(x, 1.44269504088896341f, -hi));       // log2(e) in two pieces
-  const float e = __builtin_amdgcn_exp2f(hi) * fmaf(lo, 0.693147180559945309f, 1.f);
-  return {e, __builtin_amdgcn_rcpf(1.f + e)};
+  const float x = -__builtin_amdgcn_fmed3f(z, -88.7f, 126.f), hi = x * 1.44269504088896341f;
+  const float p = __builtin_amdgcn_exp2f(hi), e = fmaf(p, fmaf(-hi, 0.693147180559945309f, x), p), d = 1.f + e, s = __builtin_amdgcn_rcpf(d);
+  return {e, fmaf(s, fmaf(-d, s, 1.f), s)};
 }
 // The tanh form as a logistic function: (1 + tanh u) / 2 = 1 / (1 + exp(-2u)), which keeps its digits where tanh is near -1 and takes one exponential.
 __device__ __forceinline__ float tanh_gelu_arg(float z) { return 1.5957691216057308f * (z + 0.044715f * z * z * z); }

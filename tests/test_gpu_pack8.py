@@ -291,3 +291,33 @@ def test_captured_and_replayed(mb):
         torch.cuda.synchronize()
         for name, t in out.items():
             assert np.array_equal(want[name], bits(t)), name
+
+
+def test_swiglu_from_8_bits_rounds_like_the_plain_form(mb):
+    """Gates from 2 to 17 times up numbers of 7 bits, where results often lie within a few u of a tie between two bf16 numbers, so that the last bits of s = 1 / (1 + e)
+    decide them (5.9375 times a power of two is 1.6 u from one): those of the plain form in 32 bits, bit for bit.  e, off by 5 u of its size here, gives
+    d = fl(1 + e) = 1 + 2 u k but for gates whose e / 2u lies that near to a half; the approximate reciprocal, one bit off at most, is after a step of Newton's
+    2^-46 from 1 / d, and its nearest number is that of 1 / d but for gates where 1 / d lies that near to a tie.  Both are left out."""
+    gates = np.concatenate([np.arange(2.0, 7.95, 0.0625), np.arange(8.0, 15.9, 0.125), np.arange(16.0, 17.1, 0.25)])
+    from_half = lambda v: np.abs(v - np.floor(v) - 0.5)
+    ratio = np.exp(-gates) / (2 * U)
+    d = np.float32(1) + np.exp(-gates).astype(np.float32)
+    s = np.float32(1) / d
+    gates, s = (v[(from_half(ratio) > 5 * U * ratio + 1e-6) & (from_half(1 / d.astype(np.float64) / U) > 1e-3)] for v in (gates, s))
+    assert len(gates) > 130 and 5.9375 in gates
+    T, f = len(gates), 1024
+    up = np.clip(np.round(synth.normal(8200, (T, f), 0.0, 60.0)), -127, 127)
+    up[:, ::32] = 127.0
+    up[:, 1:8] = 2.0 ** np.arange(7)
+    z = np.concatenate([np.repeat(gates[:, None], f, 1), up], axis=1)
+    q_ref, byte_ref = P.pack8(z)
+    assert np.array_equal(P.unpack8(q_ref, byte_ref).reshape(z.shape), z)             # nothing is lost in 8 bits
+    want = quantize((gates.astype(np.float32) * s)[:, None] * up.astype(np.float32), "bf16")
+    z_, da = to_dev(z, "bf16"), torch.ones((T, f), dtype=torch.bfloat16, device="cuda")
+    a, again, dz = torch.empty_like(da), torch.empty_like(da), torch.empty_like(z_)
+    q, scale = torch.empty(z.size, dtype=torch.int8, device="cuda"), torch.empty(z.size // 32, dtype=torch.uint8, device="cuda")
+    mb.op_act_fwd_pack8(None, 256, "bf16", "swiglu", T, f, z_, a, q, scale)
+    mb.op_act_bwd_pack8(None, 256, "bf16", "swiglu", T, f, q, scale, da, dz, again)
+    for got in (a, again):
+        off = from_dev(got) != want
+        assert not off.any(), (int(off.sum()), gates[off.any(1)])
