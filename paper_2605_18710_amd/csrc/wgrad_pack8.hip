@@ -61,7 +61,8 @@ struct Args {
 // where a CU has one workgroup of four waves; the second group fills its gaps (0.57 us for both steps).
 // Steps are requested kAhead rounds ahead, in registers; a group's two tiles in LDS take turns, and the next round's numbers are converted while
 // these operands are on their way from LDS.
-template <int G>
+// SHARED: one tile holds columns 0 to 15 and the last block, which T k ends within.
+template <int G, bool SHARED>
 __global__ __launch_bounds__(256 * G) void wgrad_pack8_kernel(Args p) {
   constexpr int kAhead = 4, kSteps = kTokens / 16;
   constexpr int kTileBytes = kTile * kTokens * 2, kStage = 2 * kTileBytes;
@@ -69,7 +70,8 @@ __global__ __launch_bounds__(256 * G) void wgrad_pack8_kernel(Args p) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, lane = threadIdx.x & 63, tid = threadIdx.x & 255;
   lds_byte* const lds = (lds_byte*)smem + group * 2 * kStage;
   const int wm = (wave >> 1 & 1) * 32, wn = (wave & 1) * 32;
-  const auto rq = rsrc(p.q, (int64_t)p.T * p.k), rs = rsrc(p.scale, ((int64_t)p.T * p.k + 31) / 32), ry = rsrc(p.dy, (int64_t)p.T * p.n * 2);
+  const auto rq = rsrc(p.q, (int64_t)p.T * p.k), ry = rsrc(p.dy, (int64_t)p.T * p.n * 2);
+  const unsigned numbers = (unsigned)p.T * (unsigned)p.k;
   const int rounds = (p.T + G * kTokens - 1) / (G * kTokens);
   const int row_a = tid >> 2, col_a = (tid & 3) * 16, row_b = tid >> 3, col_b = (tid & 7) * 8;
   for (int item = blockIdx.x; item < p.tiles_m * p.tiles_n; item += gridDim.x) {
@@ -77,12 +79,16 @@ __global__ __launch_bounds__(256 * G) void wgrad_pack8_kernel(Args p) {
     const bool with_db = p.db && m0 == 0;
     // Where this thread reads next.  Past the last token an offset is past its descriptor's end, and so is every offset of a column that the matrix does not
     // have: such requests give zeros, with no branch.  (Offsets stay below 2^31 + 2^31: wgrad_pack8_small.)
+    // So do those of exponent bytes but for one: where T k ends within a block, columns 0 to 15 behind the last token would get that block's byte, a NaN's
+    // perhaps, which makes NaN of zeros.  The tile that holds these columns holds none of that block's from 80 columns on: its bytes end before the block.  With fewer
+    // (SHARED) offsets are compared (2048 tokens 1024 x 1024 13.1 us, compared 14.2).
+    const auto rs = rsrc(p.scale, (numbers + (SHARED || m0 > 0 ? 31u : 0u)) / 32u);
     unsigned at_a = (m0 + col_a < p.k ? 0u : kOut) + (unsigned)(group * kTokens + row_a) * (unsigned)p.k + (unsigned)(m0 + col_a);
     unsigned at_b = (n0 + col_b < p.n ? 0u : kOut) + ((unsigned)(group * kTokens + row_b) * (unsigned)p.n + (unsigned)(n0 + col_b)) * 2u;
     struct Step { u32x4 q; unsigned s; u32x4 y[2]; } in[kAhead];
     auto request = [&](Step& r) {
       r.q = __builtin_amdgcn_raw_buffer_load_b128(rq, (int)at_a, 0, 0);
-      r.s = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(at_a >> 5), 0, 0);
+      r.s = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(SHARED && at_a >= numbers ? kOut : at_a >> 5), 0, 0);
       r.y[0] = __builtin_amdgcn_raw_buffer_load_b128(ry, (int)at_b, 0, 0);
       r.y[1] = __builtin_amdgcn_raw_buffer_load_b128(ry, (int)(at_b + 64u * (unsigned)p.n), 0, 0);
       at_a += (unsigned)(G * kTokens) * (unsigned)p.k;
@@ -195,8 +201,11 @@ mosaic_status launch_wgrad_pack8_small(hipStream_t s, int quota, int64_t T, int6
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
   // Two groups where a CU would have a workgroup to itself (1568 tokens 768 x 768 13.1 -> 11.5 us, 4096 tokens 1024 x 1024 28.8 -> 24.5; but 1500 tokens
   // 1280 x 1280, 400 tiles, 18.2 -> 19.6), and more than one step to share.
-  if (tiles <= 256 && T > kTokens) wgrad_pack8_kernel<2><<<grid_for(quota, 2, tiles), 512, 0, s>>>(p);
-  else wgrad_pack8_kernel<1><<<grid_for(quota, 2, tiles), 256, 0, s>>>(p);
+  auto launch = [&](auto shared) {
+    if (tiles <= 256 && T > kTokens) wgrad_pack8_kernel<2, decltype(shared)::value><<<grid_for(quota, 2, tiles), 512, 0, s>>>(p);
+    else wgrad_pack8_kernel<1, decltype(shared)::value><<<grid_for(quota, 2, tiles), 256, 0, s>>>(p);
+  };
+  if (k <= kTile && T * k % 32) launch(std::true_type{}); else launch(std::false_type{});
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }

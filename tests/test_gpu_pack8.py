@@ -321,3 +321,23 @@ def test_swiglu_from_8_bits_rounds_like_the_plain_form(mb):
     for got in (a, again):
         off = from_dev(got) != want
         assert not off.any(), (int(off.sum()), gates[off.any(1)])
+
+
+@pytest.mark.parametrize("T,k,n", [(37, 48, 64), (101, 48, 72), (101, 16, 520), (37, 80, 64), (101, 112, 200), (201, 1040, 1048), (4501, 48, 64)])
+def test_weight_gradient_of_a_last_block_with_nan(mb, T, k, n):
+    """T * k ends within a block: the NaN of that block stays in its columns, the last sixteen, in one launch (one group of waves or two, few or many
+    tiles) and, with many tokens and few tiles, in several."""
+    assert T * k % 32 == 16
+    x, dy = quantize(synth.normal(8300, (T, k)), "bf16"), quantize(synth.normal(8301, (T, n)), "bf16")
+    x[T - 1, k - 5] = np.inf
+    q, byte = P.pack8(x)
+    assert byte[-1] == 255 and (byte[:-1] < 255).all()
+    kept = P.unpack8(q, byte).reshape(T, k)
+    dw, db = torch.empty((k, n), dtype=torch.bfloat16, device="cuda"), torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    scratch = torch.empty(mb.linear_wgrad_pack8_scratch_bytes("bf16", T, k, n), dtype=torch.uint8, device="cuda")
+    mb.op_linear_wgrad_pack8(None, 256, "bf16", T, k, n, torch.from_numpy(q).cuda(), torch.from_numpy(byte).cuda(), to_dev(dy, "bf16"), dw, db, scratch)
+    got = from_dev(dw)
+    assert np.isnan(got[k - 16:]).all()
+    ref = kept[:, :k - 16].T @ dy
+    within(got[:k - 16], ref, last("bf16", ref) + (T + 8) * U * (np.abs(kept[:, :k - 16]).T @ np.abs(dy)), "dw")
+    within(from_dev(db), dy.sum(0), last("bf16", dy.sum(0)) + (T + 8) * U * np.abs(dy).sum(0), "db")
