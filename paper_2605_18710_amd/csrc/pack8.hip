@@ -193,9 +193,9 @@ template <typename T, int ACT> __device__ __forceinline__ float act_grad_of(floa
     if constexpr (sizeof(T) == 2) {
       const Gate g = gate_of(v);
       return g.s * fmaf(z * g.rest(), w, 1.f);
-    } else {
-      const float s = sigmoid_f(v);
-      return s + z * (s * (1.0f - s)) * w;
+    } else {                                              // e s is 1 - s with its digits: w z takes what a difference loses up to thirty times
+      const float e = expf(-v), s = 1.0f / (1.0f + e);
+      return s + z * (s * (fminf(e, 3e38f) * s)) * w;
     }
   } else if constexpr (sizeof(T) == 2) {
     const Normal n = normal_of(z);

@@ -341,3 +341,28 @@ def test_weight_gradient_of_a_last_block_with_nan(mb, T, k, n):
     ref = kept[:, :k - 16].T @ dy
     within(got[:k - 16], ref, last("bf16", ref) + (T + 8) * U * (np.abs(kept[:, :k - 16]).T @ np.abs(dy)), "dw")
     within(from_dev(db), dy.sum(0), last("bf16", dy.sum(0)) + (T + 8) * U * np.abs(dy).sum(0), "db")
+
+
+def test_tanh_gelu_derivative_f32(mb):
+    """The derivative s + z w p of the tanh form in fp32 keeps its digits where s is near 1; s = 1 / (1 + e), e = exp(-v), p = s (1 - s), v = c (z + 0.044715 z^3), w = v'.
+
+    Bound in u: v 7 |v| (five operations and two constants); e 7 |v| + 2 of its size, s (1 - s)(7 |v| + 2) + 2, p 7 |v| + 8 at most, w 5, the products 2: the second
+    term 7 |v| + 15 of its size; the sum and the product with da 2 of both sizes.  (With 1 - s as a difference p would be off by up to 1.5 of 1, which w z takes up to 30 times.)"""
+    T, f = 64, 1024
+    z = quantize(synth.normal(8400, (T, f), 0.0, 1.0) * np.exp(np.linspace(-4.0, 2.5, T))[:, None], "f32")
+    da = quantize(synth.normal(8401, (T, f)), "f32")
+    q, byte = P.pack8(z)
+    z = P.unpack8(q, byte).reshape(T, f)
+    c = math.sqrt(2 / math.pi) * 2
+    v, w = c * (z + 0.044715 * z ** 3), c * (1 + 3 * 0.044715 * z * z)
+    with np.errstate(over="ignore"):
+        s, rest = 1 / (1 + np.exp(-v)), 1 / (1 + np.exp(v))
+    second = z * w * s * rest
+    bound = U * np.abs(da) * (s * (rest * (7 * np.abs(v) + 2) + 2) + np.abs(second) * (7 * np.abs(v) + 15) + 2 * (s + np.abs(second))) + 1e-36
+    dz = torch.empty((T, f), device="cuda")
+    mb.op_act_bwd_pack8(None, 256, "f32", "gelu_tanh", T, f, torch.from_numpy(q).cuda(), torch.from_numpy(byte).cuda(), to_dev(da, "f32"), dz)
+    within(from_dev(dz), da * (s + second), bound, "dz")
+    shifted, any_dz = Bytes(T * f, 1), torch.empty((T, f), device="cuda")                # element by element
+    shifted.t.copy_(torch.from_numpy(q.view(np.uint8)))
+    mb.op_act_bwd_pack8(None, 256, "f32", "gelu_tanh", T, f, shifted.t, torch.from_numpy(byte).cuda(), to_dev(da, "f32"), any_dz)
+    within(from_dev(any_dz), da * (s + second), bound, "dz, element by element")
