@@ -521,7 +521,8 @@ mosaic_status mosaic_op_act_bwd_pack8(void* stream, int32_t quota, int32_t dtype
 /* mosaic_op_linear_wgrad for an input X [T,k] that was kept in 8 bits (Xq, Xscale): dW[k,n] = X^T dY, db[n] = column
  * sums of dY (may be NULL); dY, dW, db of `dtype`, T > 0; with db, n must be a multiple of 8
  * (bf16) or 4 (fp32).  scratch: 16-byte aligned device buffer of
- * mosaic_op_linear_wgrad_pack8_scratch_bytes(dtype, T, k, n), not shared by calls that overlap in time. */
+ * mosaic_op_linear_wgrad_pack8_scratch_bytes(dtype, T, k, n), apart from all other buffers and not shared by calls
+ * that overlap in time. */
 mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t dtype, int64_t T,
                                            int64_t k, int64_t n, const void* Xq, const void* Xscale,
                                            const void* dY, void* dW, void* db, void* scratch);

@@ -420,6 +420,13 @@ mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t 
   const int vn = dtype == MOSAIC_BF16 ? 8 : 4;
   if (db && n % vn) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "column sums of rows of %lld elements, not a multiple of %d", (long long)n, vn);
   if ((uintptr_t)scratch % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 16-byte aligned");
+  const int64_t es = (int64_t)dtype_size(dtype), scales = (int64_t)mosaic_op_pack8_scale_bytes(T * k), needed = (int64_t)mosaic_op_linear_wgrad_pack8_scratch_bytes(dtype, T, k, n);
+  APART(dW, k * n * es, Xq, T * k); APART(dW, k * n * es, Xscale, scales); APART(dW, k * n * es, dY, T * n * es);
+  APART(scratch, needed, Xq, T * k); APART(scratch, needed, Xscale, scales); APART(scratch, needed, dY, T * n * es); APART(scratch, needed, dW, k * n * es);
+  if (db) {
+    APART(db, n * es, Xq, T * k); APART(db, n * es, Xscale, scales); APART(db, n * es, dY, T * n * es); APART(db, n * es, dW, k * n * es);
+    APART(db, n * es, scratch, needed);
+  }
   MOSAIC_TRY(check_common(quota, dtype));
   return launch_linear_wgrad_pack8((hipStream_t)stream, quota, dtype, T, k, n, Xq, Xscale, dY, dW, db, scratch);
 }

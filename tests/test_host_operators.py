@@ -103,3 +103,19 @@ def test_unknown_numbers():
     sections = (mb.C.c_int32 * 1)(8)
     assert l.mosaic_op_rope_axes_table(None, 256, 64, 1, sections, 3, 10.0, A) == mb.EINVAL
     assert l.mosaic_op_rope_axes_table(None, 256, 64, 1, None, 0, 10.0, A) == mb.EINVAL
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_packed_weight_gradient_with_buffers_that_overlap(dtype):
+    T, k, n, es = 40, 16, 24, 4 if dtype == "f32" else 2
+    size = mb.linear_wgrad_pack8_scratch_bytes(dtype, T, k, n)
+    G = 0x70000000
+    call = lambda q=A, scale=B, dy=C, dw=D, db=E, scratch=F: status(mb.op_linear_wgrad_pack8, None, 256, dtype, T, k, n, q, scale, dy, dw, db, scratch)
+    inputs = ((A, T * k), (B, T * k // 32), (C, T * n * es))
+    for first, length in inputs:
+        for other in (first, first + length - 1):
+            assert call(dw=other) == call(db=other) == mb.EINVAL
+        assert call(scratch=first) == call(dw=first - k * n * es + 1) == call(db=first - n * es + 1) == mb.EINVAL
+        assert call(scratch=first - (size - 1) // 16 * 16) == call(scratch=first + (length - 1) // 16 * 16) == mb.EINVAL
+    assert call(db=D) == call(db=D + k * n * es - 1) == call(db=D - n * es + 1) == call(scratch=D) == call(scratch=E) == call(db=F + size - 1) == call(dw=F + size - 1) == mb.EINVAL
+    assert status(mb.op_linear_wgrad_pack8, None, 256, dtype, T, k, n, A, B, C, C, None, G) == mb.EINVAL             # without db too
