@@ -519,7 +519,7 @@ mosaic_status mosaic_op_act_bwd_pack8(void* stream, int32_t quota, int32_t dtype
                                       int64_t f, const void* zq, const void* zscale, const void* da,
                                       void* dz, void* a);
 /* mosaic_op_linear_wgrad for an input X [T,k] that was kept in 8 bits (Xq, Xscale): dW[k,n] = X^T dY, db[n] = column
- * sums of dY (may be NULL); dY, dW, db of `dtype`, T > 0; with db, n must be a multiple of 8
+ * sums of dY (may be NULL); dY, dW, db of `dtype`, T > 0, all sizes below 2^31; with db, n must be a multiple of 8
  * (bf16) or 4 (fp32).  scratch: 16-byte aligned device buffer of
  * mosaic_op_linear_wgrad_pack8_scratch_bytes(dtype, T, k, n), apart from all other buffers and not shared by calls
  * that overlap in time. */

@@ -417,6 +417,7 @@ mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t 
   if (T < 0 || k <= 0 || n <= 0) MOSAIC_FAIL(MOSAIC_EINVAL, "bad linear sizes");
   if (T == 0) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "weight gradient over zero tokens");
   MOSAIC_TRY(check_packed(dtype, T, k)); MOSAIC_TRY(check_packed(dtype, T, n)); MOSAIC_TRY(check_packed(dtype, k, n));
+  if (T > INT32_MAX || k > INT32_MAX || n > INT32_MAX) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "sizes past 2^31 - 1: %lld x %lld x %lld", (long long)T, (long long)k, (long long)n);
   const int vn = dtype == MOSAIC_BF16 ? 8 : 4;
   if (db && n % vn) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "column sums of rows of %lld elements, not a multiple of %d", (long long)n, vn);
   if ((uintptr_t)scratch % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 16-byte aligned");

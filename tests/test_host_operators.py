@@ -119,3 +119,9 @@ def test_packed_weight_gradient_with_buffers_that_overlap(dtype):
         assert call(scratch=first - (size - 1) // 16 * 16) == call(scratch=first + (length - 1) // 16 * 16) == mb.EINVAL
     assert call(db=D) == call(db=D + k * n * es - 1) == call(db=D - n * es + 1) == call(scratch=D) == call(scratch=E) == call(db=F + size - 1) == call(dw=F + size - 1) == mb.EINVAL
     assert status(mb.op_linear_wgrad_pack8, None, 256, dtype, T, k, n, A, B, C, C, None, G) == mb.EINVAL             # without db too
+
+
+def test_packed_weight_gradient_of_sizes_past_31_bits():
+    """Refused before the input is unpacked: nothing is launched for a call that fails."""
+    for T, k, n in ((1 << 31, 8, 8), (8, 1 << 31, 8), (8, 8, 1 << 31)):
+        assert status(mb.op_linear_wgrad_pack8, None, 256, "bf16", T, k, n, 1 << 40, 1 << 42, 1 << 44, 1 << 46, None, 1 << 48) == mb.EUNSUPPORTED
