@@ -487,8 +487,9 @@ mosaic_status mosaic_op_qk_norm_rope_fwd(void* stream, int32_t quota, int32_t dt
 /* Its backward pass: x, the rows before the norm; dy, the gradient of y ([dq | dk | dv], as
  * mosaic_op_attention_gqa_bwd gives it); dx, the gradient of x (dx may be dy and must not
  * overlap x or dy otherwise; v's part is dy's); dgamma_q, dgamma_k, and for LayerNorm dbeta_q, dbeta_k, [d] each, sums over tokens and heads
- * in a fixed order (overwritten; zero for T = 0).  scratch: 16-byte aligned device buffer of
- * mosaic_op_qk_norm_rope_bwd_scratch_bytes(d), not shared by calls that overlap in time. */
+ * in a fixed order (overwritten; zero for T = 0; apart from each other and from dx).  scratch: 16-byte aligned device
+ * buffer of mosaic_op_qk_norm_rope_bwd_scratch_bytes(d), apart from all other buffers and not shared by calls that
+ * overlap in time. */
 mosaic_status mosaic_op_qk_norm_rope_bwd(void* stream, int32_t quota, int32_t dtype, int32_t norm,
                                          int64_t T, int32_t H, int32_t Hkv, int32_t d, float eps,
                                          int32_t pairing, int32_t n_axes, const int32_t* pos,

@@ -347,6 +347,18 @@ mosaic_status mosaic_op_qk_norm_rope_bwd(void* stream, int32_t quota, int32_t dt
   APART(x, bytes, dx, bytes);
   if (dy != dx) APART(dy, bytes, dx, bytes);
   if ((uintptr_t)scratch % 16) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 16-byte aligned");
+  // the gains' and shifts' gradients are sums that a second launch takes from scratch
+  const int64_t gain = d * (int64_t)dtype_size(dtype), needed = (int64_t)qk_norm_rope_bwd_scratch_bytes(d);
+  const bool layer = norm == MOSAIC_LAYERNORM;
+  const void* const sums[] = {dgamma_q, dgamma_k, layer ? dbeta_q : nullptr, layer ? dbeta_k : nullptr};
+  const char* const names[] = {"dgamma_q", "dgamma_k", "dbeta_q", "dbeta_k"};
+  for (int i = 0; i < 4; ++i) {
+    if (overlap(sums[i], gain, dx, bytes) || overlap(sums[i], gain, scratch, needed)) MOSAIC_FAIL(MOSAIC_EINVAL, "%s overlaps dx or scratch", names[i]);
+    for (int j = 0; j < i; ++j)
+      if (overlap(sums[i], gain, sums[j], gain)) MOSAIC_FAIL(MOSAIC_EINVAL, "%s overlaps %s", names[i], names[j]);
+  }
+  APART(scratch, needed, x, bytes); APART(scratch, needed, dy, bytes); APART(scratch, needed, dx, bytes);
+  APART(scratch, needed, gamma_q, gain); APART(scratch, needed, gamma_k, gain);
   MOSAIC_TRY(check_common(quota, dtype));
   return launch_qk_norm_rope_bwd((hipStream_t)stream, quota, dtype, norm, T, H, Hkv, d, eps, pairing, n_axes, pos, table, x, gamma_q, gamma_k, dy, dx,
                                  dgamma_q, dbeta_q, dgamma_k, dbeta_k, scratch);

@@ -125,3 +125,21 @@ def test_packed_weight_gradient_of_sizes_past_31_bits():
     """Refused before the input is unpacked: nothing is launched for a call that fails."""
     for T, k, n in ((1 << 31, 8, 8), (8, 1 << 31, 8), (8, 8, 1 << 31)):
         assert status(mb.op_linear_wgrad_pack8, None, 256, "bf16", T, k, n, 1 << 40, 1 << 42, 1 << 44, 1 << 46, None, 1 << 48) == mb.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("norm", ["rmsnorm", "layernorm"])
+def test_gradients_of_head_norms_that_overlap(norm):
+    """The four gradients, the rows' gradient and scratch memory each lie apart: the sums are written while others are read."""
+    d, row, es = 64, 8 * 64, 2
+    size = mb.qk_norm_rope_bwd_scratch_bytes(d)
+    layer = norm == "layernorm"
+    apart = dict(dgq=E, dgk=E + 512, **(dict(dbq=E + 1024, dbk=E + 1536) if layer else {}))
+    call = lambda **kw: bwd(norm=norm, **{**apart, **kw})
+    for one in apart:
+        for other in apart:
+            if other != one:
+                assert call(**{one: apart[other]}) == call(**{one: apart[other] + d * es - 2}) == mb.EINVAL
+        assert call(**{one: D}) == call(**{one: D + 4 * row * es - 2}) == call(**{one: F}) == call(**{one: F + size - 2}) == mb.EINVAL
+    for buffer in (C, D):
+        assert call(scratch=buffer) == call(scratch=buffer + 4 * row * es - 16) == call(scratch=buffer - size + 16) == mb.EINVAL
+    assert call(scratch=A + 64, dx=D) == call(scratch=A + 256) == mb.EINVAL                     # the gains
