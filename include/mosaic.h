@@ -468,7 +468,8 @@ mosaic_status mosaic_op_rope_axes_table(void* stream, int32_t quota, int32_t d, 
 /* x, y [T, (H + 2*Hkv)*d], row = [q (H heads) | k (Hkv heads) | v (Hkv heads)], Hkv divides H: the q
  * and k heads of x rotated (direction = +1) or turned back (-1: gradients of rotated q, k), v as it is.
  * y may be x; it must not overlap it otherwise.  A pair whose axis is n_axes or more (a
- * table made for more axes) stays as it is.  A NaN or an infinity makes its pair NaN (with a norm, its head).  The tokens may be any set: a batch, packed sequences, the
+ * table made for more axes) stays as it is.  NaNs and infinities go by the formulas: one of them makes its pair NaN or infinite (a pair that
+ * stays is turned by 0: an infinity makes the other element NaN).  The tokens may be any set: a batch, packed sequences, the
  * single tokens of a serving step. */
 mosaic_status mosaic_op_rope_axes(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t H,
                                   int32_t Hkv, int32_t d, int32_t pairing, int32_t direction,
@@ -477,7 +478,8 @@ mosaic_status mosaic_op_rope_axes(void* stream, int32_t quota, int32_t dtype, in
 /* A norm over the d elements of every query and key head, and the rotation of the result, in one
  * pass: norm = MOSAIC_RMSNORM (x * rstd * gamma; beta_q, beta_k unused) or MOSAIC_LAYERNORM
  * ((x - mean) * rstd * gamma + beta), eps > 0.  gamma_q, beta_q [d] are shared by the query heads, gamma_k, beta_k [d]
- * by the key heads.  table == NULL (then pos may be NULL and n_axes 0): no rotation. */
+ * by the key heads.  table == NULL (then pos may be NULL and n_axes 0): no rotation.  A NaN makes its head NaN, and so does an
+ * infinity under LayerNorm; under RMS norm, where rstd becomes 0, it makes its pair NaN and the rest of its head 0. */
 mosaic_status mosaic_op_qk_norm_rope_fwd(void* stream, int32_t quota, int32_t dtype, int32_t norm,
                                          int64_t T, int32_t H, int32_t Hkv, int32_t d, float eps,
                                          int32_t pairing, int32_t n_axes, const int32_t* pos,

@@ -307,3 +307,65 @@ def test_captured_and_replayed(mb):
         graph.replay()
         torch.cuda.synchronize()
         assert all(np.array_equal(a, bits(t)) for a, t in zip(want, (y, dx, *dg)))
+
+
+def same_kinds(got, ref, bound, what):
+    """NaNs and infinities where the formulas have them, with their signs, and the other numbers within the bound."""
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), (what, np.argwhere(np.isnan(got) != np.isnan(ref))[:4])
+    assert np.array_equal(np.where(np.isinf(got), got, 0), np.where(np.isinf(ref), ref, 0)), what
+    fine = np.isfinite(ref)
+    within(got[fine], ref[fine], np.broadcast_to(bound, ref.shape)[fine], what)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("norm", ["none", "rmsnorm", "layernorm"])
+@pytest.mark.parametrize("pairing", ["adjacent", "halves"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_nan_and_infinity_go_by_the_formulas(mb, dtype, norm, pairing, shift):
+    """In turned pairs and in ones that stay, of queries, keys and v; what does not meet them is as without them.  Under RMS norm an infinity makes its pair NaN
+    and the rest of its head 0; under LayerNorm its head NaN; in the backward pass either makes its head NaN, and a gain's gradient NaN where it met one."""
+    c = Case(mb, dtype, norm, 6, 4, 2, 64, (11, 12), "split", pairing)            # pairs 23 to 31 stay
+    turned, stays = (5, 26) if pairing == "halves" else (10, 52)
+    c.pos[:, 3] = 0                                                               # cosine 1 and sine 0
+    c.pos_.copy_(torch.from_numpy(c.pos.astype(np.int32)))
+    x = c.x.reshape(6, 8, 64)
+    for at, v in (((0, 1, turned), np.nan), ((1, 2, turned), np.inf), ((2, 4, turned + 1), -np.inf), ((2, 0, stays), np.inf), ((3, 5, turned), np.inf),
+                  ((4, 3, stays), np.nan), ((4, 7, 9), np.inf), ((5, 6, 8), np.nan)):
+        x[at] = v
+    x_, y = Framed(c.x, dtype, shift), Framed(None, dtype, shift, c.x.shape)
+    q, k, v = c.parts(c.x)
+    with np.errstate(invalid="ignore", over="ignore"):
+        if norm == "none":
+            mb.op_rope_axes(None, 256, dtype, 6, 4, 2, 64, pairing, 1, 2, c.pos_, c.table_, x_.t, y.t)
+            n = [q, k]
+        else:
+            norm_fwd(mb, c, x_.t, y.t, 256)
+            n = [P.head_norm(p, norm, 1e-5, g, s)[0] for p, g, s in zip((q, k), c.gains, c.shifts)]
+        ref = np.concatenate([c.rotate(p) for p in n] + [v], axis=1)
+        top = max(np.abs(p[np.isfinite(p)]).max() for p in n) + 4
+        got = from_dev(y.t).reshape(ref.shape)
+        same_kinds(got, ref, last(dtype, ref) + 64 * U * top, "y")
+        if norm == "rmsnorm":
+            other = [i for i in range(64) if i not in ((5, 37) if pairing == "halves" else (10, 11))]
+            assert np.isnan(got[1, 2]).sum() == 2 and (got[1, 2, other] == 0).all()
+        elif norm == "layernorm":
+            assert np.isnan(got[1, 2]).all() and np.isnan(got[3, 5]).all()
+        if norm == "none":
+            return
+        c.dy.reshape(6, 8, 64)[0, 0, turned] = np.nan
+        dy_, dx = Framed(c.dy, dtype, shift), Framed(None, dtype, shift, c.x.shape)
+        scratch = torch.empty(mb.qk_norm_rope_bwd_scratch_bytes(64), dtype=torch.uint8, device="cuda")
+        _, grads = norm_bwd(mb, c, x_.t, dy_.t, dx.t, 256, scratch)
+        refs = []
+        for part, (p, d, gain, sh) in enumerate(zip((q, k), c.parts(c.dy), c.gains, c.shifts)):
+            _, xhat, rstd = P.head_norm(p, norm, 1e-5, gain, sh)
+            g = c.rotate(d, -1)
+            dx_ref, dgain, dshift = P.head_norm_bwd(g, xhat, rstd, norm, gain)
+            refs.append(dx_ref)
+            assert np.array_equal(np.isnan(from_dev(grads[part].t)), np.isnan(dgain))
+            if norm == "layernorm":
+                assert np.array_equal(np.isnan(from_dev(grads[2 + part].t)), np.isnan(dshift))
+        ref = np.concatenate(refs + [c.parts(c.dy)[2]], axis=1)
+        got = from_dev(dx.t).reshape(ref.shape)
+        assert np.array_equal(np.isnan(got), np.isnan(ref)) and not np.isinf(got).any()
+        assert np.isnan(got[1, 2]).all() and np.isnan(got[0, 1]).all() and np.isfinite(got[1, 3]).all()
