@@ -366,3 +366,63 @@ def test_tanh_gelu_derivative_f32(mb):
     shifted.t.copy_(torch.from_numpy(q.view(np.uint8)))
     mb.op_act_bwd_pack8(None, 256, "f32", "gelu_tanh", T, f, shifted.t, torch.from_numpy(byte).cuda(), to_dev(da, "f32"), any_dz)
     within(from_dev(any_dz), da * (s + second), bound, "dz, element by element")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("shifts", [(1, 0, 0), (0, 1, 0), (0, 0, 1), (0, 0, 4), (1, 1, 1)])
+@pytest.mark.parametrize("T,k,n,db", [(70, 48, 72, True), (37, 64, 64, False), (513, 40, 88, True)])
+def test_weight_gradient_off_boundaries(mb, dtype, shifts, T, k, n, db):
+    """Numbers, exponent bytes, dY and the outputs off 16-byte boundaries by some elements."""
+    x, dy = quantize(synth.normal(8500, (T, k)), dtype), quantize(synth.normal(8501, (T, n)), dtype)
+    q, byte = P.pack8(x)
+    kept = P.unpack8(q, byte).reshape(T, k)
+    q_, s_ = Bytes(T * k, shifts[0]), Bytes(byte.size, 3 * shifts[0])
+    q_.t.copy_(torch.from_numpy(q.view(np.uint8))); s_.t.copy_(torch.from_numpy(byte))
+    dy_, dw, bias = Framed(dy, dtype, shifts[1]), Framed(None, dtype, shifts[2], (k, n)), Framed(None, dtype, shifts[2], (n,))
+    scratch = Bytes(mb.linear_wgrad_pack8_scratch_bytes(dtype, T, k, n))
+    mb.op_linear_wgrad_pack8(None, 256, dtype, T, k, n, q_.t, s_.t, dy_.t, dw.t, bias.t if db else None, scratch.t)
+    torch.cuda.synchronize()
+    assert all(b.framed() for b in (q_, s_, dy_, dw, bias, scratch))
+    ref = kept.T @ dy
+    within(from_dev(dw.t), ref, last(dtype, ref) + (T + 8) * U * (np.abs(kept).T @ np.abs(dy)), "dw")
+    if db:
+        within(from_dev(bias.t), dy.sum(0), last(dtype, dy.sum(0)) + (T + 8) * U * np.abs(dy).sum(0), "db")
+    else:
+        assert (bias.t == 7.0).all()
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh"])
+def test_gelu_past_the_caches(mb, act):
+    """More than 256 MB read and written, a size that is no multiple of a block: every element, against 64 bits on the GPU; with and without the activation again."""
+    T, f = 8213, 6603
+    n = T * f
+    assert 5 * n > 256 << 20 and n % 32
+    g = torch.Generator(device="cuda").manual_seed(92)
+    z, da = (torch.randn((T, f), generator=g, device="cuda") * 2).bfloat16(), torch.randn((T, f), generator=g, device="cuda").bfloat16()
+    a, again, dz, alone = (torch.empty_like(da) for _ in range(4))
+    q, scale = torch.empty(n, dtype=torch.int8, device="cuda"), torch.empty(mb.pack8_scale_bytes(n), dtype=torch.uint8, device="cuda")
+    mb.op_act_fwd_pack8(None, 256, "bf16", act, T, f, z, a, q, scale)
+    mb.op_act_bwd_pack8(None, 256, "bf16", act, T, f, q, scale, da, dz, again)
+    mb.op_act_bwd_pack8(None, 256, "bf16", act, T, f, q, scale, da, alone)
+    assert torch.equal(alone, dz)
+    q_, scale_ = torch.empty_like(q), torch.empty_like(scale)
+    mb.op_pack8(None, 256, "bf16", n, z, q_, scale_)
+    assert torch.equal(q, q_) and torch.equal(scale, scale_)
+    for part in (slice(0, 3200), slice(n // 32 * 32 - 3200, n)):
+        q_ref, byte_ref = P.pack8(from_dev(z.view(-1)[part]))
+        assert np.array_equal(q[part].cpu().numpy(), q_ref) and np.array_equal(scale[part.start // 32:][:byte_ref.size].cpu().numpy(), byte_ref)
+    kept = (q.double() * torch.exp2(scale.double() - 127).repeat_interleave(32)[:n]).view(T, f)
+
+    def ref(z):
+        if act == "gelu":
+            p = 0.5 * torch.erfc(-z * math.sqrt(0.5))
+            return z * p, p + z * torch.exp(-0.5 * z * z) / math.sqrt(2 * math.pi), 8, 8
+        c = math.sqrt(2 / math.pi)
+        t = torch.tanh(c * (z + 0.044715 * z ** 3))
+        return 0.5 * z * (1 + t), 0.5 * (1 + t) + 0.5 * z * (1 - t * t) * c * (1 + 3 * 0.044715 * z * z), 12, 128
+
+    for got, at, size in ((a, z.double(), None), (again, kept, None), (dz, kept, da.double())):
+        value, slope, by_value, by_slope = ref(at)
+        want = value if size is None else size * slope
+        bound = want.abs() * 2.0 ** -8 + (by_value * U * at.abs() if size is None else by_slope * U * (1 + at.abs()) * size.abs())
+        assert float(((got.double() - want).abs() - bound).max()) <= 0

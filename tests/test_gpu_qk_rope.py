@@ -369,3 +369,110 @@ def test_nan_and_infinity_go_by_the_formulas(mb, dtype, norm, pairing, shift):
         got = from_dev(dx.t).reshape(ref.shape)
         assert np.array_equal(np.isnan(got), np.isnan(ref)) and not np.isinf(got).any()
         assert np.isnan(got[1, 2]).all() and np.isnan(got[0, 1]).all() and np.isfinite(got[1, 3]).all()
+
+
+def rows_on_gpu(mb, dtype, norm, T, H, Hkv, d, pairing, seed):
+    """Rows, gradients and gains on the GPU, and y, dx and the gains' gradients in 64 bits from the definitions."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    td = torch.bfloat16 if dtype == "bf16" else torch.float32
+    n = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(td)
+    x, dy, w = n(T, (H + 2 * Hkv) * d), n(T, (H + 2 * Hkv) * d), H + Hkv
+    gains, shifts = [n(d) for _ in range(2)], [n(d) for _ in range(2)]
+    pos = torch.randint(-5, 300, (2, T), generator=g, device="cuda", dtype=torch.int32)
+    sections = (d // 4, d // 4)
+    axis, freq = P.pair_table(d, sections, "dealt", 1e4)
+    table = torch.empty(mb.rope_axes_table_bytes(d), dtype=torch.uint8, device="cuda")
+    mb.op_rope_axes_table(None, 256, d, sections, "dealt", 1e4, table)
+    angle = (pos.double()[torch.from_numpy(axis).cuda()].t() * torch.from_numpy(freq).cuda())[:, None]
+    cos, sin = torch.cos(angle), torch.sin(angle)
+    cut = (lambda a: a.chunk(2, 2)) if pairing == "halves" else (lambda a: (a[..., 0::2], a[..., 1::2]))
+
+    def turned(a, sign):
+        p, q = cut(a)
+        parts = (p * cos - sign * q * sin, sign * p * sin + q * cos)
+        return torch.cat(parts, 2) if pairing == "halves" else torch.stack(parts, 3).flatten(2)
+
+    per_head = lambda pair: torch.cat((pair[0].double().expand(H, d), pair[1].double().expand(Hkv, d)))
+    gain, shift = per_head(gains), per_head(shifts)
+    layer = norm == "layernorm"
+    xs, ds = x.view(T, -1, d)[:, :w].double(), dy.view(T, -1, d)[:, :w].double()
+    centred = xs - xs.mean(2, keepdim=True) if layer else xs
+    rstd = torch.rsqrt((centred * centred).mean(2, keepdim=True) + 1e-5)
+    xhat = centred * rstd
+    y = turned(xhat * gain + shift if layer else xhat * gain, 1)
+    up = turned(ds, -1)
+    m = up * gain
+    dx = rstd * (m - (m.mean(2, keepdim=True) if layer else 0) - xhat * (m * xhat).mean(2, keepdim=True))
+    peak = 2 * ds.abs().amax(2, keepdim=True) * gain.abs().max()
+    part = lambda a: (a[:, :H].sum((0, 1)), a[:, H:].sum((0, 1)))
+    return dict(x=x, dy=dy, gains=gains, shifts=shifts, pos=pos, table=table, y=y, dx=dx, y_size=2 * (xhat.abs().amax(2, keepdim=True) * gain.abs().max() + shift.abs().max()),
+                dx_size=rstd * peak * (2 + xhat.abs().amax(2, keepdim=True)), dgain=part(up * xhat), dshift=part(up), dgain_size=part((up * xhat).abs() + up.abs()),
+                dshift_size=part(2 * up.abs()))
+
+
+def near(got, ref, bound, what):
+    over = (got.double() - ref).abs() - bound
+    assert bool(torch.isfinite(got).all()) and float(over.max()) <= 0, (what, float(over.max()))
+
+
+@pytest.mark.parametrize("dtype,norm,T,H,Hkv,d,pairing", [
+    ("bf16", "rmsnorm", 33000, 12, 4, 128, "halves"), ("bf16", "layernorm", 33000, 12, 4, 128, "adjacent"), ("f32", "layernorm", 33000, 12, 4, 64, "halves"),
+    ("f32", "rmsnorm", 33000, 6, 2, 128, "adjacent"), ("bf16", "rmsnorm", 17000, 12, 4, 256, "adjacent")])
+def test_rows_past_the_caches(mb, dtype, norm, T, H, Hkv, d, pairing):
+    """More than 256 MB read and written, in rows whose halves of a head are whole lines, also in place; every element, and the gains' sums over more than 8192 tokens
+    (about 200 additions one after the other: waves of 9 tokens of 12 heads, 8 waves, slices of 64 partitions)."""
+    es = 2 if dtype == "bf16" else 4
+    assert 2 * T * (H + Hkv) * d * es > 256 << 20 and d // 2 * es % 128 == 0
+    r = rows_on_gpu(mb, dtype, norm, T, H, Hkv, d, pairing, 91)
+    layer, w, rel = norm == "layernorm", H + Hkv, 2.0 ** -8 if dtype == "bf16" else 0.0
+    head = (T, H, Hkv, d, 1e-5, pairing, 2, r["pos"], r["table"])
+    gq, gk, bq, bk = r["gains"][0], r["gains"][1], r["shifts"][0] if layer else None, r["shifts"][1] if layer else None
+    y = torch.empty_like(r["x"])
+    mb.op_qk_norm_rope_fwd(None, 256, dtype, norm, *head, r["x"], gq, bq, gk, bk, y)
+    rows = lambda t: t.view(T, -1, d)
+    near(rows(y)[:, :w], r["y"], r["y"].abs() * rel + 32 * U * r["y_size"], "y")
+    assert torch.equal(rows(y)[:, w:], rows(r["x"])[:, w:])
+    here = r["x"].clone()
+    mb.op_qk_norm_rope_fwd(None, 256, dtype, norm, *head, here, gq, bq, gk, bk, here)
+    assert torch.equal(here, y)
+    outs = []
+    for quota, into in ((256, torch.empty_like(y)), (64, torch.empty_like(y)), (256, r["dy"].clone())):
+        grads = [torch.empty_like(gq) for _ in range(4)]
+        scratch = torch.empty(mb.qk_norm_rope_bwd_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+        up = into if len(outs) == 2 else r["dy"]
+        mb.op_qk_norm_rope_bwd(None, quota, dtype, norm, *head, r["x"], gq, gk, up, into, grads[0], grads[2] if layer else None, grads[1], grads[3] if layer else None, scratch)
+        outs.append([into] + grads[:4 if layer else 2])
+    assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(outs[0], o))
+    near(rows(outs[0][0])[:, :w], r["dx"], r["dx"].abs() * rel + 64 * U * r["dx_size"], "dx")
+    assert torch.equal(rows(outs[0][0])[:, w:], rows(r["dy"])[:, w:])
+    for part in (0, 1):
+        near(outs[0][1 + part], r["dgain"][part], r["dgain"][part].abs() * rel + 512 * U * r["dgain_size"][part], ("dgain", part))
+        if layer:
+            near(outs[0][3 + part], r["dshift"][part], r["dshift"][part].abs() * rel + 512 * U * r["dshift_size"][part], ("dshift", part))
+
+
+@pytest.mark.parametrize("T,H,Hkv,d,shift", [(2100, 3, 1, 6, 0), (2600, 2, 1, 250, 0), (8300, 2, 1, 64, 1), (8300, 2, 1, 64, 0)])
+@pytest.mark.parametrize("norm", ["rmsnorm", "layernorm"])
+def test_partitions_of_more_tokens(mb, norm, T, H, Hkv, d, shift):
+    """Element by element, partitions of more than four tokens; in vectors, more than 8192 tokens; outputs off 16-byte boundaries."""
+    c = Case(mb, "bf16", norm, T, H, Hkv, d, (d // 4, d // 4), "dealt", "halves")
+    scratch = torch.full((mb.qk_norm_rope_bwd_scratch_bytes(d) // 4,), float("nan"), device="cuda")
+    outs, layer = [], norm == "layernorm"
+    for quota in (256, 24):
+        x, dy, dx = Framed(c.x, "bf16", shift), Framed(c.dy, "bf16", shift), Framed(None, "bf16", shift, c.x.shape)
+        grads, gains = [Framed(None, "bf16", 1, (d,)) for _ in range(4)], [to_dev(v, "bf16") for v in c.gains]
+        mb.op_qk_norm_rope_bwd(None, quota, "bf16", norm, T, H, Hkv, d, 1e-5, "halves", 2, c.pos_, c.table_, x.t, gains[0], gains[1], dy.t, dx.t, grads[0].t,
+                               grads[2].t if layer else None, grads[1].t, grads[3].t if layer else None, scratch)
+        torch.cuda.synchronize()
+        assert x.framed() and dy.framed() and dx.framed() and all(g.framed() for g in grads)
+        outs.append([bits(dx.t)] + [bits(g.t) for g in grads])
+    assert all(np.array_equal(a, b) for a, b in zip(*outs))
+    for part in (0, 1):
+        _, xhat, rstd = P.head_norm(c.parts(c.x)[part], norm, 1e-5, c.gains[part], c.shifts[part])
+        g = c.rotate(c.parts(c.dy)[part], -1)
+        dx_ref, dgain, dshift = P.head_norm_bwd(g, xhat, rstd, norm, c.gains[part])
+        size = rstd * 2 * np.abs(c.gains[part]).max() * np.abs(c.parts(c.dy)[part]).max(2, keepdims=True) * (2 + np.abs(xhat).max(2, keepdims=True))
+        within(c.parts(from_dev(dx.t))[part], dx_ref, last("bf16", dx_ref) + 64 * U * size, "dx")
+        within(from_dev(grads[part].t), dgain, last("bf16", dgain) + 512 * U * (np.abs(g * xhat) + np.abs(g)).sum((0, 1)), "dgain")
+        if layer:
+            within(from_dev(grads[2 + part].t), dshift, last("bf16", dshift) + 1024 * U * np.abs(g).sum((0, 1)), "dshift")
