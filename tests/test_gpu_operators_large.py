@@ -101,3 +101,41 @@ def test_activation_behind_four_gigabytes(mb, f):
         within(from_dev(a[rows]), a_ref, last("bf16", a_ref) + a_tol, "a")
         within(from_dev(again[rows]), again_ref, last("bf16", again_ref) + again_tol, "again")
         within(from_dev(dz[rows]), dz_ref, last("bf16", dz_ref) + dz_tol, "dz")
+
+
+def test_gains_gradients_over_five_million_tokens(mb):
+    """Sums over all tokens in 32 bits, against 64, of gradients that lie on the normalised rows: the sums grow with the tokens, so that a partition, or a wave's
+    share of one (1 of 4096), that were missing would be 2e-3 or 2e-4 of them.  A wave adds up 1221 tokens, all heads at once; then come 3 joins of heads, 8 waves
+    and slices of 64 partitions: below 1400 additions in a row, of terms off by 40 u, 1440 u in all (9e-5)."""
+    T, H, Hkv, d = 5000001, 2, 1, 64
+    w = (H + 2 * Hkv) * d
+    assert T * w * 4 > 1 << 32
+    x = filled(T * w, 6).view(T, w).float()
+    pos = torch.stack((torch.arange(T, device="cuda") % 4096, torch.arange(T, device="cuda") % 1000)).to(torch.int32).contiguous()
+    table = torch.empty(mb.rope_axes_table_bytes(d), dtype=torch.uint8, device="cuda")
+    mb.op_rope_axes_table(None, 256, d, (16, 16), "own", 100.0, table)
+    axis, freq = (torch.from_numpy(v).cuda() for v in P.pair_table(d, (16, 16), "own", 100.0))
+    one = torch.ones(d, device="cuda")
+    head = (T, H, Hkv, d, 1e-5, "halves", 2, pos, table)
+    y, grads = torch.empty_like(x), [torch.empty_like(one) for _ in range(4)]
+    mb.op_qk_norm_rope_fwd(None, 256, "f32", "layernorm", *head, x, one, one, one, one, y)          # turned: xhat + 1
+    scratch = torch.empty(mb.qk_norm_rope_bwd_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+    mb.op_qk_norm_rope_bwd(None, 256, "f32", "layernorm", *head, x, one, one, y, torch.empty_like(x), grads[0], grads[2], grads[1], grads[3], scratch)
+    sums = torch.zeros((4, 2, d), dtype=torch.float64, device="cuda")              # [gain q, gain k, shift q, shift k][sum, sum of sizes]
+    for first in range(0, T, 1 << 20):
+        rows = slice(first, min(T, first + (1 << 20)))
+        xs, ds = (v[rows].view(-1, H + 2 * Hkv, d)[:, :H + Hkv].double() for v in (x, y))
+        angle = (pos[:, rows].double()[axis].t() * freq)[:, None]
+        p, q = ds.chunk(2, 2)
+        g = torch.cat((p * torch.cos(angle) + q * torch.sin(angle), q * torch.cos(angle) - p * torch.sin(angle)), 2)
+        xhat = xs - xs.mean(2, keepdim=True)
+        xhat = xhat * torch.rsqrt((xhat * xhat).mean(2, keepdim=True) + 1e-5)
+        for i, term in enumerate(((g * xhat)[:, :H], (g * xhat)[:, H:], g[:, :H], g[:, H:])):
+            sums[i, 0] += term.sum((0, 1))
+            sums[i, 1] += term.abs().sum((0, 1))
+    for i, got in enumerate(grads):
+        heads = Hkv if i % 2 else H
+        # what a missing share is measured against: mean xhat^2 + xhat or xhat + 1 of a column's 131079 different numbers, off by sqrt(3 / 131079) = 0.005, six of these
+        assert float((sums[i, 0] / (T * heads) - 1).abs().max()) < 0.03
+        over = (got.double() - sums[i, 0]).abs() - 1440 * U * sums[i, 1]
+        assert float(over.max()) <= 0, (i, float(over.max()))
