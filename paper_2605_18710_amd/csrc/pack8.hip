@@ -171,7 +171,7 @@ __device__ __forceinline__ Gate gate_of(float z) {
 __device__ __forceinline__ float tanh_gelu_arg(float z) { return 1.5957691216057308f * (z + 0.044715f * z * z * z); }
 // e = exp(-z^2 / 2) and the normal distribution's phi = (1 + erf(z / sqrt 2)) / 2 for results in bf16.  erf by Hastings' approximation (Abramowitz and Stegun,
 // Handbook of Mathematical Functions, 7.1.26: 1 - (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), off by 1.5e-7), whose exponential GELU's derivative needs anyway:
-// phi is off by 1.3 * 2^-24 for it and 2 * 2^-24 for roundings.  e's rounded argument w costs w exp(-w) * 2^-24, which never passes 0.37.
+// phi is off by 1.3 * 2^-24 for it and 3 * 2^-24 for roundings (of 1, not of its own size).  e's rounded argument w costs w exp(-w) * 2^-24, which never passes 0.37.
 struct Normal { float e, phi; };
 __device__ __forceinline__ Normal normal_of(float z) {
   const float e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
@@ -265,8 +265,9 @@ __device__ __forceinline__ void place(int64_t i, int64_t fv, int64_t* r, int64_t
   }
 }
 
-// Bound by memory: 16384 x 11008 SwiGLU 240 us forward (6.1 TB/s; 281 with expf and a divide for the gate) and 295 backward (6.2), 32768 x 5120 GELU 138 (6.1) and
-// 185 (6.4; 236 with erf from a table in LDS, which keeps workgroups from starting in order).
+// Bound by memory: 16384 x 11008 SwiGLU 239 us forward (6.1 TB/s; 281 with expf and a divide for the gate) and 295 backward (6.2), 32768 x 5120 GELU 135 (6.2) and
+// 185 (6.4; 236 with erf from a table in LDS, which keeps workgroups from starting in order).  fp32, with expf, erff and a divide: 9216 x 4096 GELU 64 (5.4) and
+// 93 (5.3), its tanh form 67 (5.1) and 98 (5.0), 4096 x 5632 SwiGLU 58 (5.6) and 82 (5.1).
 // a = act(z) and z in 8 bits.  GELU forms: flat, any size.  SwiGLU: rows of f = 8 fv, f a multiple of 32, so that no block has elements of both halves.
 template <typename T, int ACT, bool PAST>
 __global__ __launch_bounds__(kThreads) void act_fwd_kernel(const T* __restrict__ z, T* __restrict__ a, int8_t* __restrict__ q, uint8_t* __restrict__ scale,
@@ -370,10 +371,11 @@ __global__ __launch_bounds__(kThreads) void act_bwd_kernel(const int8_t* __restr
   }
 }
 
-// Workgroups in order from 64 MB on (sweep_grid), striding / in order, us: 2^27 bf16 elements packed 76 / 72, unpacked 75 / 67; GELU of 12000 x 5120, forward 62 / 51
-// and backward 85 / 69, on 64 CUs 182 / 154 and 208 / 168; SwiGLU of 8192 x 5632 71 / 61 and 89 / 75, of 2048 x 5632 (93 and 116 MB) 19.5 / 20.3 and
-// 23.6 / 23.7, on 64 CUs 44.7 / 44.3 and 54.9 / 51.2.
-// Past the caches what they do not hold, of bf16: 16384 x 11008 SwiGLU 292 / 309 us -> 282 / 297, unpacking 2^27 elements 70 -> 67.  An fp32 lane's 32 bytes
+// Workgroups in order from 64 MB on (sweep_grid), striding / in order, us: 2^27 bf16 elements packed 76 / 73, unpacked 75 / 67; GELU of 12000 x 5120, forward 61 / 51
+// and backward 84 / 68, on 64 CUs 182 / 153 and 206 / 166; SwiGLU of 8192 x 5632 72 / 61 and 89 / 76, of 2048 x 5632 (93 and 116 MB) 19.3 / 20.0 and
+// 23.5 / 23.9, on 64 CUs 44.4 / 44.3 and 55.0 / 52.2.
+// Past the caches what they do not hold, of bf16: 16384 x 11008 SwiGLU 270 us forward and 330 backward -> 240 and 294, on 64 CUs 648 and 778 -> 635 and 754,
+// unpacking 2^27 elements 70 -> 67.  An fp32 lane's 32 bytes
 // are two instructions' halves of a line, which past the caches are written one by one: unpacking 2^26 elements 61 us, past them 91.
 template <typename T> bool past_caches(const Sweep& sw, int64_t bytes) { return sizeof(T) == 2 && sw.in_order && bytes > kPastCacheBytes; }
 

@@ -188,7 +188,7 @@ template <typename T, int VE, int LPH, bool HALVES> struct Share {
 
 // Rows of whole vectors: a wave takes a token (of few tokens, `per_chunk` of its groups of heads), its lanes 64 / LPH heads at a time.
 // Bound by memory: 32768 tokens, 32 + 8 + 8 heads of 128, bf16, RMS norm 139 us (5.8 TB/s; a wave per head and pair by pair 558), on 64 CUs 294; 12000 tokens, 20 heads
-// of 64, fp32, LayerNorm 71 (5.2).  Two tokens a wave, one after the other, 148.  Few tokens are a chain of latencies: 24 tokens 3.3 us.
+// of 64, fp32, LayerNorm 71 (5.2).  Two tokens a wave, one after the other, 148.  Few tokens are a chain of latencies: 24 tokens 3.8 us.
 template <typename T, int VE, int LPH, int NORM, bool HALVES, bool PAST>
 __global__ __launch_bounds__(kThreads) void qk_fwd_kernel(const T* x, T* y, Positions at, int H, int Hkv, int d, int heads, int per_chunk, int chunks,
                                                           float eps, float sign, const T* __restrict__ gq, const T* __restrict__ bq,
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(kThreads) void qk_fwd_kernel(const T* x, T* y, Posi
 // The backward pass of rows of whole vectors.  A workgroup takes one part (q, k or, to be copied, v) of a partition of the tokens, its waves every
 // (np kWavesBwd)-th token each, so that what the workgroups in flight touch lies side by side.
 // A lane holds its columns' sums of the part's gains' (and shifts') gradients, which are joined over the wave's heads and then over the waves, in order.
-// Bound by memory and, about as much, by vector instructions (some 25 an element): 32768 tokens, 32 + 8 + 8 heads of 128, bf16, RMS norm 233 us (4.9 TB/s), on 64
-// CUs 500, and 5 for the last reduction; 12000 tokens, 20 heads of 64, fp32, LayerNorm 92.  Workgroups of 256 threads 250, of 640 245, of 1024 241 us; q and k in one
+// Bound by memory and, about as much, by vector instructions (some 25 an element): 32768 tokens, 32 + 8 + 8 heads of 128, bf16, RMS norm 231 us (4.9 TB/s), on 64
+// CUs 500, and 5 for the last reduction; 12000 tokens, 20 heads of 64, fp32, LayerNorm 94; bf16 LayerNorm 59, 4096 tokens of 40 + 8 + 8 heads of 72 27.  Workgroups of 256 threads 250, of 640 245, of 1024 241 us; q and k in one
 // loop with sums of both 250; partitions of consecutive tokens 260.
 template <typename T, int VE, int LPH, int NORM, bool HALVES, bool PAST>
 __global__ __launch_bounds__(kThreadsBwd) void qk_bwd_kernel(const T* __restrict__ x, const T* dy, T* dx, Positions at, int H, int Hkv, int d, int parts, float eps,
@@ -642,7 +642,7 @@ mosaic_status launch_qk_norm_rope_bwd(hipStream_t s, int quota, int dtype, int n
         constexpr int VE = decltype(ve)::value, LPH = decltype(lph)::value;
         const int64_t bytes = T * (2 * heads + H + Hkv) * d * (int64_t)sizeof(E);
         const int parts = dx == dy ? 2 : 3;            // in place, v lies where it should
-        // As many tokens for every wave, and of fewer than 8192 tokens no more than 256 partitions: a wave then starts, and adds up its sums, for two tokens
+        // As many tokens for every wave, and of up to 8192 tokens no more than 256 partitions: a wave then starts, and adds up its sums, for two tokens
         // or more (512 / 256: 8192 tokens of 16 + 4 heads of 128 38.3 / 33.5 us, 4096 of 40 + 8 heads of 72 33.9 / 30.5; 12000 of 20 heads of 64 62.9 / 64.6).
         const int64_t each = ceil_div(T, (T <= 8192 ? kMaxParts / 2 : kMaxParts) * (int64_t)kWavesBwd);
         np = (int)ceil_div(T, each * kWavesBwd);
