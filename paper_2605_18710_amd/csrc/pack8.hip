@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kThreads) void unpack8_any_kernel(const int8_t* __r
 // third of the instructions of expf and a divide.  s is the approximate reciprocal after one step of Newton's, which makes it the number that the divide gives: its
 // last bits decide results that lie near a tie between two bf16 numbers, and of numbers from 8 bits, which repeat, those are many (16384 x 11008 SwiGLU formed
 // again: without the step 2.4e-5 of the results were not the nearest number, with it and in the plain form 2.4e-6).
-// 1 - s is e s (`rest`), which keeps its digits.  From -88.7 down s is 0, an infinitesimal that the reciprocal drops, so that no size of z brings it back, and
+// 1 - s is e s (`rest`), which keeps its digits.  From -88.7 down s is 0 (the reciprocal drops denormal results), so that no size of z brings it back, and
 // e stays finite for the step; a NaN reaches the results through the gate itself.
 struct Gate {
   float e, s;
