@@ -274,7 +274,7 @@ def _kept(case):
         T, E, k, n = case["T"], case["groups"], case["k"], case["n"]
         return {"y": {"fwd": lambda: empty(T, n), "dgrad": lambda: empty(T, k), "wgrad": lambda: empty(E, k, n)}[case["form"]]()}
     T, h, V = case["T"], case["h"], case["V"]
-    kept = {"loss": empty((), dtype=torch.float32), "losses": empty(T, dtype=torch.float32)}
+    kept = {"loss": empty(dtype=torch.float32), "losses": empty(T, dtype=torch.float32)}
     if op == "ce_fwd":
         size = mb.linear_ce_fwd_scratch_bytes(case["dtype"], T, h, V)
     else:
