@@ -531,6 +531,49 @@ mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t 
                                            const void* dY, void* dW, void* db, void* scratch);
 size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t T, int64_t k, int64_t n);
 
+/* Softmax cross entropy behind a linear layer, without the logits.  z_t = X[t] table^T over the V rows of table [V,h] (laid out like a TEXT_STEM's),
+ * targets: device int32 [T].  A token counts if its target lies in [0, V); the others (padding, prompts, image tokens: any other value) give no
+ * loss and no gradient, and their rows of X may hold anything.  For those that count
+ *   losses[t] = log sum_v exp(z_t[v]) - (1 - smoothing) z_t[target] - smoothing * mean_v z_t[v],      0 <= smoothing < 1,
+ * losses[t] = 0 for the others (device float [T], may be NULL), and *loss (device float) = sum of the losses / D with D = denom, or, denom = 0, the number of tokens that
+ * count (no such token: loss 0, gradients 0).  mosaic_op_linear_ce_grad also writes the gradients of *loss: dX [T,h] and dtable [V,h] (overwritten; one of
+ * them may be NULL).  Logits are fp32; bf16: the probabilities that the gradients are formed of are bf16, rounded twice relative to themselves.  What lies between is kept in
+ * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
+ * it holds the logits' exponentials for as many tokens at a time as 2^29 of them (1 GiB in bf16) belong to.  bf16: h a multiple of 8 and all tensors 16-byte aligned
+ * (MOSAIC_EUNSUPPORTED otherwise); the table is smaller than 4 GiB. */
+size_t        mosaic_op_linear_ce_fwd_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
+size_t        mosaic_op_linear_ce_grad_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
+mosaic_status mosaic_op_linear_ce_fwd(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t h, int64_t V,
+                                      float smoothing, float denom, const int32_t* targets, const void* X,
+                                      const void* table, float* loss, float* losses, void* scratch);
+mosaic_status mosaic_op_linear_ce_grad(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t h, int64_t V,
+                                       float smoothing, float denom, const int32_t* targets, const void* X,
+                                       const void* table, float* loss, float* losses, void* dX, void* dtable,
+                                       void* scratch);
+
+/* Products of rows sorted by group with their group's matrix (the MLPs of experts): offsets is a DEVICE int32 [groups + 1], non-decreasing, and rows offsets[g] ..
+ * offsets[g+1] - 1 of X, Y, dX, dY belong to group g, whose matrix is W[g] of W [groups,k,n] (up to 1024 groups, any of them without rows).
+ *   fwd    Y[r] = X[r] W[g(r)]          dgrad  dX[r] = dY[r] W[g(r)]^T          wgrad  dW[g] = X[rows of g]^T dY[rows of g], zero for a group without rows
+ * Offsets are held to 0 .. T.  Rows of no group (before offsets[0], from offsets[groups] on) are not read, and left as they were in Y and dX.  The
+ * output overlaps no input.  bf16 with k and n multiples of 8 and 16-byte aligned tensors takes the matrix-core kernel, everything else one that multiplies in fp32. */
+mosaic_status mosaic_op_grouped_linear_fwd(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups,
+                                           int64_t k, int64_t n, const int32_t* offsets, const void* X, const void* W,
+                                           void* Y);
+mosaic_status mosaic_op_grouped_linear_dgrad(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups,
+                                             int64_t k, int64_t n, const int32_t* offsets, const void* dY,
+                                             const void* W, void* dX);
+mosaic_status mosaic_op_grouped_linear_wgrad(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups,
+                                             int64_t k, int64_t n, const int32_t* offsets, const void* X,
+                                             const void* dY, void* dW);
+
+/* Dropout whose mask is never stored: y = x * keep / (1 - p) (+ R, may be NULL) over n elements, p in [0, 1]; the same call on dy, without R, is the backward
+ * pass.  An element is kept where 16 random bits are at least p * 65536 rounded, and divided by the exact probability of that; a dropped one leaves 0, whatever it was.  The
+ * bits are those of Philox4x32-10 at the counter (i / 8, rng[1] + site), low words first, under the key rng[0], for elements 8i .. 8i + 7: two of them to a word, the
+ * low half first; the same in either dtype.  rng: device uint64 [2], seed and offset, read when the call runs, so that a captured call draws anew
+ * when the program moves the offset between replays; site: which of the program's dropouts this is.  y may be x or R; it must not overlap them otherwise. */
+mosaic_status mosaic_op_dropout(void* stream, int32_t quota, int32_t dtype, int64_t n, float p, uint64_t site,
+                                const uint64_t* rng, const void* x, const void* R, void* y);
+
 /* AdamW over n elements: m = b1 m + (1-b1) g; v = b2 v + (1-b2) g^2;
  * p -= lr * ( (m / (1-b1^step)) / (sqrt(v / (1-b2^step)) + eps) + weight_decay * p ).
  * params, grads in `dtype`; m, v and master (may be NULL) fp32; master, when given, is the

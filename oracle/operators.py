@@ -1,5 +1,6 @@
 """Plain definitions, in 64 bits, of the operators around a layer's products: rotary positions with several axes, the
-norm of every query and key head with that rotation, and activations kept in 8 bits."""
+norm of every query and key head with that rotation, activations kept in 8 bits, softmax cross entropy behind a linear
+layer, products grouped by expert, and dropout."""
 import math
 
 import numpy as np
@@ -73,3 +74,59 @@ def pack8(x):
 def unpack8(q, byte):
     step = np.where(byte == 255, np.nan, 2.0 ** (byte.astype(np.float64) - 127))
     return q.astype(np.float64) * np.repeat(step, 32)[:q.size]
+
+
+def linear_ce(x, table, targets, smoothing=0.0, denom=0.0):
+    """(loss, losses [T], dx, dtable) of softmax cross entropy behind z = x table^T; a target outside the table: the token does not count."""
+    T, V = len(x), len(table)
+    counts = (targets >= 0) & (targets < V)
+    at = np.flatnonzero(counts)
+    D = denom if denom > 0 else max(1, len(at))
+    losses, dx, dtable = np.zeros(T), np.zeros(x.shape), np.zeros(table.shape)
+    rows = x[at]
+    z = rows @ table.T
+    top = z.max(1, keepdims=True) if len(at) else z[:, :1]
+    lse = top + np.log(np.exp(z - top).sum(1, keepdims=True))
+    one = np.zeros(z.shape)
+    one[np.arange(len(at)), targets[at]] = 1.0
+    q = (1.0 - smoothing) * one + smoothing / V
+    losses[at] = lse[:, 0] - (z * q).sum(1)
+    dz = (np.exp(z - lse) - q) / D
+    dx[at] = dz @ table
+    return losses.sum() / D, losses, dx, dz.T @ rows
+
+
+def grouped_linear(form, offsets, a, b, out):
+    """Rows offsets[g] .. offsets[g + 1] - 1 with matrix g; `out` [T, n], [T, k] or [groups, k, n] keeps its rows of no group."""
+    out = out.copy()
+    for g in range(len(offsets) - 1):
+        r = slice(offsets[g], offsets[g + 1])
+        if form == "fwd":
+            out[r] = a[r] @ b[g]
+        elif form == "dgrad":
+            out[r] = a[r] @ b[g].T
+        else:
+            out[g] = a[r].T @ b[r]
+    return out
+
+
+def philox4x32(counter, key):
+    """Ten rounds of Philox4x32 (Salmon, Moraes, Dror and Shaw, 2011) on Python's whole numbers."""
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        a, b = c[0] * 0xD2511F53, c[2] * 0xCD9E8D57
+        c = [(b >> 32) ^ c[1] ^ k[0], b & 0xFFFFFFFF, (a >> 32) ^ c[3] ^ k[1], a & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def dropout_keeps(elements, p, site, seed, offset):
+    """Whether each of the elements (whole numbers) is kept."""
+    drop, turn = int(np.rint(np.float32(p) * np.float32(65536))), (offset + site) % (1 << 64)
+    out, words = [], {}
+    for i in elements:
+        b = int(i) // 8
+        if b not in words:
+            words[b] = philox4x32((b & 0xFFFFFFFF, b >> 32, turn & 0xFFFFFFFF, turn >> 32), (seed & 0xFFFFFFFF, (seed >> 32) & 0xFFFFFFFF))
+        out.append((words[b][int(i) % 8 // 2] >> (16 * (int(i) % 2))) & 0xFFFF >= drop)
+    return np.array(out, dtype=bool), 1.0 / (1.0 - drop / 65536) if drop < 65536 else 0.0

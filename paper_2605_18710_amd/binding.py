@@ -149,6 +149,14 @@ SIGNATURES = {
     "mosaic_op_act_bwd_pack8": (_i32, [_vp, _i32, _i32, _i32, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
     "mosaic_op_linear_wgrad_pack8": (_i32, [_vp, _i32, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp]),
     "mosaic_op_linear_wgrad_pack8_scratch_bytes": (_sz, [_i32, _i64, _i64, _i64]),
+    "mosaic_op_linear_ce_fwd_scratch_bytes": (_sz, [_i32, _i64, _i64, _i64]),
+    "mosaic_op_linear_ce_grad_scratch_bytes": (_sz, [_i32, _i64, _i64, _i64]),
+    "mosaic_op_linear_ce_fwd": (_i32, [_vp, _i32, _i32, _i64, _i64, _i64, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mosaic_op_linear_ce_grad": (_i32, [_vp, _i32, _i32, _i64, _i64, _i64, _f32, _f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "mosaic_op_grouped_linear_fwd": (_i32, [_vp, _i32, _i32, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "mosaic_op_grouped_linear_dgrad": (_i32, [_vp, _i32, _i32, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "mosaic_op_grouped_linear_wgrad": (_i32, [_vp, _i32, _i32, _i64, _i32, _i64, _i64, _vp, _vp, _vp, _vp]),
+    "mosaic_op_dropout": (_i32, [_vp, _i32, _i32, _i64, _f32, C.c_uint64, _vp, _vp, _vp, _vp]),
     "mosaic_op_adamw": (_i32, [_vp, _i32, _i32, _i64, _vp, _vp, _vp, _vp, _vp, _f32, _f32, _f32, _f32, _f32, _i64]),
     "mosaic_op_swiglu_fwd": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp]),
     "mosaic_op_swiglu_bwd": (_i32, [_vp, _i32, _i32, _i64, _i64, _vp, _vp, _vp]),
@@ -633,6 +641,44 @@ def op_linear_wgrad_pack8(stream, quota, dtype, T, k, n, Xq, Xscale, dY, dW, db,
 
 def linear_wgrad_pack8_scratch_bytes(dtype: str, T: int, k: int, n: int) -> int:
     return int(lib().mosaic_op_linear_wgrad_pack8_scratch_bytes(_dt(dtype), T, k, n))
+
+
+def linear_ce_fwd_scratch_bytes(dtype: str, T: int, h: int, V: int) -> int:
+    return int(lib().mosaic_op_linear_ce_fwd_scratch_bytes(_dt(dtype), T, h, V))
+
+
+def linear_ce_grad_scratch_bytes(dtype: str, T: int, h: int, V: int) -> int:
+    return int(lib().mosaic_op_linear_ce_grad_scratch_bytes(_dt(dtype), T, h, V))
+
+
+def op_linear_ce_fwd(stream, quota, dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, scratch):
+    """targets: int32 [T]; denom 0: the mean over the tokens that count; losses may be None."""
+    check(lib().mosaic_op_linear_ce_fwd(stream, quota, _dt(dtype), T, h, V, smoothing, denom, _ptr(targets), _ptr(X), _ptr(table), _ptr(loss), _ptr(losses),
+                                        _ptr(scratch)))
+
+
+def op_linear_ce_grad(stream, quota, dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, dX, dtable, scratch):
+    """dX or dtable may be None."""
+    check(lib().mosaic_op_linear_ce_grad(stream, quota, _dt(dtype), T, h, V, smoothing, denom, _ptr(targets), _ptr(X), _ptr(table), _ptr(loss), _ptr(losses),
+                                         _ptr(dX), _ptr(dtable), _ptr(scratch)))
+
+
+def op_grouped_linear_fwd(stream, quota, dtype, T, groups, k, n, offsets, X, W, Y):
+    """offsets: int32 [groups + 1] on the device."""
+    check(lib().mosaic_op_grouped_linear_fwd(stream, quota, _dt(dtype), T, groups, k, n, _ptr(offsets), _ptr(X), _ptr(W), _ptr(Y)))
+
+
+def op_grouped_linear_dgrad(stream, quota, dtype, T, groups, k, n, offsets, dY, W, dX):
+    check(lib().mosaic_op_grouped_linear_dgrad(stream, quota, _dt(dtype), T, groups, k, n, _ptr(offsets), _ptr(dY), _ptr(W), _ptr(dX)))
+
+
+def op_grouped_linear_wgrad(stream, quota, dtype, T, groups, k, n, offsets, X, dY, dW):
+    check(lib().mosaic_op_grouped_linear_wgrad(stream, quota, _dt(dtype), T, groups, k, n, _ptr(offsets), _ptr(X), _ptr(dY), _ptr(dW)))
+
+
+def op_dropout(stream, quota, dtype, n, p, site, rng, x, R, y):
+    """rng: int64 or uint64 [2] on the device, seed and offset; R may be None."""
+    check(lib().mosaic_op_dropout(stream, quota, _dt(dtype), n, p, site, _ptr(rng), _ptr(x), _ptr(R), _ptr(y)))
 
 
 def op_adamw(stream, quota, dtype, n, params, grads, m, v, master, lr, beta1, beta2, eps, weight_decay, step):

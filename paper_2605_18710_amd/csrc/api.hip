@@ -1,5 +1,6 @@
 // C-ABI wrappers of the single operations, and the dispatch between the MFMA attention
 // kernels for bf16 and the fp32 ones.
+#include <math.h>
 #include <mutex>
 #include "kernels.h"
 
@@ -442,6 +443,107 @@ mosaic_status mosaic_op_linear_wgrad_pack8(void* stream, int32_t quota, int32_t 
   }
   MOSAIC_TRY(check_common(quota, dtype));
   return launch_linear_wgrad_pack8((hipStream_t)stream, quota, dtype, T, k, n, Xq, Xscale, dY, dW, db, scratch);
+}
+
+// the calls with a loss over a vocabulary: `dX`, `dtable` and `scratch` as given (null: none)
+static mosaic_status check_ce(int32_t dtype, int64_t T, int64_t h, int64_t V, float smoothing, float denom, const void* targets, const void* X, const void* table,
+                              const void* loss, const void* losses, bool grad, const void* dX, const void* dtable, const void* scratch) {
+  NONNULL(table); NONNULL(loss); NONNULL(scratch);
+  if (T != 0) { NONNULL(targets); NONNULL(X); }          // an empty tensor has no address
+  if (grad && T != 0 && !dX && !dtable) MOSAIC_FAIL(MOSAIC_EINVAL, "null pointers: neither dX nor dtable is asked for");
+  if (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) MOSAIC_FAIL(MOSAIC_EINVAL, "bad dtype %d", dtype);
+  if (T < 0 || h <= 0 || V <= 0) MOSAIC_FAIL(MOSAIC_EINVAL, "bad sizes T=%lld h=%lld V=%lld", (long long)T, (long long)h, (long long)V);
+  if (!(smoothing >= 0.f) || !(smoothing < 1.f)) MOSAIC_FAIL(MOSAIC_EINVAL, "label smoothing must lie in [0, 1)");
+  if (!(denom >= 0.f) || denom > 3.4028234e38f) MOSAIC_FAIL(MOSAIC_EINVAL, "the denominator must be positive and finite, or 0 for the mean");
+  const int64_t es = (int64_t)dtype_size(dtype);
+  if (T > INT32_MAX / 2 || h > (1 << 20) || V > (1 << 22) || V > ((int64_t)1 << 32) / es / h - 1)
+    MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "T=%lld h=%lld V=%lld: tables of 4 GiB or more, or sizes past 2^30 tokens, 2^20 values a row or 2^22 rows", (long long)T, (long long)h, (long long)V);
+  if (dtype == MOSAIC_BF16 && h % 8) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "rows of %lld bf16 elements, not a multiple of 8", (long long)h);
+  if (dtype == MOSAIC_BF16 && (((uintptr_t)X | (uintptr_t)table | (uintptr_t)dX | (uintptr_t)dtable) & 15)) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "bf16 tensors off 16-byte boundaries");
+  if ((uintptr_t)scratch % 256) MOSAIC_FAIL(MOSAIC_EINVAL, "scratch must be 256-byte aligned");
+  struct Span { const char* name; const void* p; int64_t n; };
+  const int64_t rows = T * h * es, words = V * h * es;
+  const Span in[] = {{"targets", targets, 4 * T}, {"X", X, rows}, {"table", table, words}};
+  const Span out[] = {{"loss", loss, 4}, {"losses", losses, 4 * T}, {"dX", dX, rows}, {"dtable", dtable, words}, {"scratch", scratch, (int64_t)linear_ce_scratch_bytes(dtype, T, h, V, grad)}};
+  for (int o = 0; o < 5; ++o) {
+    for (const Span& i : in) if (overlap(out[o].p, out[o].n, i.p, i.n)) MOSAIC_FAIL(MOSAIC_EINVAL, "%s overlaps %s", out[o].name, i.name);
+    for (int q = 0; q < o; ++q) if (overlap(out[o].p, out[o].n, out[q].p, out[q].n)) MOSAIC_FAIL(MOSAIC_EINVAL, "%s overlaps %s", out[o].name, out[q].name);
+  }
+  return MOSAIC_OK;
+}
+
+static size_t ce_scratch(int32_t dtype, int64_t T, int64_t h, int64_t V, bool grad) {
+  if ((dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) || T < 0 || h <= 0 || V <= 0 || T > INT32_MAX / 2 || h > (1 << 20) || V > (1 << 22)) return 0;
+  return linear_ce_scratch_bytes(dtype, T, h, V, grad);
+}
+size_t mosaic_op_linear_ce_fwd_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V) { return ce_scratch(dtype, T, h, V, false); }
+size_t mosaic_op_linear_ce_grad_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V) { return ce_scratch(dtype, T, h, V, true); }
+
+mosaic_status mosaic_op_linear_ce_fwd(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t h, int64_t V, float smoothing, float denom,
+                                      const int32_t* targets, const void* X, const void* table, float* loss, float* losses, void* scratch) {
+  MOSAIC_TRY(check_ce(dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, false, nullptr, nullptr, scratch));
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_linear_ce((hipStream_t)stream, quota, dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, false, nullptr, nullptr, scratch);
+}
+
+mosaic_status mosaic_op_linear_ce_grad(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t h, int64_t V, float smoothing, float denom,
+                                       const int32_t* targets, const void* X, const void* table, float* loss, float* losses, void* dX, void* dtable,
+                                       void* scratch) {
+  MOSAIC_TRY(check_ce(dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, true, dX, dtable, scratch));
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_linear_ce((hipStream_t)stream, quota, dtype, T, h, V, smoothing, denom, targets, X, table, loss, losses, true, dX, dtable, scratch);
+}
+
+static mosaic_status grouped(void* stream, int32_t quota, int32_t dtype, GroupedForm form, int64_t T, int32_t groups, int64_t k, int64_t n,
+                             const int32_t* offsets, const void* A, const void* B, void* C) {
+  if (dtype != MOSAIC_F32 && dtype != MOSAIC_BF16) MOSAIC_FAIL(MOSAIC_EINVAL, "bad dtype %d", dtype);
+  if (T < 0 || groups < 0 || k <= 0 || n <= 0) MOSAIC_FAIL(MOSAIC_EINVAL, "bad sizes T=%lld groups=%d k=%lld n=%lld", (long long)T, groups, (long long)k, (long long)n);
+  if (groups > 1024) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "%d groups; up to 1024", groups);
+  if (T > INT32_MAX / 2 || k > (1 << 28) || n > (1 << 28) || k * n > (int64_t)1 << 40) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "sizes T=%lld k=%lld n=%lld", (long long)T, (long long)k, (long long)n);
+  const int64_t es = (int64_t)dtype_size(dtype), x = T * k * es, y = T * n * es, w = groups * k * n * es;
+  const int64_t a = form == GROUPED_DGRAD ? y : x, b = form == GROUPED_WGRAD ? y : w, c = form == GROUPED_FWD ? y : form == GROUPED_DGRAD ? x : w;
+  if (overlap(C, c, A, a) || overlap(C, c, B, b) || overlap(C, c, offsets, 4 * ((int64_t)groups + 1))) MOSAIC_FAIL(MOSAIC_EINVAL, "the output overlaps an input");
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_grouped((hipStream_t)stream, quota, dtype, form, T, groups, k, n, offsets, A, B, C);
+}
+
+mosaic_status mosaic_op_grouped_linear_fwd(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups, int64_t k, int64_t n, const int32_t* offsets,
+                                           const void* X, const void* W, void* Y) {
+  NONNULL(offsets);
+  if (T != 0) { NONNULL(X); NONNULL(Y); }
+  if (groups != 0) NONNULL(W);
+  return grouped(stream, quota, dtype, GROUPED_FWD, T, groups, k, n, offsets, X, W, Y);
+}
+
+mosaic_status mosaic_op_grouped_linear_dgrad(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups, int64_t k, int64_t n, const int32_t* offsets,
+                                             const void* dY, const void* W, void* dX) {
+  NONNULL(offsets);
+  if (T != 0) { NONNULL(dY); NONNULL(dX); }
+  if (groups != 0) NONNULL(W);
+  return grouped(stream, quota, dtype, GROUPED_DGRAD, T, groups, k, n, offsets, dY, W, dX);
+}
+
+mosaic_status mosaic_op_grouped_linear_wgrad(void* stream, int32_t quota, int32_t dtype, int64_t T, int32_t groups, int64_t k, int64_t n, const int32_t* offsets,
+                                             const void* X, const void* dY, void* dW) {
+  NONNULL(offsets);
+  if (T != 0) { NONNULL(X); NONNULL(dY); }
+  if (groups != 0) NONNULL(dW);
+  return grouped(stream, quota, dtype, GROUPED_WGRAD, T, groups, k, n, offsets, X, dY, dW);
+}
+
+mosaic_status mosaic_op_dropout(void* stream, int32_t quota, int32_t dtype, int64_t n, float p, uint64_t site, const uint64_t* rng, const void* x,
+                                const void* R, void* y) {
+  NONNULL(rng);
+  if (n != 0) { NONNULL(x); NONNULL(y); }
+  if (!(p >= 0.f) || !(p <= 1.f)) MOSAIC_FAIL(MOSAIC_EINVAL, "the probability of dropping must lie in [0, 1]");
+  if ((uintptr_t)rng % 8) MOSAIC_FAIL(MOSAIC_EINVAL, "rng must be 8-byte aligned");
+  MOSAIC_TRY(check_packed(dtype, n, 1));
+  const int64_t bytes = n * (int64_t)dtype_size(dtype);
+  if (x != y) APART(x, bytes, y, bytes);
+  if (R != y) APART(R, bytes, y, bytes);
+  APART(rng, 16, y, bytes);
+  MOSAIC_TRY(check_common(quota, dtype));
+  return launch_dropout((hipStream_t)stream, quota, dtype, n, (uint32_t)lrintf(p * 65536.f), site, rng, x, R, y);
 }
 
 size_t mosaic_op_mse_scratch_bytes(void) { return mse_scratch_bytes(); }

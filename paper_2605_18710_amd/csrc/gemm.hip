@@ -43,29 +43,14 @@
 #include <type_traits>
 #include "activations.h"
 #include "gemm_plan.h"
+#include "gemm_w4.h"
 #include "kernels.h"
 #include "tile_queue.h"
 
 namespace {
 
-#pragma clang diagnostic ignored "-Winline-asm"   // m0 is named as a clobber on purpose
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 
 constexpr int BK = 32;            // k-values per K-tile (64 bytes of a K-contiguous row); 64 where stated (BKT)
-constexpr unsigned kOob = 0xFFFFFFF0u;   // byte offset beyond any descriptor's range
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t make_rsrc(const void* p, uint32_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00020000);
-}
-
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(4))) int i32x4;
 constexpr int NS = 5;             // LDS stages
 constexpr int AHEAD = 4;          // K-tiles between the load cursor and the compute cursor
 
@@ -214,25 +199,6 @@ struct FragReader {
   }
 };
 
-// Position `tile` of the tile list -> (tile row, tile column).  The list is panel-major: panels
-// of 8 tile columns, row-major inside a panel, so 32 consecutive entries form a 4 x 8 patch that
-// shares operand panels in one XCD's L2.  Above that, tile rows are taken in super-blocks of
-// `row_block` rows (all panels of a super-block before the next super-block), sized on the
-// host so that the row operand of a super-block (row_block x 256 rows x K) stays in the
-// last-level cache: it is then re-read from there, not from HBM, once per panel (measured on
-// the 7B-shaped products: +3 % forward, +4 % input gradient; the board is power-bound and HBM
-// reads cost energy).  Both kernels and both launches of a mixed plan use this one order.
-__device__ __forceinline__ void tile_coords(int tile, int tiles_m, int tiles_n, int row_block, int* row, int* col) {
-  const int per_sb = row_block * tiles_n;
-  const int sb = tile / per_sb, rem = tile - sb * per_sb;
-  const int rows_sb = min(row_block, tiles_m - sb * row_block);
-  const int panel = rem / (rows_sb * 8);
-  const int pw = min(8, tiles_n - panel * 8);
-  const int in_panel = rem - panel * rows_sb * 8;
-  *row = sb * row_block + in_panel / pw;
-  *col = panel * 8 + in_panel % pw;
-}
-
 // One unit of work: an output tile, or (PIECES_APART) one K-piece of an output tile.
 struct WorkItem {
   int m0, n0, kt0, kt_end, split, tl;      // tl: position of the item's coarse tile in this launch's range
@@ -266,24 +232,6 @@ struct ActArgs {
   uint32_t r_rows = 0, r_magic = 0;   // r_rows > 0: R has that many rows, and row r of C gets row r mod r_rows (a position table)
   // ACT_TAPS: GELU, and C2 is the gathered input [M / 2, 3N] of a three-tap convolution of stride 2 over samples of 2 * r_rows rows
 };
-// Where row r of the activation goes in that input (24000 x 1280 from 240 k-values: product 59 us and gather 35 -> 82): tap 1 of output r / 2 (even rows), or tap 2 of it and tap 0 of the next one; the last row
-// of a sample, which has no next one, clears tap 0 of the sample's first output.  Element offsets of its first column, -1: none.
-struct TapRows { int64_t first, second; bool zero; };
-// r mod r_rows with r_magic = 2^32 / r_rows + 1: exact as long as r * r_rows < 2^32 (checked by the launcher)
-__device__ __forceinline__ int table_row(int r, uint32_t r_rows, uint32_t r_magic) { return r - (int)(__umulhi((uint32_t)r, r_magic) * r_rows); }
-__device__ __forceinline__ TapRows tap_rows(int r, int M, int64_t n, uint32_t lo, uint32_t magic) {
-  const int t = r >> 1;
-  TapRows o = {-1, -1, false};
-  if (r < M) {
-    o.first = (3 * (int64_t)t + 1 + (r & 1)) * n;
-    if (r & 1) {
-      o.zero = table_row(t + 1, lo, magic) == 0;
-      o.second = 3 * (int64_t)(o.zero ? t + 1 - (int)lo : t + 1) * n;
-    }
-  }
-  return o;
-}
-
 // PIECES_CHAINED: one workgroup takes the pieces of its tile one after the other and adds them in registers,
 // in the order and with the additions of the second kernel: the same bits as PIECES_APART, no scratch.
 constexpr int PIECES_NONE = 0, PIECES_APART = 1, PIECES_CHAINED = 2;
@@ -981,384 +929,6 @@ __global__ __launch_bounds__(256, 2) void gemm_bf16_pair_kernel(PairHalf dg, Pai
                                                                       wg.ktiles_per, nullptr, wg.tq, wg.aa);
 }
 
-// ------------------------------------------------------------------ four-wave kernel
-// 256x256x64 tiles, four waves of 128x128, v_mfma_f32_16x16x32_bf16, for every form whose
-// K-contiguous operands have a contraction of whole K-tiles (K a multiple of 64).  Where the row operand is
-// K-contiguous the tile may be 32 * MI rows high, MI = 8, 7, 6 or 5 (launch_mfma_shape says when).
-//
-// What bounds it: on the whole chip the board's power.  Registers only, random data, the
-// 16x16x32 instruction delivers 1830 TFLOP/s and the 32x32x16 one 1760 (it reads and writes twice
-// the accumulator bytes per flop); around it the kernel spends as little as it can: a wave tile of
-// 128x128 reads 1 LDS byte per 64 flops (two thirds of what 128x64 wave tiles read), a K-tile of 64
-// brings whole 128-byte lines, operands go HBM -> LDS without passing registers, 128 matrix instructions
-// come with about 135 others per K-tile.
-//   LDS: two stages of 64 KB.  The fragments of a K-tile's second half are read under its first 16
-//     matrix instructions; after a barrier (slot 24 of 128) the stage is free and the K-tile after the
-//     next is requested into it, one request per six matrix instructions: requests made faster than
-//     the CU's vector cache takes them (16 cycles each, four waves) hold up the wave that makes
-//     them.  The next K-tile has to be there, behind a second barrier, at slot 88, when its first
-//     fragments are read.  Measured on 32768 x 4096 x 22016 input gradient / 12000 x 5120 x 1280
-//     forward: a request per two slots, one barrier in the middle 4697 / 118 us; per four 4734 / 112;
-//     two barriers and one per six 3960 / 112; without any requests the K loop takes 20 % less than
-//     the first of these.
-//   The stream of K-tiles runs on across output tiles; the epilogue passes through 4 KB per
-//     wave behind the stages, so the next tile's first K-tiles land under it.
-//   K-contiguous operand: rows of 128 bytes, 16-byte chunks XOR-swizzled by (row/2)%8, a fragment is
-//     one ds_read_b128.  K-strided operand: k-rows of 512 bytes as in HBM, 32-byte chunks XOR-swizzled
-//     by 2*(k%4) + (k/8)%2, a fragment is two ds_read_b64_tr_b16.  Both touch every bank once.
-//   Requests take a constant offset per lane; the K-tile moves the descriptor (base and remaining
-//     bytes: scalar instructions), which also bounds it: rows past the end read zeros, columns past
-//     the end read the next row's values and only reach outputs that are not stored.
-//   The matrix instruction is written in assembly to tie the result to its accumulator: left to
-//     itself the compiler copied 400 accumulator registers per K-tile.
-// Each output element is accumulated in ascending k: same bits as gemm_bf16_kernel's.
-// Measured, whole device, eight-wave kernel (input gradient: a four-wave kernel that staged through
-// registers) -> this: forward 32768 x 4096 x 12288 2525 -> 2300 us (1434 TFLOP/s), 8192 x 5632 x 2048
-// 149 -> 129; with GELU 12000 x 1280 x 5120 199 -> 151, with SwiGLU 8192 x 2048 x 11264 365 -> 338;
-// input gradient 32768 x 4096 x 22016 4433 -> 3960 (1492 TFLOP/s), 9216 x 4096 x 1024 77 -> 70;
-// weight gradient 4096 x 32768 x 22016 4268 -> 4000, 2048 x 8192 x 11264 339 -> 331.
-struct W4Args {
-  const bf16 *A, *B, *bias, *R;
-  bf16 *C, *C2;
-  int M, N, K;
-  int64_t lda, ldb, ldc, ldc2;
-  uint32_t a_bytes, b_bytes, c_bytes, c2_bytes;
-  int tiles_m, tiles_n, tile_begin, tile_count, row_block, gu_f;
-  uint32_t r_rows, r_magic;        // W4_TABLE, W4_TAPS: see ActArgs
-};
-enum { W4_PLAIN, W4_BIAS, W4_RES, W4_GELU, W4_SWIGLU, W4_TABLE, W4_TAPS };
-constexpr int kW4Stage = 2 * 256 * 64 * 2;                         // both operands of a K-tile
-constexpr int kW4Pitch = 68;                                       // floats per row of the epilogue's patch: 16 rows of 64
-constexpr int kW4Patch = 4 * 16 * kW4Pitch * 4;
-constexpr int w4_lds(int epi) { return 2 * kW4Stage + kW4Patch + (epi == W4_GELU || epi == W4_TAPS ? ErfTable::kEntries * 4 : 0); }
-
-// One operand: what a lane requests of a K-tile, and where its fragments are.
-template <bool KC, bool GU, int NF = 8>
-struct W4Operand {
-  unsigned voff[NF];                       // byte offset of request j from the K-tile's first byte
-  int frag[KC ? 2 : 8];                    // LDS offsets: KC: of k-half 0 / 1, + 2048 per 16 rows; else of 16 columns each, + 16384 per k-half
-  __device__ __forceinline__ void init(int wave, int w0, int64_t ld, int gu_f) {
-    const int lane = threadIdx.x & 63, lr = lane & 15, g = lane >> 4;
-#pragma unroll
-    for (int j = 0; j < NF; ++j) {
-      if constexpr (KC) {
-        const int r = 8 * NF * wave + 8 * j + (lane >> 3), ch = (lane & 7) ^ ((r >> 1) & 7);
-        voff[j] = (unsigned)((int64_t)r * ld * 2 + ch * 16);
-      } else {
-        const int kr = 16 * wave + 2 * j + (lane >> 5), pos = lane & 31;
-        const int c32 = (pos >> 1) ^ (((kr & 3) << 1) | ((kr >> 3) & 1));
-        // GU: 16-column group c32 of the tile belongs to the gate half (even) or the up half (odd)
-        const int64_t byte = GU ? (c32 >> 1) * 32 + (int64_t)(c32 & 1) * gu_f * 2 : c32 * 32;
-        voff[j] = (unsigned)((int64_t)kr * ld * 2 + byte + (pos & 1) * 16);
-      }
-    }
-    if constexpr (KC) {
-      const int sw = (lr >> 1) & 7;
-      frag[0] = (w0 + lr) * 128 + ((g ^ sw) << 4);
-      frag[1] = (w0 + lr) * 128 + (((4 + g) ^ sw) << 4);
-    } else {
-      const int q = lr >> 2, f = (q << 1) | (g & 1);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) frag[i] = (8 * g + q) * 512 + (((w0 >> 4) + (i ^ f)) << 5) + 8 * (lr & 3);
-    }
-  }
-  __device__ __forceinline__ u32x4 read(const lds_byte* area, int i, int half) const {
-    if constexpr (KC) {
-      return *reinterpret_cast<const __attribute__((address_space(3))) u32x4*>(area + frag[half] + 2048 * i);
-    } else {
-      const lds_byte* p = area + frag[i] + 16384 * half;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 2048));
-      typedef __attribute__((ext_vector_type(8))) short s16x8;
-      return __builtin_bit_cast(u32x4, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-    }
-  }
-};
-
-// Where an operand's next K-tile starts and how many bytes of the tensor lie behind that point.
-struct W4Cursor {
-  uint64_t at;
-  uint32_t left;
-  __device__ __forceinline__ void set(const void* base, uint64_t off, uint32_t bytes) {
-    at = (uint64_t)(uintptr_t)base + off;
-    left = off < bytes ? (uint32_t)(bytes - off) : 0u;
-  }
-  __device__ __forceinline__ void advance(uint32_t step) { at += step; left = left > step ? left - step : 0u; }
-  __device__ __forceinline__ i32x4 desc(bool live) const {
-    i32x4 d;
-    d.x = __builtin_amdgcn_readfirstlane((int)(uint32_t)at); d.y = __builtin_amdgcn_readfirstlane((int)((uint32_t)(at >> 32) & 0xffffu));
-    d.z = __builtin_amdgcn_readfirstlane((int)(live ? left : 0u)); d.w = 0x00020000;
-    return d;
-  }
-};
-
-template <bool A_KC, bool B_KC, int EPI, int MI>
-__global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueueArgs tq) {
-  typedef __attribute__((ext_vector_type(4))) float f32x4;
-  constexpr int OPB = kW4Stage / 2;
-  static_assert(MI == 8 || A_KC, "a K-strided row operand fills whole requests with 256 rows only");
-  extern __shared__ __align__(16) unsigned char smem[];
-  lds_byte* const lds = (lds_byte*)smem;
-  const unsigned lds0 = (unsigned)(uintptr_t)lds;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int wm = (wave >> 1) * (16 * MI), wn = (wave & 1) * 128;
-  const int nk = (p.K + 63) / 64;              // at least two, the depth of the request stream
-  const uint32_t astep = A_KC ? 128u : (uint32_t)(64 * p.lda * 2), bstep = B_KC ? 128u : (uint32_t)(64 * p.ldb * 2);
-  W4Operand<A_KC, false, MI> oa;
-  W4Operand<B_KC, EPI == W4_SWIGLU> ob;
-  oa.init(wave, wm, p.lda, 0);
-  ob.init(wave, wn, p.ldb, p.gu_f);
-
-  struct Item { int m0, n0; };
-  auto decode = [&](int item) -> Item {
-    int trow, tcol;
-    tile_coords(p.tile_begin + item, p.tiles_m, p.tiles_n, p.row_block, &trow, &tcol);
-    return {trow * (32 * MI), tcol * 256};
-  };
-  W4Cursor ca, cb;
-  auto point = [&](const Item& it) {
-    ca.set(p.A, A_KC ? (uint64_t)it.m0 * p.lda * 2 : (uint64_t)it.m0 * 2, p.a_bytes);
-    cb.set(p.B, B_KC ? (uint64_t)it.n0 * p.ldb * 2 : (uint64_t)(EPI == W4_SWIGLU ? it.n0 : it.n0 * 2), p.b_bytes);
-  };
-  const unsigned wdst = lds0 + (unsigned)wave * 8192, adst = lds0 + (unsigned)wave * (MI * 1024);
-  auto request = [&](const i32x4& d, unsigned off, unsigned dst) {
-    // m0 = LDS address of lane 0's 16 bytes; lane l lands at m0 + 16*l.  Completion is waited for by hand.
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(dst), "v"(off), "s"(d) : "m0");
-  };
-  auto request_tile = [&](int st) {
-    i32x4 da = ca.desc(true), db = cb.desc(true);
-    // A memory instruction may read a scalar register that the vector unit wrote (v_readfirstlane) five wait
-    // states later at the earliest, and the compiler does not see the requests: both descriptors
-    // pass through these five, so that no part of them is formed later.
-    asm volatile("s_nop 4" : "+s"(da), "+s"(db));
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int j = 0; j < MI; ++j) request(da, oa.voff[j], adst + (unsigned)(st * kW4Stage + j * 1024));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) request(db, ob.voff[j], wdst + (unsigned)(st * kW4Stage + OPB + j * 1024));
-    ca.advance(astep);
-    cb.advance(bstep);
-  };
-
-  __shared__ int mail;
-  TileQueueCursor qc;
-  int item = tq_first(tq, qc, &mail);
-  if (item < 0) { tq_done(tq); return; }
-  Item it = decode(item);
-  point(it);
-  request_tile(0);
-  request_tile(1);
-  // 256 values of a tile to a thread: seven erff to fill the table instead of 256 (the epilogue of 12000 x 1280 x 5120
-  // takes 10 us of 150; with erff in it, four waves a CU, 83 of 239)
-  float* const erf_table = reinterpret_cast<float*>(smem + 2 * kW4Stage + kW4Patch);
-  if constexpr (EPI == W4_GELU || EPI == W4_TAPS) {
-    ErfTable::fill(erf_table, threadIdx.x, 256);
-    __syncthreads();
-  }
-  f32x4 acc[MI][8];
-#pragma unroll
-  for (int i = 0; i < MI; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 ax[MI], bx[8], ay[MI], by[8];          // fragments of the first and of the second half
-  __builtin_amdgcn_s_waitcnt(((MI + 8) & 15) | (7 << 4) | (15 << 8) | (((MI + 8) >> 4) << 14));      // vmcnt: the first K-tile has landed
-  __builtin_amdgcn_s_barrier();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (i < MI) ax[i] = oa.read(lds, i, 0);
-    bx[i] = ob.read(lds + OPB, i, 0);
-  }
-  int st = 0;
-  bool live = true;
-  auto mfma = [](f32x4& c, const u32x4& b, const u32x4& a) {
-    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(b), "v"(a));
-  };
-  // The compiler knows nothing of the latency of an assembly instruction: this stands between the
-  // matrix instructions and other reads or writes of their registers (more than the 19 wait
-  // states that the longest of those dependencies wants).
-  auto settle = [] { asm volatile("s_nop 15\n\ts_nop 15"); __builtin_amdgcn_sched_barrier(0); };
-  // One K-tile: 128 slots of one matrix instruction, the rest placed between them (see above).
-  constexpr int NR = MI + 8;                  // requests of a K-tile, fragments of half of it
-  constexpr int kFree = NR + 8, kLanded = 16 * MI - 2 * NR - 8, kRequest = kFree + 1, kEvery = MI == 8 ? 6 : MI - 1;
-  constexpr int kBefore = (kLanded - kRequest + kEvery - 1) / kEvery;        // requests made before kLanded
-  static_assert(kFree <= 8 * MI && kLanded >= 8 * MI && kRequest + (NR - 1) * kEvery < 16 * MI, "slots of a K-tile");
-  auto step = [&]() {
-    const lds_byte* const here = lds + st * kW4Stage;
-    const lds_byte* const there = lds + (st ^ 1) * kW4Stage;
-    // formed here, ahead of the scheduling barrier, and first read kRequest matrix instructions on: far beyond the
-    // five wait states that request_tile waits out
-    const i32x4 da = ca.desc(live), db = cb.desc(live);
-    const unsigned dst = wdst + (unsigned)(st * kW4Stage), dsta = adst + (unsigned)(st * kW4Stage);
-    __builtin_amdgcn_sched_barrier(0);
-    auto half = [&](auto first) {
-      constexpr int t0 = decltype(first)::value;
-#pragma unroll
-      for (int q = 0; q < 8 * MI; ++q) {
-        const int t = t0 + q, i = q % MI, j = q / MI;
-        if constexpr (t0 == 0) mfma(acc[i][j], bx[j], ax[i]);
-        else mfma(acc[i][j], by[j], ay[i]);
-        if (t < MI) ay[t] = oa.read(here, t, 1);
-        else if (t < NR) by[t - MI] = ob.read(here + OPB, t - MI, 1);
-        if (t == kFree) {
-          __builtin_amdgcn_s_waitcnt(15 | (7 << 4) | (0 << 8) | (3 << 14));                                       // lgkmcnt(0)
-          __builtin_amdgcn_s_barrier();
-        }
-        if (t == kLanded) {
-          __builtin_amdgcn_s_waitcnt((kBefore & 15) | (7 << 4) | (15 << 8) | ((kBefore >> 4) << 14));             // vmcnt(kBefore)
-          __builtin_amdgcn_s_barrier();
-        }
-        if (t >= kRequest && (t - kRequest) % kEvery == 0 && (t - kRequest) / kEvery < NR) {
-          const int r = (t - kRequest) / kEvery;
-          if (r < MI) request(da, oa.voff[r], dsta + (unsigned)(r * 1024));
-          else request(db, ob.voff[r - MI], dst + (unsigned)(OPB + (r - MI) * 1024));
-        }
-        if (t >= kLanded && (t - kLanded) % 2 == 0 && t < kLanded + 2 * NR) {
-          const int r = (t - kLanded) / 2;
-          if (r < MI) ax[r] = oa.read(there, r, 0);
-          else bx[r - MI] = ob.read(there + OPB, r - MI, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    };
-    half(std::integral_constant<int, 0>{});
-    half(std::integral_constant<int, 8 * MI>{});
-    ca.advance(astep);
-    cb.advance(bstep);
-    st ^= 1;
-  };
-  const __amdgpu_buffer_rsrc_t rc = make_rsrc(p.C, p.c_bytes), rc2 = make_rsrc(p.C2, p.C2 ? p.c2_bytes : 0u);
-  const __amdgpu_buffer_rsrc_t rr = make_rsrc(p.R, !p.R ? 0u : EPI == W4_TABLE ? (uint32_t)(p.r_rows * p.ldc * 2) : p.c_bytes), rbias = make_rsrc(p.bias, p.bias ? (uint32_t)p.N * 2u : 0u);
-  while (true) {
-    settle();
-    for (int n = nk - 2; n > 0; --n) step();
-    // the last K-tile of this item has been requested: the requests move on to the next item
-    const unsigned entry = tq_claim_ahead(tq, qc);
-    const int next = tq_next(tq, qc, entry, &mail);
-    live = next >= 0;
-    const Item nit = decode(live ? next : item);
-    point(nit);
-    for (int n = 2; n > 0; --n) step();
-    settle();
-    // Epilogue, 16 rows x 64 columns at a time through the patch, leaving row-contiguous.
-    // acc[i][j][e] is output (row m0+wm+16i+lr, column n0+wn+16j+4g+e).
-    {
-      float* const patch = reinterpret_cast<float*>(smem + 2 * kW4Stage) + wave * (16 * kW4Pitch);
-      int ln = lane;
-      asm volatile("" : "+v"(ln));           // write-back offsets are formed here, not kept across the K loop
-      const int elr = ln & 15, eg = ln >> 4;
-      constexpr bool GU = EPI == W4_SWIGLU;
-      // a lane writes 8 columns: of rows prow and prow + 8, or (SwiGLU) of gate, up and activation of row prow
-      const int prow = GU ? ln >> 2 : ln >> 3, pcol = GU ? 32 * ((ln >> 1) & 1) + 8 * (ln & 1) : 8 * (ln & 7);
-      auto out_col = [&](int h) { return GU ? (it.n0 >> 1) + ((wn + 64 * h) >> 1) + (pcol >> 5) * 16 + (pcol & 15) : it.n0 + wn + 64 * h + pcol; };
-      const int ncols = GU ? p.gu_f : p.N;
-      auto off = [&](int row, int col, int64_t ld, bool ok) -> int { return ok ? (int)(unsigned)(((int64_t)row * ld + col) * 2) : (int)kOob; };
-      u32x4 bias_[2] = {}, bias_up[2] = {};
-      if constexpr (EPI != W4_PLAIN) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int col = out_col(h);
-          bias_[h] = __builtin_amdgcn_raw_buffer_load_b128(rbias, col < ncols ? col * 2 : (int)kOob, 0, 0);
-          if constexpr (GU) bias_up[h] = __builtin_amdgcn_raw_buffer_load_b128(rbias, col < ncols ? (col + p.gu_f) * 2 : (int)kOob, 0, 0);
-        }
-      }
-      auto patch_sync = [] {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      };
-      // What is added to block b, requested RAHEAD blocks before: one block's stores and its way through the patch take less than the latency of
-      // memory (a table of positions comes from the caches).  Forward with a residual, requested in its own block -> three ahead: 32768 x 4096 x 4096
-      // 863 -> 822 us, 32768 x 11008 x 4096 2091 -> 2056, 12000 x 5120 x 1280 120.2 -> 117.3, 9216 x 1024 x 1024 24.4 -> 23.8.
-      constexpr bool HAS_R = EPI == W4_RES || EPI == W4_TABLE;
-      constexpr int RAHEAD = EPI == W4_RES ? 3 : EPI == W4_TABLE ? 1 : 0;
-      u32x4 ring[RAHEAD + 1][2] = {};
-      auto request_res = [&](int b) {
-        const int col = out_col(b & 1);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int row = it.m0 + wm + 16 * (b >> 1) + prow + 8 * q;
-          ring[b % (RAHEAD + 1)][q] = __builtin_amdgcn_raw_buffer_load_b128(rr, off(EPI == W4_TABLE ? table_row(row, p.r_rows, p.r_magic) : row, col, p.ldc, col < ncols), 0, 0);
-        }
-      };
-      if constexpr (HAS_R) {
-#pragma unroll
-        for (int b = 0; b < RAHEAD; ++b) request_res(b);
-      }
-#pragma unroll
-      for (int b = 0; b < 2 * MI; ++b) {
-        const int i = b >> 1, h = b & 1, row0 = it.m0 + wm + 16 * i, col = out_col(h);
-        const bool ok = col < ncols;
-        if constexpr (HAS_R) if (b + RAHEAD < 2 * MI) request_res(b + RAHEAD);
-        const u32x4* const res = ring[b % (RAHEAD + 1)];
-#pragma unroll
-        for (int jj = 0; jj < 4; ++jj) {
-          f32x4& a = acc[i][4 * h + jj];
-          *reinterpret_cast<float4*>(patch + elr * kW4Pitch + 16 * jj + 4 * eg) = make_float4(a[0], a[1], a[2], a[3]);
-          a = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        patch_sync();
-        auto row8 = [&](int r, int c, float* v) {
-          const float4 x = *reinterpret_cast<const float4*>(patch + r * kW4Pitch + c), y = *reinterpret_cast<const float4*>(patch + r * kW4Pitch + c + 4);
-          v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-        };
-        if constexpr (GU) {
-          float gv[8], uv[8];
-          row8(prow, pcol, gv);
-          row8(prow, pcol + 16, uv);
-          const bf16x8 bg = __builtin_bit_cast(bf16x8, bias_[h]), bu = __builtin_bit_cast(bf16x8, bias_up[h]);
-          bf16x8 og, ou, oc;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            og[e] = (bf16)(gv[e] + (float)bg[e]);
-            ou[e] = (bf16)(uv[e] + (float)bu[e]);
-            oc[e] = (bf16)swiglu_f((float)og[e], (float)ou[e]);     // of the values as stored
-          }
-          const int row = row0 + prow;
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, og), rc, off(row, col, p.ldc, ok), 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, ou), rc, off(row, col + p.gu_f, p.ldc, ok), 0, 0);
-          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, oc), rc2, off(row, col, p.ldc2, ok), 0, 0);
-        } else {
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int row = row0 + prow + 8 * q;
-            float v[8];
-            row8(prow + 8 * q, pcol, v);
-            const bf16x8 bv = __builtin_bit_cast(bf16x8, bias_[h]), rv = __builtin_bit_cast(bf16x8, res[q]);
-            bf16x8 o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float x = v[e];
-              if constexpr (EPI != W4_PLAIN) x += (float)bv[e];
-              if constexpr (EPI == W4_RES || EPI == W4_TABLE) x += (float)rv[e];
-              o[e] = (bf16)x;
-            }
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rc, off(row, col, p.ldc, ok), 0, 0);
-            if constexpr (EPI == W4_GELU || EPI == W4_TAPS) {
-              bf16x8 a2;
-#pragma unroll
-              for (int e = 0; e < 8; ++e) a2[e] = (bf16)ErfTable::gelu(erf_table, (float)o[e]);     // of the value as stored
-              const u32x4 av = __builtin_bit_cast(u32x4, a2);
-              if constexpr (EPI == W4_TAPS) {
-                const TapRows t = tap_rows(row, p.M, p.N, p.r_rows, p.r_magic);
-                __builtin_amdgcn_raw_buffer_store_b128(av, rc2, ok && t.first >= 0 ? (int)(unsigned)((t.first + col) * 2) : (int)kOob, 0, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(t.zero ? u32x4{0u, 0u, 0u, 0u} : av, rc2, ok && t.second >= 0 ? (int)(unsigned)((t.second + col) * 2) : (int)kOob, 0, 0);
-              } else {
-                __builtin_amdgcn_raw_buffer_store_b128(av, rc2, off(row, col, p.ldc2, ok), 0, 0);
-              }
-            }
-          }
-        }
-        patch_sync();
-      }
-    }
-    if (!live) break;
-    item = next;
-    it = nit;
-  }
-  __builtin_amdgcn_s_waitcnt(0);
-  tq_done(tq);
-}
-
 // out = bf16( P[0] + P[1] + ... ) in ascending piece order, for the tiles [tile_begin,
 // tile_begin + tile_count) of the TE x TE tile list that the split launch covered.  One block
 // iteration takes 256 float4 of one tile (1024 / TE rows), so the tile's place is found once per
@@ -1456,23 +1026,6 @@ mosaic_status launch_mfma(hipStream_t s, int quota, int M, int N, int K, const b
 // The four-wave kernel takes a product when its K-contiguous operands are whole K-tiles long.
 template <bool A_KC, bool B_KC> constexpr bool w4_form() { return A_KC || !B_KC; }
 template <bool A_KC, bool B_KC> bool w4_takes(int64_t K) { return w4_form<A_KC, B_KC>() && K >= 128 && (!(A_KC || B_KC) || K % 64 == 0); }
-
-template <bool A_KC, bool B_KC, int EPI, int MI = 8>
-mosaic_status launch_w4_epi(hipStream_t s, int quota, const W4Args& p) {
-  auto kern = gemm_bf16_w4_kernel<A_KC, B_KC, EPI, MI>;
-  static std::once_flag attr_once;
-  static hipError_t attr_rc = hipSuccess;
-  std::call_once(attr_once, [&] {
-    attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, w4_lds(EPI));
-  });
-  MOSAIC_HIP(attr_rc);
-  TileQueueArgs tq;
-  int grid;
-  MOSAIC_TRY(tile_queue_plan(s, quota, 1, p.tile_count, 0, false, &tq, &grid));
-  kern<<<grid, 256, w4_lds(EPI), s>>>(p, tq);
-  MOSAIC_LAUNCH_CHECK();
-  return MOSAIC_OK;
-}
 
 // Tiles [tile_begin, tile_begin + tile_count) of the 256x256 tile list (tile_count < 0: all from
 // tile_begin on).  MI < 8: tiles of 32 * MI rows, the whole list.

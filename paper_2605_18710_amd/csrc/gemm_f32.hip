@@ -516,6 +516,85 @@ mosaic_status launch_t(hipStream_t s, int quota, F32Gemm p) {
   return MOSAIC_OK;
 }
 
+// Products of groups of rows with a matrix each (grouped.hip says how they are laid out).  A K-contiguous A: group g is rows offsets[g] ..
+// offsets[g + 1] - 1 of A and C, its tiles follow those of the group before; a K-strided A: those rows are g's contraction, of both operands, and C
+// is a matrix of its own.  Offsets are held to 0 .. bound.
+struct F32Groups {
+  const int32_t* offsets;
+  int groups, bound;
+  int64_t stride;            // elements between two groups' B, or C
+};
+constexpr int kGroupsAtOnce = 256;       // of which the first tiles are kept in LDS, a thread each
+template <typename T, int BT, int KS, bool A_KC, bool B_KC, bool VEC>
+__global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Groups gr) {
+  constexpr int STAGE = F32Tile<T, BT, KS, A_KC, VEC>::FLOATS + F32Tile<T, BT, KS, B_KC, VEC>::FLOATS;
+  __shared__ __align__(16) float lds[2 * STAGE];
+  __shared__ int starts[kGroupsAtOnce + 1], wave_total[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // tiles of all groups are dealt out as one list, wherever the batches of groups end
+  int64_t before = 0;
+  for (int g0 = 0; g0 < gr.groups; g0 += kGroupsAtOnce) {
+    const int ng = min(kGroupsAtOnce, gr.groups - g0);
+    int lo = 0, n = 0;
+    if (tid < ng) {
+      lo = min(max(gr.offsets[g0 + tid], 0), gr.bound);
+      n = max(min(max(gr.offsets[g0 + tid + 1], 0), gr.bound) - lo, 0);
+    }
+    const int mine = tid < ng ? (A_KC ? (n + BT - 1) / BT : p.tiles_m) * p.tiles_n : 0;
+    int scan = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(scan, o, 64);
+      if (lane >= o) scan += v;
+    }
+    __syncthreads();                               // everybody is done with the batch before
+    if (lane == 63) wave_total[wave] = scan;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) scan += wave_total[w];
+    if (tid < ng) starts[tid] = scan - mine;
+    if (tid == 255) starts[ng] = scan;             // threads without a group add nothing
+    __syncthreads();
+    const int all = starts[ng];
+    int64_t item = before % gridDim.x;             // the list goes on where the batch before left it
+    item = ((int64_t)blockIdx.x - item + gridDim.x) % gridDim.x;
+    for (; item < all; item += gridDim.x) {
+      int a = 0, b = ng;                           // the last group that starts at or before the tile
+      while (b - a > 1) { const int mid = (a + b) >> 1; if (starts[mid] <= item) a = mid; else b = mid; }
+      const int first = min(max(gr.offsets[g0 + a], 0), gr.bound);
+      const int rows = max(min(max(gr.offsets[g0 + a + 1], 0), gr.bound) - first, 0);
+      F32Gemm q = p;
+      q.A = (const T*)p.A + (int64_t)first * p.lda;
+      if constexpr (A_KC) {
+        q.B = (const T*)p.B + (g0 + a) * gr.stride;
+        q.C = (T*)p.C + (int64_t)first * p.ldc;
+        q.M = rows;
+        q.tiles_m = (rows + BT - 1) / BT;
+      } else {
+        q.B = (const T*)p.B + (int64_t)first * p.ldb;
+        q.C = (T*)p.C + (g0 + a) * gr.stride;
+        q.K = rows;
+        if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
+      }
+      gemm_f32_tile<T, BT, KS, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
+    }
+    before += all;
+  }
+}
+
+template <typename T, bool A_KC, bool B_KC, bool VEC>
+mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
+  const bool large = large_tiles(p.M, p.N);
+  const int bt = large ? 64 : 32;
+  const int64_t tm = ceil_div(p.M, bt), tn = ceil_div(p.N, bt), most = A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups;
+  if (most > INT32_MAX / 2) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "too many output tiles");
+  p.tiles_m = (int)tm; p.tiles_n = (int)tn;
+  const int grid = grid_for(quota, 4, most);
+  if (large) gemm_f32_grouped_kernel<T, 64, 32, A_KC, B_KC, VEC><<<grid, 256, 0, s>>>(p, gr);
+  else gemm_f32_grouped_kernel<T, 32, 64, A_KC, B_KC, VEC><<<grid, 256, 0, s>>>(p, gr);
+  MOSAIC_LAUNCH_CHECK();
+  return MOSAIC_OK;
+}
+
 template <typename T>
 mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const F32Gemm& p) {
   const uintptr_t mask = 4 * sizeof(T) - 1;                        // four elements per access where every row allows it
@@ -529,6 +608,25 @@ mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const 
 }
 
 }  // namespace
+
+// M: rows of A for all groups together, the most that there can be (a K-strided A: of each C).  K: the contraction (a K-strided A: the longest).
+mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
+                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride) {
+  if (M == 0 || N == 0 || groups == 0) return MOSAIC_OK;
+  F32Gemm p = {};
+  p.A = A; p.B = B; p.C = C; p.R = R; p.M = M; p.N = N; p.K = K; p.lda = lda; p.ldb = ldb; p.ldc = ldc;
+  const F32Groups gr = {offsets, groups, bound, stride};
+  auto go = [&](auto t) {
+    typedef decltype(t) T;
+    const uintptr_t mask = 4 * sizeof(T) - 1;
+    const bool vec = lda % 4 == 0 && ldb % 4 == 0 && ldc % 4 == 0 && N % 4 == 0 && (a_kc ? K : M) % 4 == 0 && (b_kc ? K : N) % 4 == 0 && stride % 4 == 0 &&
+                     (((uintptr_t)A | (uintptr_t)B | (uintptr_t)C | (uintptr_t)R) & mask) == 0;
+    if (!a_kc) return vec ? launch_grouped_t<T, false, false, true>(s, quota, p, gr) : launch_grouped_t<T, false, false, false>(s, quota, p, gr);
+    if (b_kc) return vec ? launch_grouped_t<T, true, true, true>(s, quota, p, gr) : launch_grouped_t<T, true, true, false>(s, quota, p, gr);
+    return vec ? launch_grouped_t<T, true, false, true>(s, quota, p, gr) : launch_grouped_t<T, true, false, false>(s, quota, p, gr);
+  };
+  return dtype == MOSAIC_BF16 ? go(bf16()) : go(float());
+}
 
 // (norm and) product (and activation) of fp32 tensors, dense rows, no output on an input or on another; *taken: in one launch
 mosaic_status launch_layer_fwd_f32(hipStream_t s, int quota, int norm, int act, int64_t T, int64_t k, int64_t n, float eps, const void* X, const void* gamma,

@@ -25,6 +25,12 @@ mosaic_status launch_gemm(hipStream_t s, int quota, int dtype, bool a_kc, bool b
 // Bytes of fp32 scratch the weight-gradient form wants for a deterministic split of a long
 // contraction over few output tiles (0 when no split is used for this shape).
 size_t gemm_splitk_scratch_bytes(int64_t M, int64_t N, int64_t K);
+// Products of rows sorted by group with their group's matrix W[k,n]; group g is rows offsets[g] .. offsets[g+1] - 1 (device memory, held to 0 .. T).
+// FWD: A = X[T,k], B = W, C = Y[T,n];  DGRAD: A = dY[T,n], B = W, C = dX[T,k];  WGRAD: A = X, B = dY, C = dW[groups,k,n].
+// Rows of no group are neither read nor written.
+enum GroupedForm { GROUPED_FWD, GROUPED_DGRAD, GROUPED_WGRAD };
+mosaic_status launch_grouped(hipStream_t s, int quota, int dtype, GroupedForm form, int64_t T, int groups, int64_t k, int64_t n, const int32_t* offsets,
+                             const void* A, const void* B, void* C);
 // Y[b, t, :] = X[b, t, :] W + bias + table[t, :]: B x rows patches of k values, ldx apart (zeros past k), W [k, n].  One rounding
 // where the bf16 matrix-core kernel takes the product and the table in its epilogue, else the product and add_pos.
 mosaic_status launch_embed_fwd(hipStream_t s, int quota, int dtype, int64_t B, int64_t rows, int64_t n, int64_t k, int64_t ldx, const void* X,
@@ -160,6 +166,12 @@ mosaic_status launch_linear_wgrad_pack8(hipStream_t s, int quota, int dtype, int
 // the same in one launch, for bf16 and small outputs (wgrad_pack8.hip)
 bool wgrad_pack8_small(int64_t T, int64_t k, int64_t n, const void* q, const void* dY, const void* dW);
 mosaic_status launch_wgrad_pack8_small(hipStream_t s, int quota, int64_t T, int64_t k, int64_t n, const void* q, const void* scale, const void* dY, void* dW, void* db);
+// softmax cross entropy behind a linear layer whose rows are table[V,h]; grad: with the gradients (either may be null)
+size_t linear_ce_scratch_bytes(int dtype, int64_t T, int64_t h, int64_t V, bool grad);
+mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, int64_t h, int64_t V, float smoothing, float denom, const int32_t* targets,
+                               const void* X, const void* table, float* loss, float* losses, bool grad, void* dX, void* dtable, void* scratch);
+// y = x * keep / (1 - drop / 65536) (+ R); rng: seed and offset on the device
+mosaic_status launch_dropout(hipStream_t s, int quota, int dtype, int64_t n, uint32_t drop, uint64_t site, const void* rng, const void* x, const void* R, void* y);
 // k=3, pad=1 convolution over frames-major [B, L, C] as gather + GEMM: out [B*Lo, 3*C] with
 // column index tap*C + channel; col2im1d is the transposed gather at stride 1 (one owner per element)
 mosaic_status launch_im2col1d(hipStream_t s, int quota, int dtype, int64_t B, int L, int Lo, int C,
