@@ -539,7 +539,7 @@ size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t 
  * count (no such token: loss 0, gradients 0).  mosaic_op_linear_ce_grad also writes the gradients of *loss: dX [T,h] and dtable [V,h] (overwritten; one of
  * them may be NULL).  Logits are fp32; bf16: the probabilities that the gradients are formed of are bf16, rounded twice relative to themselves.  What lies between is kept in
  * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
- * it holds the logits' exponentials for as many tokens at a time as 2^29 of them (1 GiB in bf16) belong to.  bf16: h a multiple of 8 and all tensors 16-byte aligned
+ * it holds the logits' exponentials for as many tokens at a time as 2^30 of them (2 GiB in bf16) belong to.  bf16: h a multiple of 8 and all tensors 16-byte aligned
  * (MOSAIC_EUNSUPPORTED otherwise); the table is smaller than 4 GiB. */
 size_t        mosaic_op_linear_ce_fwd_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
 size_t        mosaic_op_linear_ce_grad_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);

@@ -112,21 +112,41 @@ struct W4Args {
   const int32_t* offsets;          // [groups + 1], on the device: group g is rows offsets[g] .. offsets[g + 1] - 1 of A (and of B, where A is K-strided)
   int groups, bound;               // offsets are held to 0 .. bound
   int64_t stride;                  // elements between two groups' B (C, where A is K-strided)
-  int splits, split_k;             // W4_PIECES: the contraction in `splits` pieces of split_k k-values, whole K-tiles
-  const int32_t* rows;             // W4_SCATTER: where a row of the product goes in C.  W4_SOFTMAX: its target, a column or -1
-  float* sums;                     // W4_PIECES: [splits][M][N]; W4_ADD: what is there already, [M][N]
-  int first, last;                 // W4_ADD: nothing is there yet; the sum is complete and goes to C
+  int splits, split_k;             // W4_PIECES, K-strided A: the contraction in `splits` pieces of split_k k-values, whole K-tiles
+  const int32_t* rows;             // W4_PIECES, K-contiguous A: where a row of the product goes in C.  W4_SOFTMAX: its target, a column or -1
+  float* sums;                     // W4_PIECES: [pieces][rows][N], rows M, or those of the tiles that there are; W4_ADD: what is there already, [M][N]
+  int first;                       // W4_ADD: nothing is there yet
+  const int32_t* piece;            // null, or [2], on the device: a row that the operands of all rows are counted from (A: W4_SOFTMAX, B: K-strided A, and
+                                   // `rows`), and (W4_ADD) whether the sum is complete with this launch and goes to C
   // W4_SOFTMAX: see there
   float* at_target;
   float2* stats;
   float* totals;
 };
-enum { W4_PLAIN, W4_BIAS, W4_RES, W4_GELU, W4_SWIGLU, W4_TABLE, W4_TAPS, W4_SCATTER, W4_PIECES, W4_ADD, W4_SOFTMAX };
+enum { W4_PLAIN, W4_BIAS, W4_RES, W4_GELU, W4_SWIGLU, W4_TABLE, W4_TAPS, W4_PIECES, W4_ADD, W4_SOFTMAX };
 // W4_GROUPED: products of groups of rows with a matrix each; how many rows a group has is known on the device only.  The tiles of a group's
 // product follow those of the one before; tiles of a K-contiguous A are cut at the ends of its groups, a K-strided A has all tiles of
 // C for every group.  Group sizes bound the descriptors, so no tile reads or writes another group's rows.
 enum { W4_WHOLE, W4_GROUPED };
 constexpr int kMaxGroups = 1024;
+
+// W4_PIECES, K-contiguous A: into how many pieces the contraction of `tiles` tiles is cut, by the shape alone (256: CUs of the device that the kernels are written
+// for).  Microseconds: 1.45 for 64 k-values of a tile, 8 around them; the pass that adds the pieces at 5 TB/s behind 5.  dz table for 4096, 1280 of 51001: 30 tiles,
+// one round however long; 6144 x 4096 of 128000: 384 tiles, 5600 us in two rounds, 4400 as three rounds of half the length.
+constexpr int kMostPieces = 16, kMostPieceTiles = 2048;
+struct W4Cut { int pieces, k; };
+__device__ __host__ __forceinline__ W4Cut w4_cut(int tiles, int K) {
+  W4Cut best = {1, (K + 63) / 64 * 64};
+  float least = (float)((tiles + 255) / 256) * ((float)(best.k / 64) * 1.45f + 8.f);
+  for (int n = 2; n <= kMostPieces && n * tiles <= kMostPieceTiles; ++n) {
+    const int k = ((K + n - 1) / n + 63) / 64 * 64;
+    if (k < 1024) break;
+    const int pieces = (K + k - 1) / k;
+    const float us = (float)((tiles * pieces + 255) / 256) * ((float)(k / 64) * 1.45f + 8.f) + (float)tiles * (float)(4 * pieces + 2) * 0.0131f + 5.f;
+    if (us < least) { least = us; best = {pieces, k}; }
+  }
+  return best;
+}
 constexpr int kW4Stage = 2 * 256 * 64 * 2;                         // both operands of a K-tile
 constexpr int kW4Pitch = 68;                                       // floats per row of the epilogue's patch: 16 rows of 64
 constexpr int kW4Patch = 4 * 16 * kW4Pitch * 4;
@@ -244,52 +264,60 @@ struct W4GroupTiles {
 // Rounded relative to its block's maximum a probability keeps bf16's 2^-9 relative to itself whatever the logits' size; the logits in bf16 would
 // be off by 2^-9 of theirs, which the exponential turns into that much of a probability times the logit.
 // A block whose largest logit is -infinity counts from 0: its sum is 0.  NaN and +infinity make the sum NaN.  m is kept times log2 e.
-// Here for eight columns col.. of one row; the eight lanes of a block lie side by side.
+// Here for one row of a block, a lane's sixteen values v[j][e], columns col + 16j + 4g + e; the four lanes of a row lie 16 apart (g = 0 .. 3).
 constexpr int kCeBlock = 64;
-template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
-constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppMirror8 = 0x141;      // the last one gives the other four lanes' where all four have the same
-__device__ __forceinline__ bf16x8 w4_softmax(const W4Args& p, float (&v)[8], int row, int col, int target, bool in) {
+// what the four lanes of a row make of their values together
+template <typename F> __device__ __forceinline__ float across_rows(float x, F f) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);       // the low half's in both halves, and the high half's
+  x = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);       // the same by 16 lanes
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ void w4_softmax(const W4Args& p, f32x4 (&v)[4], int row, int col, int g, int target, bool in) {
   constexpr float kLog2e = 1.44269504088896340736f;
+  auto add = [](float a, float b) { return a + b; };
+  auto high = [](float a, float b) { return fmaxf(a, b); };
   const int hit = target - col;
-  const float a = hit & 1 ? v[1] : v[0], b = hit & 1 ? v[3] : v[2], c = hit & 1 ? v[5] : v[4], d = hit & 1 ? v[7] : v[6];
-  const float ab = hit & 2 ? b : a, cd = hit & 2 ? d : c;
-  if (hit >= 0 && hit < 8 && in && target < p.N) p.at_target[row] = hit & 4 ? cd : ab;
-  const bool first = (threadIdx.x & 7) == 0 && in && col < p.N;
+  const bool mine = in && hit >= 0 && hit < kCeBlock && target < p.N && ((hit >> 2) & 3) == g;
+  if (__ballot(mine)) {
+    float t = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = hit & 1 ? v[j][1] : v[j][0], b = hit & 1 ? v[j][3] : v[j][2];
+      t = hit >> 4 == j ? (hit & 2 ? b : a) : t;
+    }
+    if (mine) p.at_target[row] = t;
+  }
+  const bool first = g == 0 && in && col < p.N;
   const int64_t slot = (int64_t)(col / kCeBlock) * p.M + row;
   if (p.totals) {
     float total = 0.f;                             // rows of the table past its end read zeros
 #pragma unroll
-    for (int e = 0; e < 8; ++e) total += v[e];
-    total += dpp<kDppXor1>(total);
-    total += dpp<kDppXor2>(total);
-    total += dpp<kDppMirror8>(total);
+    for (int j = 0; j < 4; ++j) total += (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
+    total = across_rows(total, add);
     if (first) p.totals[slot] = total;
   }
-  if (col + 8 > p.N) {
+  if (col + kCeBlock > p.N) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = col + e < p.N ? v[e] : -INFINITY;
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[j][e] = col + 16 * j + 4 * g + e < p.N ? v[j][e] : -INFINITY;
   }
-  float m = v[0];
+  float m = -INFINITY;
 #pragma unroll
-  for (int e = 1; e < 8; ++e) m = fmaxf(m, v[e]);
-  m = fmaxf(m, dpp<kDppXor1>(m));
-  m = fmaxf(m, dpp<kDppXor2>(m));
-  m = fmaxf(m, dpp<kDppMirror8>(m));
+  for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fmaxf(v[j][0], v[j][1]), fmaxf(v[j][2], v[j][3])));
+  m = across_rows(m, high);
   const float ref = m == -INFINITY ? 0.f : m * kLog2e;
   float sum = 0.f;
-  bf16x8 o;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int j = 0; j < 4; ++j) {
     // fused: the product rounded before the subtraction would cost 2^-24 of the logit
-    const float x = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, -ref));
-    sum += x;
-    o[e] = (bf16)x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[j][e] = __builtin_amdgcn_exp2f(fmaf(v[j][e], kLog2e, -ref));
+    sum += (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
   }
-  sum += dpp<kDppXor1>(sum);
-  sum += dpp<kDppXor2>(sum);
-  sum += dpp<kDppMirror8>(sum);
+  sum = across_rows(sum, add);
   if (first) p.stats[slot] = make_float2(ref, sum);
-  return o;
 }
 
 template <bool A_KC, bool B_KC, int EPI, int MI, int MAP = W4_WHOLE>
@@ -318,10 +346,20 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
     tiles_of.fill(p.offsets, p.bound, 32 * MI);
     __syncthreads();
     // the list is as long as the groups make it; the host's length is that of the longest
-    tq.n_items = tiles_of.starts[p.groups] * p.tiles_n * (EPI == W4_PIECES ? p.splits : 1);
+    tq.n_items = tiles_of.starts[p.groups] * p.tiles_n;
+    if constexpr (EPI == W4_PIECES) {
+      const W4Cut cut = w4_cut(tq.n_items, p.K);
+      p.splits = cut.pieces;
+      p.split_k = cut.k;
+      p.M = tiles_of.starts[p.groups] * 32 * MI;
+      tq.n_items *= cut.pieces;
+    }
     tq.n_full = tq.n_items / (8 * tq.chunk) * (8 * tq.chunk);
     tq.tail_per = (tq.n_items - tq.n_full + 7) / 8;
   }
+  const int start = GROUPED && p.piece ? __builtin_amdgcn_readfirstlane(p.piece[0]) : 0;
+  const bool last = EPI == W4_ADD && p.piece && __builtin_amdgcn_readfirstlane(p.piece[1]);
+  if (EPI == W4_ADD && !p.first && !last && p.offsets[1] <= p.offsets[0]) { tq.n_items = tq.n_full = tq.tail_per = 0; }      // nothing to add
   auto decode = [&](int item) -> Item {
     int trow, tcol;
     if constexpr (GROUPED) {
@@ -365,12 +403,13 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
     k_left = p.K - it.k0;
     if constexpr (GROUPED && A_KC) {
       const bf16* B = p.B + it.g * p.stride;
-      ca.set(p.A + it.lo * p.lda, ((uint64_t)it.m0 * p.lda + it.k0) * 2, ((uint64_t)(it.hi - it.lo - 1) * p.lda + p.K) * 2);
+      ca.set(p.A + (int64_t)(it.lo + (EPI == W4_SOFTMAX ? start : 0)) * p.lda, ((uint64_t)it.m0 * p.lda + it.k0) * 2,
+             ((uint64_t)(it.hi - it.lo - 1) * p.lda + p.K) * 2);
       cb.set(B, ((uint64_t)it.n0 * (B_KC ? p.ldb : 1) + (uint64_t)it.k0 * (B_KC ? 1 : p.ldb)) * 2, p.b_bytes);
     } else if constexpr (GROUPED) {
       const uint64_t n = (uint64_t)(it.hi - it.lo);
-      ca.set(p.A + it.lo * p.lda, (uint64_t)it.m0 * 2, n ? ((n - 1) * p.lda + (p.M + 7) / 8 * 8) * 2 : 0);      // whole 16-byte pieces: a row has them
-      cb.set(p.B + it.lo * p.ldb, (uint64_t)it.n0 * 2, n ? ((n - 1) * p.ldb + p.N) * 2 : 0);
+      ca.set(p.A + (int64_t)it.lo * p.lda, (uint64_t)it.m0 * 2, n ? ((n - 1) * p.lda + (p.M + 7) / 8 * 8) * 2 : 0);      // whole 16-byte pieces: a row has them
+      cb.set(p.B + (int64_t)(it.lo + start) * p.ldb, (uint64_t)it.n0 * 2, n ? ((n - 1) * p.ldb + p.N) * 2 : 0);
     } else {
       ca.set(p.A, A_KC ? (uint64_t)it.m0 * p.lda * 2 : (uint64_t)it.m0 * 2, p.a_bytes);
       cb.set(p.B, B_KC ? (uint64_t)it.n0 * p.ldb * 2 : (uint64_t)(EPI == W4_SWIGLU ? it.n0 : it.n0 * 2), p.b_bytes);
@@ -519,7 +558,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
       const int ncols = GU ? p.gu_f : p.N;
       auto off = [&](int row, int col, int64_t ld, bool ok) -> int { return ok ? (int)(unsigned)(((int64_t)row * ld + col) * 2) : (int)kOob; };
       u32x4 bias_[2] = {}, bias_up[2] = {};
-      constexpr bool HAS_BIAS = EPI != W4_PLAIN && EPI < W4_SCATTER;
+      constexpr bool HAS_BIAS = EPI != W4_PLAIN && EPI < W4_PIECES;
       if constexpr (HAS_BIAS) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -551,15 +590,77 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
 #pragma unroll
         for (int b = 0; b < RAHEAD; ++b) request_res(b);
       }
-      // W4_SCATTER: where this lane's rows go; W4_SOFTMAX: their targets
-      int of_row[EPI == W4_SCATTER || EPI == W4_SOFTMAX ? 2 * MI : 1];
-      if constexpr (EPI == W4_SCATTER || EPI == W4_SOFTMAX) {
+      // W4_PIECES: where this lane's rows go; W4_SOFTMAX: their targets
+      constexpr bool TO_ROWS = EPI == W4_PIECES && A_KC;
+      int of_row[2 * MI];
+      if constexpr (TO_ROWS || EPI == W4_SOFTMAX) {
 #pragma unroll
-        for (int i = 0; i < 2 * MI; ++i) {
-          const int row = wm + 8 * i + prow;
-          of_row[i] = row < rows ? p.rows[it.lo + it.m0 + row] : -1;
+        for (int i = 0; i < (EPI == W4_SOFTMAX ? MI : 2 * MI); ++i) {
+          const int row = wm + (EPI == W4_SOFTMAX ? 16 * i + elr : 8 * i + prow);
+          of_row[i] = row < rows ? p.rows[start + it.lo + it.m0 + row] : -1;
         }
       }
+      // Groups of rows, no sums: 16 rows x 64 columns are rounded to bf16 where they are and pass through one of two patches of 2 KB (rows of 128
+      // bytes, 16-byte chunks XOR-swizzled by the row), from which a block is read while the next is worked on and stored behind it.
+      if constexpr (GROUPED && (EPI == W4_PLAIN || EPI == W4_SOFTMAX || EPI == W4_PIECES)) {
+        unsigned char* const half = reinterpret_cast<unsigned char*>(smem + 2 * kW4Stage) + wave * (64 * kW4Pitch);
+        u32x4 leaving[2][2];
+        const int last_col = EPI == W4_SOFTMAX ? (int)p.ldc : p.N;
+        auto leave = [&](int b) {
+          const int col = it.n0 + wn + 64 * (b & 1) + 8 * (ln & 7);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const int row = wm + 16 * (b >> 1) + prow + 8 * q;
+            if constexpr (TO_ROWS) {
+              const int to = of_row[2 * (b >> 1) + q];
+              if (col < last_col && to >= 0) *reinterpret_cast<u32x4*>(p.C + (int64_t)to * p.ldc + col) = leaving[b & 1][q];
+            } else {
+              __builtin_amdgcn_raw_buffer_store_b128(leaving[b & 1][q], rc, off(row, col, p.ldc, col < last_col), 0, 0);
+            }
+          }
+        };
+#pragma unroll
+        for (int b = 0; b < 2 * MI; ++b) {
+          const int i = b >> 1, h = b & 1;
+          f32x4 v[4];
+#pragma unroll
+          for (int jj = 0; jj < 4; ++jj) {
+            // moved here and not before: left to itself the compiler moves all 256 accumulators at once, to registers that there are not
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float x;
+              asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[i][4 * h + jj][e]));
+              v[jj][e] = x;
+            }
+            acc[i][4 * h + jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+          }
+          if constexpr (EPI == W4_SOFTMAX) {
+            const int row = wm + 16 * i + elr;
+            w4_softmax(p, v, it.m0 + row, it.n0 + wn + 64 * h, eg, of_row[i], row < rows);
+          }
+          if (EPI == W4_PIECES && p.splits > 1) {        // a piece's sums, in fp32
+            const int row = wm + 16 * i + elr, col = it.n0 + wn + 64 * h + 4 * eg;
+            float* const at = p.sums + ((int64_t)it.split * p.M + (A_KC ? it.lo : 0) + it.m0 + row) * p.N + col;
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj) if (row < rows && col + 16 * jj < p.N) *reinterpret_cast<f32x4*>(at + 16 * jj) = v[jj];
+          } else if (EPI != W4_SOFTMAX || p.C) {
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj) {
+              bf16x4 o;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[e] = (bf16)v[jj][e];
+              *reinterpret_cast<bf16x4*>(half + 2048 * (b & 1) + elr * 128 + (((2 * jj + (eg >> 1)) ^ (elr & 7)) << 4) + 8 * (eg & 1)) = o;
+            }
+            patch_sync();
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              leaving[b & 1][q] = *reinterpret_cast<const u32x4*>(half + 2048 * (b & 1) + (prow + 8 * q) * 128 + (((ln & 7) ^ (prow & 7)) << 4));
+            if (b > 0) leave(b - 1);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (EPI == W4_PIECES ? p.splits == 1 : EPI != W4_SOFTMAX || p.C) leave(2 * MI - 1);
+      } else {
       // W4_ADD: the sums so far, requested a block ahead
       float4 before[EPI == W4_ADD ? 2 : 1][2][2];
       auto sum_at = [&](int b, int q) -> float4* {
@@ -615,25 +716,12 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
             const int row = row0 + prow + 8 * q;
             float v[8];
             row8(prow + 8 * q, pcol, v);
-            if constexpr (EPI == W4_SOFTMAX) {
-              const bf16x8 x = w4_softmax(p, v, it.m0 + row, col, of_row[2 * i + q], row < rows);
-              if (p.C) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), rc, off(row, col, p.ldc, col < p.ldc), 0, 0);
-              continue;
-            }
-            if constexpr (EPI == W4_PIECES) {
-              if (row < rows && ok) {
-                float4* at = reinterpret_cast<float4*>(p.sums + ((int64_t)it.split * p.M + (A_KC ? it.lo : 0) + it.m0 + row) * p.N + col);
-                at[0] = make_float4(v[0], v[1], v[2], v[3]);
-                at[1] = make_float4(v[4], v[5], v[6], v[7]);
-              }
-              continue;
-            }
             if constexpr (EPI == W4_ADD) {
               const float4 x = before[b & 1][q][0], y = before[b & 1][q][1];
               const float old[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
               for (int e = 0; e < 8; ++e) v[e] += old[e];
-              if (!p.last) {
+              if (!last) {
                 if (float4* at = sum_at(b, q)) {
                   at[0] = make_float4(v[0], v[1], v[2], v[3]);
                   at[1] = make_float4(v[4], v[5], v[6], v[7]);
@@ -649,11 +737,6 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
               if constexpr (HAS_BIAS) x += (float)bv[e];
               if constexpr (EPI == W4_RES || EPI == W4_TABLE) x += (float)rv[e];
               o[e] = (bf16)x;
-            }
-            if constexpr (EPI == W4_SCATTER) {
-              const int to = of_row[2 * i + q];
-              if (ok && to >= 0) *reinterpret_cast<bf16x8*>(p.C + (int64_t)to * p.ldc + col) = o;
-              continue;
             }
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o), rc, off(row, col, p.ldc, ok), 0, 0);
             if constexpr (EPI == W4_GELU || EPI == W4_TAPS) {
@@ -672,6 +755,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
           }
         }
         patch_sync();
+      }
       }
     }
     if (!live) break;

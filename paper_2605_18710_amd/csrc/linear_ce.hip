@@ -4,7 +4,7 @@
 //   loss = sum l_t / D;  dz_tv = (softmax(z_t)_v - (1 - s) [v = target] - s / V) / D;  dX = dz table;  dtable = dz^T X
 // with D given, or the number of such tokens.  The others take no part: their rows of X are not multiplied (they may hold anything).
 //
-//   1. The tokens that count are listed in order, and their rows copied side by side (rows_kernel, gather_kernel): how many there are
+//   1. The tokens that count are listed in order, and their rows copied side by side (list_kernel, place_kernel): how many there are
 //      stays on the device, where the products' workgroups read it.
 //   2. In pieces of tokens (kPieceElems): the product with the table, whose epilogue leaves exp(z - m) in bf16 and, for each row and 64 columns, the
 //      largest logit m and the sum (w4_softmax in gemm_w4.h); or only these, when the loss alone is asked for.
@@ -27,21 +27,31 @@ constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f
 
 // ------------------------------------------------------------------------- the tokens that count
 struct CeHead { int count; float per_token; };      // their number, and 1 / D
+struct CeSpan { int zero, live, start, last; };     // of a piece: 0, how many tokens it has, the first of them, whether none follow
 
-// In order: rows[i] = token, target[i] = its target; slot[t] = i, or -1; piece_rows[2p], [2p + 1] = 0 and how many of them piece p of `piece` tokens has.
-// One workgroup: 16 waves in order, lanes in order.
-constexpr int kRowsThreads = 1024;
-__global__ __launch_bounds__(kRowsThreads) void rows_kernel(const int32_t* __restrict__ targets, int T, int V, float denom, int piece, int pieces,
-                                                            CeHead* __restrict__ head, int32_t* __restrict__ piece_rows, int32_t* __restrict__ rows,
-                                                            int32_t* __restrict__ target, int32_t* __restrict__ slot) {
-  constexpr int kWaves = kRowsThreads / 64;
+struct CeList {
+  const int32_t* targets;
+  int T, V, piece, pieces;
+  float denom;
+  int balanced;            // pieces of equal size, as few as hold the tokens (else `piece` tokens each)
+  CeHead* head;
+  CeSpan* spans;
+  int32_t *rows, *target;  // in order: the token, and its target
+  int32_t* slot;           // of a token: its place in that order, or -1
+};
+
+// One workgroup: 16 waves in order, lanes in order.  `write`: to memory; each(t, at) for every token a thread looks at, at < 0 where it does not count.
+constexpr int kListThreads = 1024;
+template <typename F>
+__device__ __forceinline__ void list_tokens(const CeList& l, bool write, F each) {
+  constexpr int kWaves = kListThreads / 64;
   __shared__ int wave_count[2][kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int run = 0;
-  for (int t0 = 0, turn = 0; t0 < T; t0 += kRowsThreads, turn ^= 1) {
-    const int t = t0 + threadIdx.x;
-    const int y = t < T ? targets[t] : -1;
-    const bool counts = y >= 0 && y < V;
+  int run = 0, y = (int)threadIdx.x < l.T ? l.targets[threadIdx.x] : -1;
+  for (int t0 = 0, turn = 0; t0 < l.T; t0 += kListThreads, turn ^= 1) {
+    const int t = t0 + threadIdx.x, here = y;
+    y = t + kListThreads < l.T ? l.targets[t + kListThreads] : -1;       // its latency passes under this turn
+    const bool counts = here >= 0 && here < l.V;
     const unsigned long long m = __ballot(counts);
     if (lane == 0) wave_count[turn][wave] = __popcll(m);
     __syncthreads();                             // the other half of wave_count was read before the barrier of the turn before
@@ -52,38 +62,56 @@ __global__ __launch_bounds__(kRowsThreads) void rows_kernel(const int32_t* __res
       if (w < wave) before += n;
       run += n;
     }
-    const int at = before + __popcll(m & ((1ull << lane) - 1ull));
-    if (counts) { rows[at] = t; target[at] = y; }
-    if (t < T) slot[t] = counts ? at : -1;
+    const int at = counts ? before + __popcll(m & ((1ull << lane) - 1ull)) : -1;
+    if (write && counts) { l.rows[at] = t; l.target[at] = here; }
+    if (t < l.T) each(t, at);
   }
-  for (int p = threadIdx.x; p < pieces; p += kRowsThreads) {
-    piece_rows[2 * p] = 0;
-    piece_rows[2 * p + 1] = (int)min((int64_t)piece, max((int64_t)run - (int64_t)p * piece, (int64_t)0));
+  if (!write) return;
+  const int n = l.balanced ? max(1, (int)(((int64_t)run + l.piece - 1) / l.piece)) : l.pieces;
+  const int size = l.balanced ? min(l.piece, ((run + n - 1) / n + 255) / 256 * 256) : l.piece;
+  for (int p = threadIdx.x; p < l.pieces; p += kListThreads) {
+    const int start = (int)min((int64_t)p * size, (int64_t)run);
+    l.spans[p] = {0, p < n ? min(size, run - start) : 0, start, p == n - 1};
   }
-  if (threadIdx.x == 0) *head = {run, denom > 0.f ? 1.f / denom : run ? 1.f / (float)run : 0.f};
+  if (threadIdx.x == 0) *l.head = {run, l.denom > 0.f ? 1.f / l.denom : run ? 1.f / (float)run : 0.f};
 }
 
-// A wave per token: its row of X to where it counts, or zeros to its gradient and loss.
+// A token's row of X to its place, or zeros to its gradient and loss; by one wave
 template <typename T, int V>
-__global__ __launch_bounds__(256) void gather_kernel(const T* __restrict__ X, const int32_t* __restrict__ slot, int tokens, int64_t h, T* __restrict__ Xc,
-                                                     T* __restrict__ dX, float* __restrict__ losses) {
+__device__ __forceinline__ void place_row(int64_t t, int at, const T* X, int64_t h, T* Xc, T* dX, float* losses) {
   typedef typename Pack<T, V>::type vec;
   const int lane = threadIdx.x & 63;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += (int64_t)gridDim.x * 4) {
-    const int at = slot[t];
-    if (at >= 0) {
-      for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(Xc + at * h + c) = *reinterpret_cast<const vec*>(X + t * h + c);
-    } else {
-      if (dX) for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(dX + t * h + c) = vec{};
-      if (lane == 0) losses[t] = 0.f;
-    }
+  if (at >= 0) {
+    for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(Xc + at * h + c) = *reinterpret_cast<const vec*>(X + t * h + c);
+  } else {
+    if (dX) for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(dX + t * h + c) = vec{};
+    if (lane == 0) losses[t] = 0.f;
   }
+}
+__global__ __launch_bounds__(kListThreads) void list_kernel(CeList l) {
+  list_tokens(l, true, [&](int t, int at) { l.slot[t] = at; });
+}
+template <typename T, int V>
+__global__ __launch_bounds__(256) void place_kernel(const int32_t* __restrict__ slot, int tokens, const T* __restrict__ X, int64_t h, T* __restrict__ Xc,
+                                                    T* __restrict__ dX, float* __restrict__ losses) {
+  for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += (int64_t)gridDim.x * 4) place_row<T, V>(t, slot[t], X, h, Xc, dX, losses);
+}
+// Both in one launch up to kListMax tokens: every workgroup makes the list for itself (a turn of 1024 tokens takes a microsecond, a launch four),
+// the first one writes it.
+constexpr int kListMax = 4096;
+template <typename T, int V>
+__global__ __launch_bounds__(kListThreads) void list_place_kernel(CeList l, const T* __restrict__ X, int64_t h, T* __restrict__ Xc, T* __restrict__ dX,
+                                                                  float* __restrict__ losses) {
+  __shared__ int slot[kListMax];
+  list_tokens(l, blockIdx.x == 0, [&](int t, int at) { slot[t] = at; });
+  __syncthreads();
+  for (int t = blockIdx.x * 16 + (threadIdx.x >> 6); t < l.T; t += gridDim.x * 16) place_row<T, V>(t, slot[t], X, h, Xc, dX, losses);
 }
 
 // -------------------------------------------------------------------------- rows of the softmax
 struct CePiece {
-  const int32_t* live;         // [1]: how many tokens it has
-  const int32_t *rows, *target;
+  const CeSpan* span;
+  const int32_t *rows, *target;      // of all tokens
   const float* at_target;
   int capacity, V;
   float smoothing;
@@ -91,80 +119,105 @@ struct CePiece {
   float* losses;
 };
 
-// 64 rows to a workgroup, a lane each; sixteen waves share their blocks, whose statistics lie row by row.
+// (m, sum) of two sets of columns; where nothing has come yet there is nothing to scale; infinities and NaN go into the sum as they are
+__device__ __forceinline__ void join_sums(float& top, float& sum, float m, float s) {
+  const float high = fmaxf(top, m);
+  sum = (top == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f(top - high)) + (m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f(m - high));
+  top = high;
+}
+// A row's (m, sum) and totals over its blocks, by 64 groups of 16 lanes, a lane to a row; in the first group on return.
+struct RowSums { float (*top)[16], (*sum)[16], (*total)[16]; };       // [16][16] each, in LDS
+__device__ __forceinline__ void row_sums(const float2* stats, const float* totals, int blocks, int64_t pitch, int row, RowSums lds, float& top, float& sum, float& total) {
+  const int r = threadIdx.x & 15, wave = threadIdx.x >> 6;
+  top = -INFINITY; sum = 0.f; total = 0.f;
+  for (int b0 = threadIdx.x >> 4; b0 < blocks; b0 += 64 * 8) {
+    float2 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = b0 + 64 * u < blocks ? stats[(b0 + 64 * u) * pitch + row] : make_float2(-INFINITY, 0.f);
+    float high = top;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) high = fmaxf(high, v[u].x);
+    if (high != top) { sum = top == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f(top - high); top = high; }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) sum = fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - top), sum);
+    if (totals) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) total += totals[(b0 + 64 * u) * pitch + row];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {
+    const float m = __shfl_xor(top, o, 64), s = __shfl_xor(sum, o, 64);
+    // in the same order on both sides
+    if (threadIdx.x & o) { float a = m, b = s; join_sums(a, b, top, sum); top = a; sum = b; }
+    else join_sums(top, sum, m, s);
+    total += __shfl_xor(total, o, 64);
+  }
+  if ((threadIdx.x & 63) < 16) { lds.top[wave][r] = top; lds.sum[wave][r] = sum; lds.total[wave][r] = total; }
+  __syncthreads();
+  if (threadIdx.x < 16) {
+#pragma unroll
+    for (int w = 1; w < 16; ++w) { join_sums(top, sum, lds.top[w][r], lds.sum[w][r]); total += lds.total[w][r]; }
+  }
+  __syncthreads();
+}
+__device__ __forceinline__ float token_loss(float lse, float at_target, float total, float smoothing, int V) {
+  const float loss = lse * kLn2 - (1.f - smoothing) * at_target;
+  return smoothing > 0.f ? loss - smoothing * (total / (float)V) : loss;
+}
+
+// 16 rows to a workgroup: their statistics lie side by side.
 __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, int blocks) {
-  __shared__ float top_of[16][64], sum_of[16][64], total_of[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, live = p.live[1];
-  for (int r0 = blockIdx.x * 64; r0 < live; r0 += gridDim.x * 64) {
-    const int row = r0 + lane;                   // below capacity, a multiple of 64
-    float top = -INFINITY, sum = 0.f, total = 0.f;
-    for (int b0 = wave; b0 < blocks; b0 += 16 * 8) {
-      float2 v[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) v[u] = b0 + 16 * u < blocks ? stats[(int64_t)(b0 + 16 * u) * p.capacity + row] : make_float2(-INFINITY, 0.f);
-      float high = top;
-#pragma unroll
-      for (int u = 0; u < 8; ++u) high = fmaxf(high, v[u].x);
-      // where nothing has come yet there is nothing to scale; infinities and NaN go into the sum as they are
-      if (high != top) { sum *= __builtin_amdgcn_exp2f(top - high); top = high; }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) if (b0 + 16 * u < blocks) sum = fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - top), sum);
-      if (totals) {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) if (b0 + 16 * u < blocks) total += totals[(int64_t)(b0 + 16 * u) * p.capacity + row];
-      }
-    }
-    top_of[wave][lane] = top; sum_of[wave][lane] = sum; total_of[wave][lane] = total;
-    __syncthreads();
-    if (wave == 0 && row < live) {
-      float high = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) high = fmaxf(high, top_of[w][lane]);
-      float all = 0.f, z = 0.f;
-#pragma unroll
-      for (int w = 0; w < 16; ++w) {
-        if (top_of[w][lane] != -INFINITY) all = fmaf(sum_of[w][lane], __builtin_amdgcn_exp2f(top_of[w][lane] - high), all);
-        z += total_of[w][lane];
-      }
-      const float lse = high + __builtin_amdgcn_logf(all);      // to the base of 2
+  __shared__ float top_of[16][16], sum_of[16][16], total_of[16][16];
+  const int live = p.span->live, start = p.span->start;
+  for (int r0 = blockIdx.x * 16; r0 < live; r0 += gridDim.x * 16) {
+    const int row = r0 + (threadIdx.x & 15);     // below capacity, a multiple of 16
+    float top, sum, total;
+    row_sums(stats, totals, blocks, p.capacity, row, {top_of, sum_of, total_of}, top, sum, total);
+    if (threadIdx.x < 16 && row < live) {
+      const float lse = top + __builtin_amdgcn_logf(sum);      // to the base of 2
       p.lse[row] = lse;
-      float loss = lse * kLn2 - (1.f - p.smoothing) * p.at_target[row];
-      if (totals) loss -= p.smoothing * (z / (float)p.V);
-      p.losses[p.rows[row]] = loss;
+      p.losses[p.rows[start + row]] = token_loss(lse, p.at_target[row], total, p.smoothing, p.V);
     }
-    __syncthreads();
   }
 }
 
-// exp(z - m) -> dz, in place: a strip of 16 rows and 1024 columns at a time, 16 bytes to a lane.
+// exp(z - m) -> dz, in place: a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
 constexpr int kStrip = 1024;
+template <bool PAST>
 __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const CeHead* __restrict__ head, const float2* __restrict__ stats, bf16* __restrict__ E, int64_t ld) {
-  const int live = p.live[1], strips = (int)((ld + kStrip - 1) / kStrip);
+  const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
   const float g = head->per_token, even = p.smoothing / (float)p.V;
   const int64_t items = (int64_t)((live + 15) / 16) * strips;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int r0 = (int)(item / strips) * 16, c0 = (int)(item % strips) * kStrip;
+    const int col = c0 + 8 * (threadIdx.x & 127);
     Vec16<bf16> v[8];
+    float scale[8], lse[8];
+    int hit[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = r0 + 2 * i + (threadIdx.x >> 7), col = c0 + 8 * (threadIdx.x & 127);
-      if (row < live && col < ld) v[i].load(E + (int64_t)row * ld + col);
+      const int row = r0 + 2 * i + (threadIdx.x >> 7);
+      if (row >= live || col >= ld) continue;
+      v[i].load<PAST>(E + (int64_t)row * ld + col);
+      lse[i] = p.lse[row];
+      scale[i] = stats[(int64_t)(col / kCeBlock) * p.capacity + row].x;
+      hit[i] = p.target[start + row] - col;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int row = r0 + 2 * i + (threadIdx.x >> 7), col = c0 + 8 * (threadIdx.x & 127);
+      const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
-      const float lse = p.lse[row];
-      const float scale = __builtin_amdgcn_exp2f(stats[(int64_t)(col / kCeBlock) * p.capacity + row].x - lse);
-      const int hit = p.target[row] - col;
+      const float f = __builtin_amdgcn_exp2f(scale[i] - lse[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float d = v[i].get(e) * scale - even;
+      for (int e = 0; e < 8; ++e) v[i].set(e, col + e < p.V ? (v[i].get(e) * f - even) * g : 0.f);
+      if (hit[i] >= 0 && hit[i] < 8) {
         // the target's probability from its own logit: 1 - p keeps its digits where p is near 1
-        if (e == hit) d = (__builtin_amdgcn_exp2f(fmaf(p.at_target[row], kLog2e, -lse)) - 1.f) + (p.smoothing - even);
-        v[i].set(e, col + e < p.V ? d * g : 0.f);
+        const float d = ((__builtin_amdgcn_exp2f(fmaf(p.at_target[row], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even)) * g;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) if (e == hit[i]) v[i].set(e, d);
       }
-      v[i].store(E + (int64_t)row * ld + col);
+      v[i].store<PAST>(E + (int64_t)row * ld + col);
     }
   }
 }
@@ -180,11 +233,11 @@ __device__ __forceinline__ float block_reduce(float x, bool max, float* lds) {
 // fp32 logits, a workgroup per row: loss and (Z written) dz in place
 __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, int grad) {
   __shared__ float lds[4];
-  const int live = p.live[1];
+  const int live = p.span->live, start = p.span->start;
   const float g = head->per_token, even = p.smoothing / (float)p.V;
   for (int row = blockIdx.x; row < live; row += gridDim.x) {
     float* z = Z + row * ld;
-    const int target = p.target[row];
+    const int target = p.target[start + row];
     float top = -INFINITY, total = 0.f;
     for (int c = threadIdx.x; c < p.V; c += 256) { top = fmaxf(top, z[c]); total += z[c]; }
     top = block_reduce(top, true, lds);
@@ -196,7 +249,7 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* 
     if (threadIdx.x == 0) {
       float loss = lse - (1.f - p.smoothing) * z[target];
       if (p.smoothing > 0.f) loss -= p.smoothing * (total / (float)p.V);
-      p.losses[p.rows[row]] = loss;
+      p.losses[p.rows[start + row]] = loss;
     }
     if (!grad) continue;
     __syncthreads();                             // the target's logit has been read
@@ -207,12 +260,168 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* 
   }
 }
 
+// ------------------------------------------------------------------------- a few tokens
+// The loss alone of up to 16 tokens (a scored continuation, the single token of a serving step): the table is read once, and that is the time.  Every
+// wave takes 16 of its rows at a time straight into registers, 64 k-values of each (whole 128-byte lines, 32 bytes to a lane) in two matrix instructions
+// whose second operand are the tokens, which lie in LDS; what leaves is (m, sum) of the 16 rows for every token.  Eight steps are requested ahead,
+// eight waves to a CU: 32 MB in flight.  One token, h 4096, V 32000 (262 MB): 52.5 us (5.0 TB/s), by the four-wave kernel in tiles of 128 rows 94.
+constexpr int kFew = 16, kFewThreads = 512, kFewAhead = 8;
+constexpr int kFewLds = 150 << 10;
+inline int few_pitch(int64_t h) { return (int)(align_up((size_t)h, 64) * 2 + 16); }      // bytes of a token in LDS: 16 past whole steps, so that 16 rows touch every bank
+struct CeFew {
+  const int32_t* targets;
+  const bf16 *X, *table;
+  int T, h, V, pitch;
+  float smoothing, denom;
+  float2* stats;           // [kFew][ceil(V / 16)]
+  float *totals, *at_target;
+  float *losses, *loss;
+};
+// lane t's target, its place among the tokens that count (-1: none); *live: their number.  T <= kFew
+__device__ __forceinline__ int few_place(const CeFew& p, int lane, int* y, int* live) {
+  *y = lane < p.T ? p.targets[lane] : -1;
+  const bool counts = *y >= 0 && *y < p.V;
+  const unsigned long long m = __ballot(counts);
+  *live = __popcll(m);
+  return counts ? __popcll(m & ((1ull << lane) - 1ull)) : -1;
+}
+__global__ __launch_bounds__(kFewThreads) void few_kernel(CeFew p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int token_of[kFew], target_of[kFew];
+  typedef std::integral_constant<int, 0> B0;
+  typedef std::integral_constant<int, 1> B1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, g = lane >> 4;
+  const int tiles = (p.V + 15) / 16, stride = (int)gridDim.x * (kFewThreads / 64), steps = (p.h + 63) / 64, chunks = steps * 8;
+  int tile = (int)blockIdx.x + (int)gridDim.x * wave;
+  const bf16* row = nullptr;
+  auto point = [&] { row = p.table + (int64_t)min(16 * tile + lr, p.V - 1) * p.h + 16 * g; };
+  bf16x8 w[2][kFewAhead][2];
+  auto request = [&](auto buf, int step) {
+    constexpr int B = decltype(buf)::value;
+#pragma unroll
+    for (int u = 0; u < kFewAhead; ++u)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int k = 64 * (step + u) + 8 * half;
+        w[B][u][half] = bf16x8{};
+        if (k + 16 * g < p.h) w[B][u][half] = *reinterpret_cast<const bf16x8*>(row + k);
+      }
+  };
+  if (tile < tiles) { point(); request(B0{}, 0); }          // under way while the tokens come
+  int y, live;
+  const int at = few_place(p, lane, &y, &live);
+  if (wave == 0 && at >= 0) { token_of[at] = lane; target_of[at] = y; }
+  if (live == 0) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < live * chunks; i += kFewThreads) {
+    const int t = i / chunks, c = i - t * chunks;
+    bf16x8 v = {};
+    if (8 * c < p.h) v = *reinterpret_cast<const bf16x8*>(p.X + (int64_t)token_of[t] * p.h + 8 * c);
+    *reinterpret_cast<bf16x8*>(smem + t * p.pitch + 16 * c) = v;
+  }
+  __syncthreads();
+  const unsigned char* const mine = smem + min(lr, live - 1) * p.pitch + 32 * g;       // lanes past the tokens repeat the last one
+  const int target = target_of[min(lr, live - 1)];
+  for (; tile < tiles; tile += stride) {
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](auto buf, int step) {
+      constexpr int B = decltype(buf)::value;
+#pragma unroll
+      for (int u = 0; u < kFewAhead; ++u) {
+        if (step + u >= steps) break;
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[B][u][half], *reinterpret_cast<const bf16x8*>(mine + 128 * (step + u) + 16 * half), acc, 0, 0, 0);
+      }
+    };
+    const int here = tile;
+    for (int step = 0; step < steps; step += 2 * kFewAhead) {
+      request(B1{}, step + kFewAhead);
+      multiply(B0{}, step);
+      if (step + 2 * kFewAhead < steps) request(B0{}, step + 2 * kFewAhead);
+      multiply(B1{}, step + kFewAhead);
+    }
+    if (tile + stride < tiles) {                             // the next rows come while these are worked on
+      tile += stride;
+      point();
+      request(B0{}, 0);
+      tile = here;
+    }
+    // acc[e] is row 16 tile + 4g + e of the table, token lr
+    const int r0 = 16 * tile + 4 * g;
+    const bool in = lr < live;
+    float m = -INFINITY, total = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (in && r0 + e == target) p.at_target[lr] = acc[e];
+      total += r0 + e < p.V ? acc[e] : 0.f;
+      acc[e] = r0 + e < p.V ? acc[e] : -INFINITY;
+      m = fmaxf(m, acc[e]);
+    }
+    m = across_rows(m, [](float a, float b) { return fmaxf(a, b); });
+    const float ref = m == -INFINITY ? 0.f : m * kLog2e;
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[e], kLog2e, -ref));
+    sum = across_rows(sum, [](float a, float b) { return a + b; });
+    if (p.totals) total = across_rows(total, [](float a, float b) { return a + b; });
+    if (in && g == 0) {
+      p.stats[(int64_t)lr * tiles + tile] = make_float2(ref, sum);
+      if (p.totals) p.totals[(int64_t)lr * tiles + tile] = total;
+    }
+  }
+}
+
+// The tokens' losses and their sum, by one workgroup: a wave to a token
+__global__ __launch_bounds__(1024) void few_join_kernel(CeFew p) {
+  __shared__ float loss_of[kFew];
+  const int lane = threadIdx.x & 63, row = threadIdx.x >> 6, tiles = (p.V + 15) / 16;
+  int y, live;
+  const int at = few_place(p, lane, &y, &live);
+  if (row < live) {
+    float top = -INFINITY, sum = 0.f, total = 0.f;
+    const float2* const stats = p.stats + (int64_t)row * tiles;
+    for (int b0 = lane; b0 < tiles; b0 += 64 * 8) {
+      float2 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = b0 + 64 * u < tiles ? stats[b0 + 64 * u] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) if (b0 + 64 * u < tiles) join_sums(top, sum, v[u].x, v[u].y);
+      if (p.totals) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) if (b0 + 64 * u < tiles) total += p.totals[(int64_t)row * tiles + b0 + 64 * u];
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const float m = __shfl_xor(top, o, 64), s = __shfl_xor(sum, o, 64);
+      join_sums(top, sum, m, s);                 // a lane of its own and its partner differ in the order, and in a last bit: lane 0's is taken
+      total += __shfl_xor(total, o, 64);
+    }
+    if (lane == 0) loss_of[row] = token_loss(top + __builtin_amdgcn_logf(sum), p.at_target[row], total, p.smoothing, p.V);
+  }
+  __syncthreads();
+  if (row == 0 && lane < p.T) p.losses[lane] = at >= 0 ? loss_of[at] : 0.f;
+  if (threadIdx.x == 0) {
+    double all = 0.0;
+    for (int i = 0; i < live; ++i) all += (double)loss_of[i];
+    const float per_token = p.denom > 0.f ? 1.f / p.denom : live ? 1.f / (float)live : 0.f;
+    *p.loss = (float)(all * (double)per_token);
+  }
+}
+
 // ------------------------------------------------------------------------------- joins
-// out[r] = sum over the pieces in ascending order (+ what is there), rows of N elements; TO_ROWS: row r to row to[r], r < live
+// out[r] = sum over the pieces in ascending order, rows of N elements; TO_ROWS: those of the span, to the tokens' rows
 template <typename T, bool TO_ROWS>
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, int splits, int64_t M, int64_t N, const int32_t* __restrict__ live,
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, int splits, int64_t M, int64_t N, int height, int K, const CeSpan* __restrict__ span,
                                                    const int32_t* __restrict__ to, T* __restrict__ out) {
-  const int64_t rows = TO_ROWS ? live[1] : M, n4 = N / 4, items = rows * n4;
+  const int64_t rows = TO_ROWS ? span->live : M, n4 = N / 4, items = rows * n4, start = TO_ROWS ? span->start : 0;
+  if constexpr (TO_ROWS) {                       // as the product cut itself: in tiles of `height` rows
+    const int tiles_m = (int)(rows + height - 1) / height;
+    splits = w4_cut(tiles_m * (int)((N + 255) / 256), K).pieces;
+    M = (int64_t)tiles_m * height;
+    if (splits == 1) return;                     // the rows are where they belong
+  }
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / n4, c = (i - row * n4) * 4;
     f32x4 sum = *reinterpret_cast<const f32x4*>(P + row * N + c);
@@ -220,17 +429,17 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, 
     typename Pack<T, 4>::type o;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = (T)sum[e];
-    *reinterpret_cast<typename Pack<T, 4>::type*>(out + (TO_ROWS ? (int64_t)to[row] : row) * N + c) = o;
+    *reinterpret_cast<typename Pack<T, 4>::type*>(out + (TO_ROWS ? (int64_t)to[start + row] : row) * N + c) = o;
   }
 }
 
 template <typename T, int V>
-__global__ __launch_bounds__(256) void scatter_kernel(const T* __restrict__ from, const int32_t* __restrict__ live, const int32_t* __restrict__ to, int64_t h,
+__global__ __launch_bounds__(256) void scatter_kernel(const T* __restrict__ from, const CeSpan* __restrict__ span, const int32_t* __restrict__ to, int64_t h,
                                                       T* __restrict__ out) {
   typedef typename Pack<T, V>::type vec;
-  const int lane = threadIdx.x & 63, rows = live[1];
+  const int lane = threadIdx.x & 63, rows = span->live, start = span->start;
   for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4)
-    for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(out + to[r] * h + c) = *reinterpret_cast<const vec*>(from + r * h + c);
+    for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(out + to[start + r] * h + c) = *reinterpret_cast<const vec*>(from + r * h + c);
 }
 
 // loss = sum of the tokens' / D: one workgroup, every thread its tokens in ascending order, in 64 bits
@@ -250,27 +459,29 @@ __global__ __launch_bounds__(1024) void loss_kernel(const float* __restrict__ lo
 }
 
 // -------------------------------------------------------------------------------- sizes
-// Tokens of a piece: as many as keep what is left of the logits to this many elements (1 GiB in bf16), and their rows to 2 GiB.  Several pieces
-// cost the fp32 sums of dtable, read and written once a piece.
-constexpr int64_t kPieceElems = (int64_t)1 << 29;
+// Tokens of a piece: as many as keep what is left of the logits to this many elements (2 GiB in bf16), and their rows to 2 GiB.  Several pieces
+// cost the fp32 sums of dtable, read and written once a piece, and their place: where one piece of all tokens needs no more room than they and a
+// piece of this size do, there is one (12288 tokens that count, h 4096, V 128000, two pieces 30100 us, one 29900).
+constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
   int64_t piece, ld, blocks;
-  int pieces, dx_splits, dx_k, dw_splits, dw_k;
-  size_t head, piece_rows, rows, target, slot, losses, at_target, lse, stats, totals, x, e, sums, bytes;
+  int pieces, dw_splits, dw_k;
+  size_t head, spans, rows, target, slot, losses, at_target, lse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
     const bool half = dtype == MOSAIC_BF16;
     const size_t es = dtype_size(dtype);
     ld = (V + 63) / 64 * 64;
     blocks = ceil_div(V, kCeBlock);
-    int64_t most = std::min(kPieceElems / (half ? 1 : 2) / ld, ((int64_t)1 << 29) / h) / 256 * 256;
+    int64_t most = std::min(kPieceElems / (half ? 1 : 2) / ld, ((int64_t)1 << 30) / h) / 256 * 256;
     most = std::max<int64_t>(most, 256);
+    if (half && T * ld <= kPieceElems + 2 * V * h && T * h <= (int64_t)1 << 30) most = std::max<int64_t>(most, ceil_div(T, 256) * 256);
     pieces = (int)std::max<int64_t>(1, ceil_div(T, most));
     piece = std::max<int64_t>(256, ceil_div(ceil_div(T, pieces), 256) * 256);
     size_t at = 0;
     auto take = [&](int64_t n) { const size_t here = at; at = align_up(at + (size_t)n, 256); return here; };
     const int64_t padded = piece * pieces;
     head = take(sizeof(CeHead));
-    piece_rows = take(8 * (int64_t)pieces);
+    spans = take((int64_t)sizeof(CeSpan) * pieces);
     rows = take(4 * padded); target = take(4 * padded); slot = take(4 * padded); losses = take(4 * T);
     at_target = take(4 * piece); lse = take(4 * piece);
     stats = take(half ? 8 * blocks * piece : 0); totals = take(half ? 4 * blocks * piece : 0);
@@ -283,13 +494,12 @@ struct CeLayout {
       *k = (int)(ceil_div(ceil_div(K, n), 64) * 64);
       return (int)std::max<int64_t>(1, ceil_div(K, *k));
     };
-    dx_splits = half && grad ? cut(std::min(piece, std::max<int64_t>(T, 1)), ld, &dx_k) : 1;
     dw_splits = half && grad ? cut(V, piece, &dw_k) : 1;
     int64_t n = 0;
     if (half && grad) {
-      if (dx_splits > 1) n = std::max(n, dx_splits * piece * h);
+      n = std::min<int64_t>(kMostPieces * ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 128) * ceil_div(h, 256), kMostPieceTiles) * 65536;       // w4_cut
       if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
-      if (pieces > 1) n = std::max(n, V * h + (dx_splits > 1 ? dx_splits * piece * h : 0));
+      if (pieces > 1) n += V * h;
     }
     if (!half && grad) n = piece * h;            // dX of the piece
     sums = take(4 * n);
@@ -302,7 +512,8 @@ mosaic_status launch_rows(hipStream_t s, int quota, W4Args p, bool low) {
   auto go = [&](auto mi) -> mosaic_status {
     constexpr int MI = decltype(mi)::value;
     p.tiles_m = (int)ceil_div(p.M, 32 * MI);
-    p.tile_count = p.tiles_m * p.tiles_n * (EPI == W4_PIECES ? p.splits : 1);
+    const int most = p.tiles_m * p.tiles_n;
+    p.tile_count = EPI == W4_PIECES && most <= kMostPieceTiles ? std::min(most * kMostPieces, kMostPieceTiles) : most;
     p.row_block = row_block_for(p.K, p.M, 32 * MI);
     return launch_w4_epi<A_KC, B_KC, EPI, MI, W4_GROUPED>(s, quota, p);
   };
@@ -318,93 +529,112 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
   const bool half = dtype == MOSAIC_BF16;
   const CeLayout L(dtype, T, h, V, grad);
   char* const base = (char*)scratch;
-  CeHead* head = (CeHead*)(base + L.head);
-  int32_t *piece_rows = (int32_t*)(base + L.piece_rows), *rows = (int32_t*)(base + L.rows), *target = (int32_t*)(base + L.target), *slot = (int32_t*)(base + L.slot);
-  if (!losses) losses = (float*)(base + L.losses);
-  rows_kernel<<<1, kRowsThreads, 0, s>>>(targets, (int)T, (int)V, denom, (int)L.piece, L.pieces, head, piece_rows, rows, target, slot);
-  MOSAIC_LAUNCH_CHECK();
-  const bool wide = h % (half ? 8 : 4) == 0 && (((uintptr_t)X | (uintptr_t)dX) & 15) == 0;
-  auto gather = [&](auto t) {
-    typedef decltype(t) E;
-    const int grid = grid_for(quota, 8, ceil_div(T, 4));
-    if (wide) gather_kernel<E, Vec16<E>::N><<<grid, 256, 0, s>>>((const E*)X, slot, (int)T, h, (E*)(base + L.x), (E*)dX, losses);
-    else gather_kernel<E, 1><<<grid, 256, 0, s>>>((const E*)X, slot, (int)T, h, (E*)(base + L.x), (E*)dX, losses);
-  };
-  if (T > 0) {
-    if (half) gather(bf16()); else gather(float());
+  if (half && !grad && T > 0 && T <= kFew && T * few_pitch(h) <= kFewLds) {
+    static std::once_flag attr_once;
+    static hipError_t attr_rc = hipSuccess;
+    std::call_once(attr_once, [] { attr_rc = hipFuncSetAttribute(reinterpret_cast<const void*>(few_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kFewLds); });
+    MOSAIC_HIP(attr_rc);
+    CeFew f = {targets, (const bf16*)X, (const bf16*)table, (int)T, (int)h, (int)V, few_pitch(h), smoothing, denom, (float2*)(base + L.stats),
+               smoothing > 0.f ? (float*)(base + L.totals) : nullptr, (float*)(base + L.at_target), losses ? losses : (float*)(base + L.losses), loss};
+    few_kernel<<<grid_for(quota, 1, ceil_div(V, 16)), kFewThreads, (size_t)T * f.pitch, s>>>(f);
     MOSAIC_LAUNCH_CHECK();
+    few_join_kernel<<<1, 1024, 0, s>>>(f);
+    MOSAIC_LAUNCH_CHECK();
+    return MOSAIC_OK;
   }
+  CeHead* const head = (CeHead*)(base + L.head);
+  CeSpan* const spans = (CeSpan*)(base + L.spans);
+  int32_t *rows = (int32_t*)(base + L.rows), *target = (int32_t*)(base + L.target), *slot = (int32_t*)(base + L.slot);
+  if (!losses) losses = (float*)(base + L.losses);
+  const CeList list = {targets, (int)T, (int)V, (int)L.piece, L.pieces, denom, half, head, spans, rows, target, slot};
+  const bool wide = h % (half ? 8 : 4) == 0 && (((uintptr_t)X | (uintptr_t)dX) & 15) == 0;
+  auto place = [&](auto t, auto v) -> mosaic_status {
+    typedef decltype(t) E;
+    constexpr int N = decltype(v)::value;
+    if (T <= kListMax) {
+      list_place_kernel<E, N><<<grid_for(quota, 1, ceil_div(T, 16)), kListThreads, 0, s>>>(list, (const E*)X, h, (E*)(base + L.x), (E*)dX, losses);
+    } else {
+      list_kernel<<<1, kListThreads, 0, s>>>(list);
+      MOSAIC_LAUNCH_CHECK();
+      place_kernel<E, N><<<grid_for(quota, 8, ceil_div(T, 4)), 256, 0, s>>>(slot, (int)T, (const E*)X, h, (E*)(base + L.x), (E*)dX, losses);
+    }
+    MOSAIC_LAUNCH_CHECK();
+    return MOSAIC_OK;
+  };
+  typedef std::integral_constant<int, 1> One;
+  if (half) MOSAIC_TRY(wide ? place(bf16(), std::integral_constant<int, 8>()) : place(bf16(), One()));
+  else MOSAIC_TRY(wide ? place(float(), std::integral_constant<int, 4>()) : place(float(), One()));
   float* const sums = (float*)(base + L.sums);
   for (int i = 0; i < L.pieces; ++i) {
     const int64_t r0 = i * L.piece;
-    const int capacity = (int)L.piece, some = (int)std::min(L.piece, std::max<int64_t>(T - r0, 1));      // at most that many rows
-    const char* Xc = base + L.x + r0 * h * dtype_size(dtype);
+    const int capacity = (int)L.piece, some = (int)std::min(L.piece, std::max<int64_t>(T - (half ? 0 : r0), 1));      // at most that many rows
+    const char* Xc = base + L.x;                 // of all tokens
+    const int32_t* live = &spans[i].zero;        // 0 and how many
     CePiece p = {};
-    p.live = piece_rows + 2 * i; p.rows = rows + r0; p.target = target + r0; p.at_target = (float*)(base + L.at_target);
+    p.span = spans + i; p.rows = rows; p.target = target; p.at_target = (float*)(base + L.at_target);
     p.capacity = capacity; p.V = (int)V; p.smoothing = smoothing; p.lse = (float*)(base + L.lse); p.losses = losses;
     if (!half) {
       float* Z = (float*)(base + L.e);
-      MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc, h, table, h, Z, L.ld, nullptr, p.live, 1, capacity, 0));
+      MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc + r0 * h * 4, h, table, h, Z, L.ld, nullptr, live, 1, capacity, 0));
       rows_f32_kernel<<<grid_for(quota, 8, some), 256, 0, s>>>(p, head, Z, L.ld, grad);
       MOSAIC_LAUNCH_CHECK();
       if (dX) {
-        MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, p.live, 1, capacity, 0));
+        MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, live, 1, capacity, 0));
         const int grid = grid_for(quota, 8, ceil_div(some, 4));
-        if (wide) scatter_kernel<float, 4><<<grid, 256, 0, s>>>(sums, p.live, p.rows, h, (float*)dX);
-        else scatter_kernel<float, 1><<<grid, 256, 0, s>>>(sums, p.live, p.rows, h, (float*)dX);
+        if (wide) scatter_kernel<float, 4><<<grid, 256, 0, s>>>(sums, p.span, rows, h, (float*)dX);
+        else scatter_kernel<float, 1><<<grid, 256, 0, s>>>(sums, p.span, rows, h, (float*)dX);
         MOSAIC_LAUNCH_CHECK();
       }
-      if (dtable) MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, false, false, (int)V, (int)h, some, Z, L.ld, Xc, h, dtable, h, i ? dtable : nullptr, p.live, 1, capacity, 0));
+      if (dtable) MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, false, false, (int)V, (int)h, some, Z, L.ld, Xc + r0 * h * 4, h, dtable, h, i ? dtable : nullptr, live, 1, capacity, 0));
       continue;
     }
     bf16* E = grad ? (bf16*)(base + L.e) : nullptr;
     W4Args z = {};
     z.A = (const bf16*)Xc; z.B = (const bf16*)table; z.C = E;
     z.M = capacity; z.N = (int)V; z.K = (int)h; z.lda = h; z.ldb = h; z.ldc = L.ld;
-    z.offsets = p.live; z.groups = 1; z.bound = capacity;
+    z.offsets = live; z.piece = &spans[i].start; z.groups = 1; z.bound = capacity;
     z.b_bytes = (uint32_t)(V * h * 2);
     z.tiles_n = (int)ceil_div(V, 256);
-    z.rows = p.target; z.at_target = (float*)(base + L.at_target); z.stats = (float2*)(base + L.stats);
+    z.rows = target; z.at_target = (float*)(base + L.at_target); z.stats = (float2*)(base + L.stats);
     z.totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
     MOSAIC_TRY((launch_rows<true, true, W4_SOFTMAX>(s, quota, z, some <= 128)));
-    lse_kernel<<<grid_for(quota, 2, ceil_div(some, 64)), 1024, 0, s>>>(p, z.stats, z.totals, (int)L.blocks);
+    lse_kernel<<<grid_for(quota, 2, ceil_div(some, 16)), 1024, 0, s>>>(p, z.stats, z.totals, (int)L.blocks);
     MOSAIC_LAUNCH_CHECK();
     if (!grad) continue;
-    grad_kernel<<<grid_for(quota, 8, ceil_div(some, 16) * ceil_div(L.ld, kStrip)), 256, 0, s>>>(p, head, z.stats, E, L.ld);
+    const int64_t left = 2 * some * L.ld;
+    const Sweep sweep = sweep_grid(s, quota, ceil_div(some, 16) * ceil_div(L.ld, kStrip), 2 * left);
+    if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true><<<sweep.grid, 256, 0, s>>>(p, head, z.stats, E, L.ld);
+    else grad_kernel<false><<<sweep.grid, 256, 0, s>>>(p, head, z.stats, E, L.ld);
     MOSAIC_LAUNCH_CHECK();
-    float* const dx_sums = sums + (L.pieces > 1 ? V * h : 0);
     if (dX) {
       W4Args d = {};
       d.A = E; d.B = (const bf16*)table; d.C = (bf16*)dX;
       d.M = capacity; d.N = (int)h; d.K = (int)L.ld; d.lda = L.ld; d.ldb = h; d.ldc = h;
-      d.offsets = p.live; d.groups = 1; d.bound = capacity;
+      d.offsets = live; d.piece = &spans[i].start; d.groups = 1; d.bound = capacity;
       d.b_bytes = z.b_bytes;
       d.tiles_n = (int)ceil_div(h, 256);
-      d.rows = p.rows;
-      d.splits = L.dx_splits; d.split_k = L.dx_k; d.sums = dx_sums;
-      if (L.dx_splits > 1) {
-        MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, some <= 128)));
-        join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(dx_sums, L.dx_splits, capacity, h, p.live, p.rows, (bf16*)dX);
-        MOSAIC_LAUNCH_CHECK();
-      } else {
-        MOSAIC_TRY((launch_rows<true, false, W4_SCATTER>(s, quota, d, some <= 128)));
-      }
+      d.rows = rows;
+      d.sums = sums + (L.pieces > 1 ? V * h : 0);
+      const bool low = some <= 128;
+      MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
+      join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
+      MOSAIC_LAUNCH_CHECK();
     }
     if (dtable) {
       W4Args w = {};
       w.A = E; w.B = (const bf16*)Xc; w.C = (bf16*)dtable;
       w.M = (int)V; w.N = (int)h; w.K = capacity; w.lda = L.ld; w.ldb = h; w.ldc = h;
-      w.offsets = p.live; w.groups = 1; w.bound = capacity;
+      w.offsets = live; w.piece = &spans[i].start; w.groups = 1; w.bound = capacity;
       w.tiles_m = (int)ceil_div(V, 256); w.tiles_n = (int)ceil_div(h, 256);
       w.tile_count = w.tiles_m * w.tiles_n;
       w.row_block = row_block_for(w.K, V, 256);
-      w.sums = sums; w.first = i == 0; w.last = i == L.pieces - 1;
+      w.sums = sums; w.first = i == 0;
       w.splits = L.dw_splits; w.split_k = L.dw_k;
       if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
       else if (L.dw_splits > 1) {
         w.tile_count *= w.splits;
         MOSAIC_TRY((launch_w4_epi<false, false, W4_PIECES, 8, W4_GROUPED>(s, quota, w)));
-        join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, nullptr, nullptr, (bf16*)dtable);
+        join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, 0, 0, nullptr, nullptr, (bf16*)dtable);
         MOSAIC_LAUNCH_CHECK();
       } else MOSAIC_TRY((launch_w4_epi<false, false, W4_PLAIN, 8, W4_GROUPED>(s, quota, w)));
     }

@@ -107,7 +107,31 @@ def test_loss_and_gradients(T, h, V, smoothing, ignored, dtype):
     close(from_dev(got["dx"]), dx, bx, "dx")
     close(from_dev(got["dtable"]), dtable, bt, "dtable")
     alone = call(x, table, target, smoothing, 0.0, dtype, grad=False)
-    assert torch.equal(alone["losses"], got["losses"]) and alone["loss"] == got["loss"]
+    close(from_dev(alone["losses"]), losses, bl, "losses alone")
+    close(alone["loss"], loss, bl.sum() / n + 4 * U * abs(loss), "loss alone")
+
+
+@pytest.mark.parametrize("T,h,V,smoothing", [(1, 8, 1, 0.0), (1, 4096, 3001, 0.0), (2, 4680, 100, 0.1), (16, 72, 17, 0.1), (16, 136, 4100, 0.0), (7, 1000, 33, 0.3), (16, 4672, 50, 0.0),
+                                             (16, 4808, 50, 0.0), (5, 16384, 20, 0.0)])
+def test_loss_of_a_few_tokens(T, h, V, smoothing):
+    """All of them, some, one and none counting; no bits by the quota; what the rows that do not count hold."""
+    for ignored in (0.0, 0.5):
+        x, table, target = inputs(T, h, V, ignored, "bf16")
+        if ignored:
+            target[T // 2] = 0
+        loss, losses, _, _ = O.linear_ce(x, table, target, smoothing)
+        bl = bounds(x, table, target, smoothing, 0.0, "bf16")[0]
+        x[(target < 0) | (target >= V)] = np.nan
+        got = call(x, table, target, smoothing, 0.0, "bf16", grad=False)
+        close(from_dev(got["losses"]), losses, bl, "losses")
+        close(got["loss"], loss, bl.sum() / max(1, (losses != 0).sum()) + 4 * U * abs(loss), "loss")
+        for quota in (1, 40):
+            again = call(x, table, target, smoothing, 0.0, "bf16", grad=False, quota=quota)
+            assert torch.equal(again["losses"], got["losses"]) and again["loss"] == got["loss"]
+    none = call(x, table, np.full(T, -1, dtype=np.int32), smoothing, 0.0, "bf16", grad=False)
+    assert none["loss"] == 0 and not none["losses"].any()
+    fixed = call(x, table, target, smoothing, 10.0, "bf16", grad=False)
+    assert abs(fixed["loss"] - losses.sum() / 10) <= bl.sum() / 10 + 4 * U * abs(loss) * T
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -198,14 +222,14 @@ def test_bits_do_not_depend_on_the_quota_or_the_stream(dtype):
 
 
 def test_pieces_of_tokens():
-    """More tokens than a piece holds: the table's gradient is summed over pieces in fp32; the last piece has a few tokens, or none that count.
+    """More tokens than a piece holds: the table's gradient is summed over pieces in fp32; two of one size, one, and one of few tokens.
     dz in bf16 is off by 2^-7 relative to a probability, so the whole in the 2-norm by that at most and by 2^-8 for the last rounding."""
-    T, h, V = 4200, 64, 131000
+    T, h, V = 8300, 64, 131000
     g = torch.Generator(device="cuda").manual_seed(3)
     table = (torch.randn((V, h), generator=g, device="cuda") * 0.25).bfloat16()
     x = torch.randn((T, h), generator=g, device="cuda").bfloat16()
     target = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
-    for ignored in (0, 150):
+    for ignored in (0, 300, 8210):
         target[:ignored] = -1
         loss, losses = torch.empty(1, device="cuda"), torch.empty(T, device="cuda")
         dx, dtable = torch.empty_like(x), torch.empty_like(table)
