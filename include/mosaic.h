@@ -537,7 +537,8 @@ size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t 
  *   losses[t] = log sum_v exp(z_t[v]) - (1 - smoothing) z_t[target] - smoothing * mean_v z_t[v],      0 <= smoothing < 1,
  * losses[t] = 0 for the others (device float [T], may be NULL), and *loss (device float) = sum of the losses / D with D = denom, or, denom = 0, the number of tokens that
  * count (no such token: loss 0, gradients 0).  mosaic_op_linear_ce_grad also writes the gradients of *loss: dX [T,h] and dtable [V,h] (overwritten; one of
- * them may be NULL).  Logits are fp32; bf16: the probabilities that the gradients are formed of are bf16, rounded twice relative to themselves.  What lies between is kept in
+ * them may be NULL).  Logits are fp32; bf16: the logits' gradient is rounded to bf16 before the products that dX and dtable are (formed of probabilities kept in fp16 relative to the
+ * largest of 64).  What lies between is kept in
  * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
  * it holds the logits' exponentials for as many tokens at a time as 2^30 of them (2 GiB in bf16) belong to.  bf16: h a multiple of 8 and all tensors 16-byte aligned
  * (MOSAIC_EUNSUPPORTED otherwise); the table is smaller than 4 GiB. */

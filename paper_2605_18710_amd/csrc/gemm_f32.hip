@@ -523,6 +523,7 @@ struct F32Groups {
   const int32_t* offsets;
   int groups, bound;
   int64_t stride;            // elements between two groups' B, or C
+  int splits, split_k;       // K-contiguous A, one group: the contraction in pieces of split_k, each with a C of its own, M rows
 };
 constexpr int kGroupsAtOnce = 256;       // of which the first tiles are kept in LDS, a thread each
 template <typename T, int BT, int KS, bool A_KC, bool B_KC, bool VEC>
@@ -554,10 +555,12 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
     if (tid < ng) starts[tid] = scan - mine;
     if (tid == 255) starts[ng] = scan;             // threads without a group add nothing
     __syncthreads();
-    const int all = starts[ng];
+    const int all = starts[ng] * gr.splits;
     int64_t item = before % gridDim.x;             // the list goes on where the batch before left it
     item = ((int64_t)blockIdx.x - item + gridDim.x) % gridDim.x;
-    for (; item < all; item += gridDim.x) {
+    for (int64_t listed = item; listed < all; listed += gridDim.x) {
+      const int piece = gr.splits > 1 ? (int)listed / starts[ng] : 0;
+      item = listed - (int64_t)piece * starts[ng];
       int a = 0, b = ng;                           // the last group that starts at or before the tile
       while (b - a > 1) { const int mid = (a + b) >> 1; if (starts[mid] <= item) a = mid; else b = mid; }
       const int first = min(max(gr.offsets[g0 + a], 0), gr.bound);
@@ -569,6 +572,13 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
         q.C = (T*)p.C + (int64_t)first * p.ldc;
         q.M = rows;
         q.tiles_m = (rows + BT - 1) / BT;
+        if (gr.splits > 1) {
+          const int k0 = piece * gr.split_k;
+          q.A = (const T*)q.A + (int64_t)k0;
+          q.B = (const T*)q.B + (B_KC ? (int64_t)k0 : (int64_t)k0 * p.ldb);
+          q.C = (T*)q.C + (int64_t)piece * p.M * p.ldc;
+          q.K = min(gr.split_k, p.K - k0);
+        }
       } else {
         q.B = (const T*)p.B + (int64_t)first * p.ldb;
         q.C = (T*)p.C + (g0 + a) * gr.stride;
@@ -585,7 +595,7 @@ template <typename T, bool A_KC, bool B_KC, bool VEC>
 mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
   const bool large = large_tiles(p.M, p.N);
   const int bt = large ? 64 : 32;
-  const int64_t tm = ceil_div(p.M, bt), tn = ceil_div(p.N, bt), most = A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups;
+  const int64_t tm = ceil_div(p.M, bt), tn = ceil_div(p.N, bt), most = (A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups) * gr.splits;
   if (most > INT32_MAX / 2) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "too many output tiles");
   p.tiles_m = (int)tm; p.tiles_n = (int)tn;
   const int grid = grid_for(quota, 4, most);
@@ -610,12 +620,13 @@ mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const 
 }  // namespace
 
 // M: rows of A for all groups together, the most that there can be (a K-strided A: of each C).  K: the contraction (a K-strided A: the longest).
+// splits > 1 (one group, K-contiguous A, fp32): the contraction in pieces of split_k, C [splits, M, ldc]
 mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
-                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride) {
+                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k, int splits) {
   if (M == 0 || N == 0 || groups == 0) return MOSAIC_OK;
   F32Gemm p = {};
   p.A = A; p.B = B; p.C = C; p.R = R; p.M = M; p.N = N; p.K = K; p.lda = lda; p.ldb = ldb; p.ldc = ldc;
-  const F32Groups gr = {offsets, groups, bound, stride};
+  const F32Groups gr = {offsets, groups, bound, stride, splits, split_k};
   auto go = [&](auto t) {
     typedef decltype(t) T;
     const uintptr_t mask = 4 * sizeof(T) - 1;

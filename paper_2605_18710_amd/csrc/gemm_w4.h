@@ -115,6 +115,7 @@ struct W4Args {
   int splits, split_k;             // W4_PIECES, K-strided A: the contraction in `splits` pieces of split_k k-values, whole K-tiles
   const int32_t* rows;             // W4_PIECES, K-contiguous A: where a row of the product goes in C.  W4_SOFTMAX: its target, a column or -1
   float* sums;                     // W4_PIECES: [pieces][rows][N], rows M, or those of the tiles that there are; W4_ADD: what is there already, [M][N]
+  const float* scale;              // null, or on the device: a factor of the sums that leave for C
   int first;                       // W4_ADD: nothing is there yet
   const int32_t* piece;            // null, or [2], on the device: a row that the operands of all rows are counted from (A: W4_SOFTMAX, B: K-strided A, and
                                    // `rows`), and (W4_ADD) whether the sum is complete with this launch and goes to C
@@ -260,9 +261,9 @@ struct W4GroupTiles {
 
 // W4_SOFTMAX: the product is a tile of logits.  What leaves is, for each row and block of kCeBlock columns, the largest logit m and the sum of
 // exp(z - m): stats[block][row], p.M rows; the sum of the logits where totals is given; the logit of the row's target; and, where C is given,
-// exp(z - m) rounded to bf16 (0 past the last column, up to ldc).
-// Rounded relative to its block's maximum a probability keeps bf16's 2^-9 relative to itself whatever the logits' size; the logits in bf16 would
-// be off by 2^-9 of theirs, which the exponential turns into that much of a probability times the logit.
+// exp(z - m) rounded to fp16 (0 past the last column, up to ldc).
+// From 0 to 1, relative to its block's largest: an fp16 number is within 2^-11 of it relative to itself, or within 2^-25 of the largest.  The logits
+// themselves in 16 bits would be off by that share of the logit, which the exponential turns into that much of a probability times the logit.
 // A block whose largest logit is -infinity counts from 0: its sum is 0.  NaN and +infinity make the sum NaN.  m is kept times log2 e.
 // Here for one row of a block, a lane's sixteen values v[j][e], columns col + 16j + 4g + e; the four lanes of a row lie 16 apart (g = 0 .. 3).
 constexpr int kCeBlock = 64;
@@ -358,6 +359,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
     tq.tail_per = (tq.n_items - tq.n_full + 7) / 8;
   }
   const int start = GROUPED && p.piece ? __builtin_amdgcn_readfirstlane(p.piece[0]) : 0;
+  const float scale = GROUPED && p.scale ? *p.scale : 1.f;
   const bool last = EPI == W4_ADD && p.piece && __builtin_amdgcn_readfirstlane(p.piece[1]);
   if (EPI == W4_ADD && !p.first && !last && p.offsets[1] <= p.offsets[0]) { tq.n_items = tq.n_full = tq.tail_per = 0; }      // nothing to add
   auto decode = [&](int item) -> Item {
@@ -646,10 +648,12 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
           } else if (EPI != W4_SOFTMAX || p.C) {
 #pragma unroll
             for (int jj = 0; jj < 4; ++jj) {
-              bf16x4 o;
+              typedef typename std::conditional<EPI == W4_SOFTMAX, _Float16, bf16>::type E;
+              typedef __attribute__((ext_vector_type(4))) E vec4;
+              vec4 o;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[e] = (bf16)v[jj][e];
-              *reinterpret_cast<bf16x4*>(half + 2048 * (b & 1) + elr * 128 + (((2 * jj + (eg >> 1)) ^ (elr & 7)) << 4) + 8 * (eg & 1)) = o;
+              for (int e = 0; e < 4; ++e) o[e] = (E)(EPI == W4_SOFTMAX ? v[jj][e] : v[jj][e] * scale);
+              *reinterpret_cast<vec4*>(half + 2048 * (b & 1) + elr * 128 + (((2 * jj + (eg >> 1)) ^ (elr & 7)) << 4) + 8 * (eg & 1)) = o;
             }
             patch_sync();
 #pragma unroll
@@ -720,7 +724,7 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
               const float4 x = before[b & 1][q][0], y = before[b & 1][q][1];
               const float old[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
-              for (int e = 0; e < 8; ++e) v[e] += old[e];
+              for (int e = 0; e < 8; ++e) v[e] = (v[e] + old[e]) * (last ? scale : 1.f);
               if (!last) {
                 if (float4* at = sum_at(b, q)) {
                   at[0] = make_float4(v[0], v[1], v[2], v[3]);

@@ -6,7 +6,7 @@
 //
 //   1. The tokens that count are listed in order, and their rows copied side by side (list_kernel, place_kernel): how many there are
 //      stays on the device, where the products' workgroups read it.
-//   2. In pieces of tokens (kPieceElems): the product with the table, whose epilogue leaves exp(z - m) in bf16 and, for each row and 64 columns, the
+//   2. In pieces of tokens (kPieceElems): the product with the table, whose epilogue leaves exp(z - m) in fp16 and, for each row and 64 columns, the
 //      largest logit m and the sum (w4_softmax in gemm_w4.h); or only these, when the loss alone is asked for.
 //   3. lse_kernel joins a row's blocks to the logarithm of the sum and the loss; grad_kernel turns what lies there into dz, in place.
 //   4. dX = dz table, into the rows of X that the tokens came from; dtable = dz^T X, summed in fp32 over the pieces.
@@ -19,7 +19,7 @@
 #include "kernels.h"
 
 mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
-                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride);
+                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k = 0, int splits = 1);
 
 namespace {
 
@@ -182,24 +182,26 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
   }
 }
 
-// exp(z - m) -> dz, in place: a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
+// exp(z - m) in fp16 -> D dz in bf16, in place (the products' results are divided by D: a target of small probability, the largest term of its row, is then
+// -1 and not rounded at all): a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
 constexpr int kStrip = 1024;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 template <bool PAST>
-__global__ __launch_bounds__(256) void grad_kernel(CePiece p, const CeHead* __restrict__ head, const float2* __restrict__ stats, bf16* __restrict__ E, int64_t ld) {
+__global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __restrict__ stats, bf16* __restrict__ E, int64_t ld) {
   const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
-  const float g = head->per_token, even = p.smoothing / (float)p.V;
+  const float even = p.smoothing / (float)p.V;
   const int64_t items = (int64_t)((live + 15) / 16) * strips;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int r0 = (int)(item / strips) * 16, c0 = (int)(item % strips) * kStrip;
     const int col = c0 + 8 * (threadIdx.x & 127);
-    Vec16<bf16> v[8];
+    f16x8 v[8];
     float scale[8], lse[8];
     int hit[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
-      v[i].load<PAST>(E + (int64_t)row * ld + col);
+      v[i] = load_from<PAST>(reinterpret_cast<const f16x8*>(E + (int64_t)row * ld + col));
       lse[i] = p.lse[row];
       scale[i] = stats[(int64_t)(col / kCeBlock) * p.capacity + row].x;
       hit[i] = p.target[start + row] - col;
@@ -209,15 +211,16 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const CeHead* __re
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
       const float f = __builtin_amdgcn_exp2f(scale[i] - lse[i]);
+      Vec16<bf16> o;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i].set(e, col + e < p.V ? (v[i].get(e) * f - even) * g : 0.f);
+      for (int e = 0; e < 8; ++e) o.set(e, col + e < p.V ? (float)v[i][e] * f - even : 0.f);
       if (hit[i] >= 0 && hit[i] < 8) {
         // the target's probability from its own logit: 1 - p keeps its digits where p is near 1
-        const float d = ((__builtin_amdgcn_exp2f(fmaf(p.at_target[row], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even)) * g;
+        const float d = (__builtin_amdgcn_exp2f(fmaf(p.at_target[row], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (e == hit[i]) v[i].set(e, d);
+        for (int e = 0; e < 8; ++e) if (e == hit[i]) o.set(e, d);
       }
-      v[i].store<PAST>(E + (int64_t)row * ld + col);
+      o.store<PAST>(E + (int64_t)row * ld + col);
     }
   }
 }
@@ -412,34 +415,27 @@ __global__ __launch_bounds__(1024) void few_join_kernel(CeFew p) {
 
 // ------------------------------------------------------------------------------- joins
 // out[r] = sum over the pieces in ascending order, rows of N elements; TO_ROWS: those of the span, to the tokens' rows
-template <typename T, bool TO_ROWS>
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, int splits, int64_t M, int64_t N, int height, int K, const CeSpan* __restrict__ span,
+template <typename T, bool TO_ROWS, int V = 4>
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, int splits, int64_t M, int64_t N, const float* __restrict__ scale, int height, int K, const CeSpan* __restrict__ span,
                                                    const int32_t* __restrict__ to, T* __restrict__ out) {
-  const int64_t rows = TO_ROWS ? span->live : M, n4 = N / 4, items = rows * n4, start = TO_ROWS ? span->start : 0;
-  if constexpr (TO_ROWS) {                       // as the product cut itself: in tiles of `height` rows
+  const int64_t rows = TO_ROWS ? span->live : M, pieces = N / V, items = rows * pieces, start = TO_ROWS ? span->start : 0;
+  if (TO_ROWS && height) {                       // as the product cut itself: in tiles of `height` rows
     const int tiles_m = (int)(rows + height - 1) / height;
     splits = w4_cut(tiles_m * (int)((N + 255) / 256), K).pieces;
     M = (int64_t)tiles_m * height;
     if (splits == 1) return;                     // the rows are where they belong
   }
+  typedef typename Pack<float, V>::type vec;
+  const float factor = scale ? *scale : 1.f;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / n4, c = (i - row * n4) * 4;
-    f32x4 sum = *reinterpret_cast<const f32x4*>(P + row * N + c);
-    for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(P + (s * M + row) * N + c);
-    typename Pack<T, 4>::type o;
+    const int64_t row = i / pieces, c = (i - row * pieces) * V;
+    vec sum = *reinterpret_cast<const vec*>(P + row * N + c);
+    for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const vec*>(P + (s * M + row) * N + c);
+    typename Pack<T, V>::type o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (T)sum[e];
-    *reinterpret_cast<typename Pack<T, 4>::type*>(out + (TO_ROWS ? (int64_t)to[start + row] : row) * N + c) = o;
+    for (int e = 0; e < V; ++e) pack_set<T, V>(o, e, pack_get<float, V>(sum, e) * factor);
+    *reinterpret_cast<typename Pack<T, V>::type*>(out + (TO_ROWS ? (int64_t)to[start + row] : row) * N + c) = o;
   }
-}
-
-template <typename T, int V>
-__global__ __launch_bounds__(256) void scatter_kernel(const T* __restrict__ from, const CeSpan* __restrict__ span, const int32_t* __restrict__ to, int64_t h,
-                                                      T* __restrict__ out) {
-  typedef typename Pack<T, V>::type vec;
-  const int lane = threadIdx.x & 63, rows = span->live, start = span->start;
-  for (int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); r < rows; r += (int64_t)gridDim.x * 4)
-    for (int64_t c = lane * V; c < h; c += 64 * V) *reinterpret_cast<vec*>(out + to[start + r] * h + c) = *reinterpret_cast<const vec*>(from + r * h + c);
 }
 
 // loss = sum of the tokens' / D: one workgroup, every thread its tokens in ascending order, in 64 bits
@@ -465,7 +461,7 @@ __global__ __launch_bounds__(1024) void loss_kernel(const float* __restrict__ lo
 constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
   int64_t piece, ld, blocks;
-  int pieces, dw_splits, dw_k;
+  int pieces, dw_splits, dw_k, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
   size_t head, spans, rows, target, slot, losses, at_target, lse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
     const bool half = dtype == MOSAIC_BF16;
@@ -501,7 +497,13 @@ struct CeLayout {
       if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
       if (pieces > 1) n += V * h;
     }
-    if (!half && grad) n = piece * h;            // dX of the piece
+    dx_splits = 1;
+    if (!half && grad) {                         // dX of the piece: tiles of 32 x 32, four workgroups to a CU, no less than 256 k-values
+      const int64_t tiles = ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 32) * ceil_div(h, 32), most = std::max<int64_t>(1, std::min(1024 / tiles, V / 256));
+      dx_k = (int)(ceil_div(ceil_div(V, most), 64) * 64);
+      dx_splits = (int)ceil_div(V, dx_k);
+      n = dx_splits * piece * h;
+    }
     sums = take(4 * n);
     bytes = at;
   }
@@ -579,10 +581,10 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       rows_f32_kernel<<<grid_for(quota, 8, some), 256, 0, s>>>(p, head, Z, L.ld, grad);
       MOSAIC_LAUNCH_CHECK();
       if (dX) {
-        MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, live, 1, capacity, 0));
-        const int grid = grid_for(quota, 8, ceil_div(some, 4));
-        if (wide) scatter_kernel<float, 4><<<grid, 256, 0, s>>>(sums, p.span, rows, h, (float*)dX);
-        else scatter_kernel<float, 1><<<grid, 256, 0, s>>>(sums, p.span, rows, h, (float*)dX);
+        MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, live, 1, capacity, 0, L.dx_k, L.dx_splits));
+        const int64_t words = some * h;
+        if (wide) join_kernel<float, true, 4><<<grid_for(quota, 8, ceil_div(words, 1024)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX);
+        else join_kernel<float, true, 1><<<grid_for(quota, 8, ceil_div(words, 256)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX);
         MOSAIC_LAUNCH_CHECK();
       }
       if (dtable) MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, false, false, (int)V, (int)h, some, Z, L.ld, Xc + r0 * h * 4, h, dtable, h, i ? dtable : nullptr, live, 1, capacity, 0));
@@ -603,8 +605,8 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     if (!grad) continue;
     const int64_t left = 2 * some * L.ld;
     const Sweep sweep = sweep_grid(s, quota, ceil_div(some, 16) * ceil_div(L.ld, kStrip), 2 * left);
-    if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true><<<sweep.grid, 256, 0, s>>>(p, head, z.stats, E, L.ld);
-    else grad_kernel<false><<<sweep.grid, 256, 0, s>>>(p, head, z.stats, E, L.ld);
+    if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true><<<sweep.grid, 256, 0, s>>>(p, z.stats, E, L.ld);
+    else grad_kernel<false><<<sweep.grid, 256, 0, s>>>(p, z.stats, E, L.ld);
     MOSAIC_LAUNCH_CHECK();
     if (dX) {
       W4Args d = {};
@@ -614,10 +616,11 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.b_bytes = z.b_bytes;
       d.tiles_n = (int)ceil_div(h, 256);
       d.rows = rows;
+      d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
       const bool low = some <= 128;
       MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
-      join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
+      join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
       MOSAIC_LAUNCH_CHECK();
     }
     if (dtable) {
@@ -628,13 +631,13 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       w.tiles_m = (int)ceil_div(V, 256); w.tiles_n = (int)ceil_div(h, 256);
       w.tile_count = w.tiles_m * w.tiles_n;
       w.row_block = row_block_for(w.K, V, 256);
-      w.sums = sums; w.first = i == 0;
+      w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
       w.splits = L.dw_splits; w.split_k = L.dw_k;
       if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
       else if (L.dw_splits > 1) {
         w.tile_count *= w.splits;
         MOSAIC_TRY((launch_w4_epi<false, false, W4_PIECES, 8, W4_GROUPED>(s, quota, w)));
-        join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, 0, 0, nullptr, nullptr, (bf16*)dtable);
+        join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, w.scale, 0, 0, nullptr, nullptr, (bf16*)dtable);
         MOSAIC_LAUNCH_CHECK();
       } else MOSAIC_TRY((launch_w4_epi<false, false, W4_PLAIN, 8, W4_GROUPED>(s, quota, w)));
     }

@@ -2,8 +2,8 @@
 
 Bounds, element by element.  u = 2^-24: a logit is a sum of h products in fp32, off by (h + 2) u sum |x w| at most (E).  The exponential and its
 argument, the sums of a block, of the blocks and their joining add (64 + V / 512) 2 u to a sum relative to itself, the
-logarithm and its factor 4 u |lse|.  bf16: a probability is rounded twice, by 2^-8 each, before the products; these
-are sums of V (rows) or T (table) terms in fp32 and are rounded once, by 2^-8."""
+logarithm and its factor 4 u |lse|.  bf16: a probability is kept in fp16 relative to the largest of its block (2^-11 of itself, or 2^-25 of that one), and
+the logits' gradient rounded, by 2^-8, before the products; these are sums of V (rows) or T (table) terms in fp32 and are rounded once, by 2^-8."""
 import numpy as np
 import pytest
 import torch
@@ -45,9 +45,9 @@ def bounds(x, table, target, smoothing, denom, dtype):
     one = np.zeros(z.shape)
     one[np.arange(len(at)), target[at]] = 1.0
     dz = np.abs(p - (1 - smoothing) * one - smoothing / V) / D
-    store = 2.0 ** -8 if dtype == "bf16" else 0.0
+    store, kept = (2.0 ** -8, 2.0 ** -11) if dtype == "bf16" else (0.0, 0.0)
     # the target's own term is formed from its fp32 logit and rounded once
-    off = (rel[:, None] + 4 * U + store * (1 - one)) * p / D * (1 + store) + store * dz + 4 * U * (smoothing + one) / D
+    off = ((rel[:, None] + 4 * U + kept * (1 - one)) * p + kept * 2.0 ** -14 * p.max(1, initial=0.0, keepdims=True)) / D * (1 + store) + store * dz + 4 * U * (smoothing + one) / D
     last = 2.0 ** -8 if dtype == "bf16" else U
     dx, dtable = np.zeros(x.shape), None
     full = off + (V + 2) * U * (dz + off)
