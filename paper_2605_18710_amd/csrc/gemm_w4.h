@@ -3,6 +3,7 @@
 #include "activations.h"
 #include "common.h"
 #include "tile_queue.h"
+#include <algorithm>
 #include <mutex>
 #include <type_traits>
 
@@ -135,16 +136,16 @@ constexpr int kMaxGroups = 1024;
 // for).  Microseconds: 1.45 for 64 k-values of a tile, 8 around them; the pass that adds the pieces at 5 TB/s behind 5.  dz table for 4096, 1280 of 51001: 30 tiles,
 // one round however long; 6144 x 4096 of 128000: 384 tiles, 5600 us in two rounds, 4400 as three rounds of half the length.
 constexpr int kMostPieces = 16, kMostPieceTiles = 2048;
-struct W4Cut { int pieces, k; };
+struct W4Cut { int pieces, k; float us; };
 __device__ __host__ __forceinline__ W4Cut w4_cut(int tiles, int K) {
-  W4Cut best = {1, (K + 63) / 64 * 64};
-  float least = (float)((tiles + 255) / 256) * ((float)(best.k / 64) * 1.45f + 8.f);
+  W4Cut best = {1, (K + 63) / 64 * 64, 0.f};
+  best.us = (float)((tiles + 255) / 256) * ((float)(best.k / 64) * 1.45f + 8.f);
   for (int n = 2; n <= kMostPieces && n * tiles <= kMostPieceTiles; ++n) {
     const int k = ((K + n - 1) / n + 63) / 64 * 64;
     if (k < 1024) break;
     const int pieces = (K + k - 1) / k;
     const float us = (float)((tiles * pieces + 255) / 256) * ((float)(k / 64) * 1.45f + 8.f) + (float)tiles * (float)(4 * pieces + 2) * 0.0131f + 5.f;
-    if (us < least) { least = us; best = {pieces, k}; }
+    if (us < best.us) best = {pieces, k, us};
   }
   return best;
 }

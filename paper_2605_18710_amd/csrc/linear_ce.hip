@@ -14,6 +14,7 @@
 // row.  fp32: the same on fp32 logits, whose rows one workgroup normalises (rows_f32_kernel).
 //
 // All sums have an order that the sizes and the targets fix.
+#include "gemm_few.h"
 #include "gemm_plan.h"
 #include "gemm_w4.h"
 #include "kernels.h"
@@ -23,6 +24,7 @@ mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc,
 
 namespace {
 
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
 
 // ------------------------------------------------------------------------- the tokens that count
@@ -115,7 +117,8 @@ struct CePiece {
   const float* at_target;
   int capacity, V;
   float smoothing;
-  float* lse;                  // of each row, to the base of 2
+  float* lse;                  // of each row, to the base of 2; where `inverse` is given, what the sum's exponentials are relative to, and 1 / the sum
+  float* inverse;
   float* losses;
 };
 
@@ -176,7 +179,8 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
     row_sums(stats, totals, blocks, p.capacity, row, {top_of, sum_of, total_of}, top, sum, total);
     if (threadIdx.x < 16 && row < live) {
       const float lse = top + __builtin_amdgcn_logf(sum);      // to the base of 2
-      p.lse[row] = lse;
+      p.lse[row] = p.inverse ? top : lse;
+      if (p.inverse) p.inverse[row] = 1.f / sum;
       p.losses[p.rows[start + row]] = token_loss(lse, p.at_target[row], total, p.smoothing, p.V);
     }
   }
@@ -185,9 +189,10 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
 // exp(z - m) in fp16 -> D dz in bf16, in place (the products' results are divided by D: a target of small probability, the largest term of its row, is then
 // -1 and not rounded at all): a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
 constexpr int kStrip = 1024;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-template <bool PAST>
-__global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __restrict__ stats, bf16* __restrict__ E, int64_t ld) {
+template <bool PAST, bool JOIN>
+__global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld) {
+  // JOIN: every workgroup joins its rows' blocks itself, of which there are at most kJoinBlocks, and no launch does before
+  __shared__ float top_of[4][16], sum_of[4][16], total_of[4][16], lse_of[16];
   const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
   const float even = p.smoothing / (float)p.V;
   const int64_t items = (int64_t)((live + 15) / 16) * strips;
@@ -202,9 +207,37 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __re
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
       v[i] = load_from<PAST>(reinterpret_cast<const f16x8*>(E + (int64_t)row * ld + col));
-      lse[i] = p.lse[row];
+      if constexpr (!JOIN) lse[i] = p.lse[row];
       scale[i] = stats[(int64_t)(col / kCeBlock) * p.capacity + row].x;
       hit[i] = p.target[start + row] - col;
+    }
+    if constexpr (JOIN) {
+      const int r = threadIdx.x & 15, wave = threadIdx.x >> 6, row = r0 + r, blocks = (p.V + kCeBlock - 1) / kCeBlock;
+      float top = -INFINITY, sum = 0.f, total = 0.f;
+      for (int b = threadIdx.x >> 4; b < blocks; b += 16) {
+        const float2 x = stats[(int64_t)b * p.capacity + row];
+        join_sums(top, sum, x.x, x.y);
+        if (totals) total += totals[(int64_t)b * p.capacity + row];
+      }
+#pragma unroll
+      for (int o = 16; o < 64; o <<= 1) {
+        const float m = __shfl_xor(top, o, 64), s = __shfl_xor(sum, o, 64);
+        join_sums(top, sum, m, s);
+        total += __shfl_xor(total, o, 64);
+      }
+      if ((threadIdx.x & 63) < 16) { top_of[wave][r] = top; sum_of[wave][r] = sum; total_of[wave][r] = total; }
+      __syncthreads();
+      if (threadIdx.x < 16) {
+#pragma unroll
+        for (int w = 1; w < 4; ++w) { join_sums(top, sum, top_of[w][r], sum_of[w][r]); total += total_of[w][r]; }
+        const float all = top + __builtin_amdgcn_logf(sum);
+        lse_of[r] = all;
+        if (c0 == 0 && row < live) p.losses[p.rows[start + row]] = token_loss(all, p.at_target[row], total, p.smoothing, p.V);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) lse[i] = lse_of[2 * i + (threadIdx.x >> 7)];
+      __syncthreads();                           // read before the next strip's rows are joined
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -224,6 +257,7 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __re
     }
   }
 }
+constexpr int kJoinBlocks = 64;                    // 16 rows' statistics are then no more than a quarter of what a strip reads
 
 __device__ __forceinline__ float block_reduce(float x, bool max, float* lds) {
   x = max ? wave_max(x) : wave_sum(x);
@@ -233,7 +267,8 @@ __device__ __forceinline__ float block_reduce(float x, bool max, float* lds) {
   return max ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// fp32 logits, a workgroup per row: loss and (Z written) dz in place
+// fp32 logits, a workgroup to a row of up to 256 PER of them, which it holds: loss and (grad) dz in place
+template <int PER>
 __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, int grad) {
   __shared__ float lds[4];
   const int live = p.span->live, start = p.span->start;
@@ -241,26 +276,188 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* 
   for (int row = blockIdx.x; row < live; row += gridDim.x) {
     float* z = Z + row * ld;
     const int target = p.target[start + row];
-    float top = -INFINITY, total = 0.f;
-    for (int c = threadIdx.x; c < p.V; c += 256) { top = fmaxf(top, z[c]); total += z[c]; }
-    top = block_reduce(top, true, lds);
-    total = block_reduce(total, false, lds);
-    float sum = 0.f;
-    for (int c = threadIdx.x; c < p.V; c += 256) sum += expf(z[c] - top);
-    sum = block_reduce(sum, false, lds);
-    const float lse = top + logf(sum);
-    if (threadIdx.x == 0) {
-      float loss = lse - (1.f - p.smoothing) * z[target];
-      if (p.smoothing > 0.f) loss -= p.smoothing * (total / (float)p.V);
-      p.losses[p.rows[start + row]] = loss;
+    float v[PER], top = -INFINITY, total = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = threadIdx.x + 256 * i;
+      v[i] = c < p.V ? z[c] : -INFINITY;
+      top = fmaxf(top, v[i]);
+      total += c < p.V ? v[i] : 0.f;
     }
+    top = block_reduce(top, true, lds);
+    if (p.smoothing > 0.f) total = block_reduce(total, false, lds);
+    const float ref = top == -INFINITY ? 0.f : top;
+    const float at_target = z[target];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      v[i] = expf(v[i] - ref);
+      sum += v[i];
+    }
+    sum = block_reduce(sum, false, lds);         // behind its barriers the target's logit has been read
+    if (threadIdx.x == 0) p.losses[p.rows[start + row]] = token_loss((ref + logf(sum)) / kLn2, at_target, total, p.smoothing, p.V);
     if (!grad) continue;
-    __syncthreads();                             // the target's logit has been read
-    for (int c = threadIdx.x; c < p.V; c += 256) {
-      const float q = expf(z[c] - lse);
-      z[c] = g * (c == target ? (q - 1.f) + (p.smoothing - even) : q - even);
+    const float inverse = 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int c = threadIdx.x + 256 * i;
+      if (c < p.V) z[c] = g * (c == target ? (v[i] * inverse - 1.f) + (p.smoothing - even) : v[i] * inverse - even);
     }
   }
+}
+// Longer rows: (m, sum) of blocks of kWideBlock columns, joined by lse_kernel, and dz in place, a workgroup to a block
+constexpr int kWideBlock = 4096;
+template <bool GRAD>
+__global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, float2* __restrict__ stats,
+                                                       float* __restrict__ totals, float* __restrict__ at_target) {
+  __shared__ float lds[4];
+  constexpr int PER = kWideBlock / 1024;
+  const int live = p.span->live, start = p.span->start, blocks = (p.V + kWideBlock - 1) / kWideBlock;
+  const float g = GRAD ? head->per_token : 0.f, even = p.smoothing / (float)p.V;
+  for (int64_t item = blockIdx.x; item < (int64_t)live * blocks; item += gridDim.x) {
+    const int row = (int)(item / blocks), block = (int)(item - (int64_t)row * blocks), c0 = block * kWideBlock + 4 * threadIdx.x;
+    float* const z = Z + row * ld + c0;          // rows of whole 16-byte pieces
+    const int target = p.target[start + row] - c0;
+    f32x4 v[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      v[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (c0 + 1024 * i < p.V) v[i] = *reinterpret_cast<const f32x4*>(z + 1024 * i);
+    }
+    const float base = GRAD ? p.lse[row] : 0.f, inverse = GRAD ? p.inverse[row] : 0.f;
+    float top = -INFINITY, total = 0.f, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 1024 * i + e;
+        if (GRAD) {
+          const float q = __builtin_amdgcn_exp2f(fmaf(v[i][e], kLog2e, -base)) * inverse;
+          v[i][e] = g * (c == target ? (q - 1.f) + (p.smoothing - even) : q - even);
+        } else {
+          if (c0 + c >= p.V) v[i][e] = -INFINITY;
+          else total += v[i][e];
+          if (c == target) at_target[row] = v[i][e];
+          top = fmaxf(top, v[i][e]);
+        }
+      }
+      if (GRAD && c0 + 1024 * i < p.V) *reinterpret_cast<f32x4*>(z + 1024 * i) = v[i];       // past the row's end there is room up to ld
+    }
+    if constexpr (!GRAD) {
+      top = block_reduce(top, true, lds);
+      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(v[i][e], kLog2e, -ref));
+      sum = block_reduce(sum, false, lds);
+      if (totals) total = block_reduce(total, false, lds);
+      if (threadIdx.x == 0) {
+        stats[(int64_t)block * p.capacity + row] = make_float2(ref, sum);
+        if (totals) totals[(int64_t)block * p.capacity + row] = total;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------- the products by few_tile
+// What the four-wave kernel makes of the same arguments (W4_SOFTMAX; dX to the tokens' rows; dtable), for few tokens, short rows or small tables.
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppMirror8 = 0x141;      // the last one gives the other four lanes' where all four have the same
+template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
+template <typename F> __device__ __forceinline__ float across_eight(float x, F f) {
+  x = f(x, dpp<kDppXor1>(x));
+  x = f(x, dpp<kDppXor2>(x));
+  return f(x, dpp<kDppMirror8>(x));
+}
+template <int RB>
+__global__ __launch_bounds__(kFewNT) void few_logits_kernel(W4Args p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  auto add = [](float a, float b) { return a + b; };
+  auto high = [](float a, float b) { return fmaxf(a, b); };
+  const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
+  const int64_t items = (int64_t)tiles_m * ((p.N + 63) / 64);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int n0 = (int)(item / tiles_m) * 64, m0 = (int)(item % tiles_m) * 16 * RB;
+    few_tile<true, true, RB>(p.A + (int64_t)start * p.lda, p.lda, m0, live, p.B, p.ldb, n0, p.N, p.K, smem, [&](int row, int col, float (&v)[8]) {
+      const bool in = row < live, first = in && (threadIdx.x & 7) == 0;
+      const int hit = (in ? p.rows[start + row] : -1) - col;
+      const int64_t slot = (int64_t)(col / kCeBlock) * p.M + row;
+      float total = 0.f, m = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e == hit) p.at_target[row] = v[e];
+        total += v[e];                           // rows of the table past its end count as zeros
+        v[e] = col + e < p.N ? v[e] : -INFINITY;
+        m = fmaxf(m, v[e]);
+      }
+      if (p.totals) {
+        total = across_eight(total, add);
+        if (first) p.totals[slot] = total;
+      }
+      m = across_eight(m, high);
+      const float ref = m == -INFINITY ? 0.f : m * kLog2e;
+      f16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, -ref));
+        sum += x;
+        o[e] = (_Float16)x;
+      }
+      sum = across_eight(sum, add);
+      if (first) p.stats[slot] = make_float2(ref, sum);
+      if (p.C && in && col < p.ldc) *reinterpret_cast<f16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
+    });
+  }
+}
+template <int RB>
+__global__ __launch_bounds__(kFewNT) void few_dx_kernel(W4Args p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
+  const float scale = *p.scale;
+  const int64_t items = (int64_t)tiles_m * ((p.N + 63) / 64);
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int n0 = (int)(item / tiles_m) * 64, m0 = (int)(item % tiles_m) * 16 * RB;
+    few_tile<true, false, RB>(p.A, p.lda, m0, live, p.B, p.ldb, n0, p.N, p.K, smem, [&](int row, int col, const float (&v)[8]) {
+      bf16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
+      if (row < live && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)p.rows[start + row] * p.ldc + col) = o;
+    });
+  }
+}
+__global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int live = p.offsets[1], start = p.piece[0], cols = (p.N + 63) / 64;
+  const float scale = *p.scale;
+  const int64_t items = (int64_t)((p.M + 63) / 64) * cols;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int m0 = (int)(item / cols) * 64, n0 = (int)(item % cols) * 64;
+    few_tile<false, false, 4>(p.A, p.lda, m0, p.M, p.B + (int64_t)start * p.ldb, p.ldb, n0, p.N, live, smem, [&](int row, int col, const float (&v)[8]) {
+      bf16x8 o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
+      if (row < p.M && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
+    });
+  }
+}
+template <int RB, bool LOGITS>
+mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& p) {
+  static std::once_flag once;
+  static hipError_t rc = hipSuccess;
+  constexpr int kLds = few_lds<true, LOGITS, RB>();
+  auto kern = [] { if constexpr (LOGITS) return few_logits_kernel<RB>; else return few_dx_kernel<RB>; }();
+  MOSAIC_TRY(few_allow_lds(kern, kLds, &once, &rc));
+  kern<<<grid_for(quota, RB <= 2 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p);
+  MOSAIC_LAUNCH_CHECK();
+  return MOSAIC_OK;
+}
+// row blocks of 16 that a product of `most` rows is computed in, or 0 where it costs `other` at most
+inline int few_rows(int64_t most, int64_t N, int64_t K, double other) {
+  int best = 0;
+  for (int blocks = 1; blocks <= 4; blocks *= 2) {
+    const double us = few_price((double)(ceil_div(most, 16 * blocks) * ceil_div(N, 64)), (double)K, blocks, blocks <= 2);
+    if (us < other) { other = us; best = blocks; }
+  }
+  return best;
 }
 
 // ------------------------------------------------------------------------- a few tokens
@@ -462,12 +659,12 @@ constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
   int64_t piece, ld, blocks;
   int pieces, dw_splits, dw_k, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
-  size_t head, spans, rows, target, slot, losses, at_target, lse, stats, totals, x, e, sums, bytes;
+  size_t head, spans, rows, target, slot, losses, at_target, lse, inverse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
     const bool half = dtype == MOSAIC_BF16;
     const size_t es = dtype_size(dtype);
     ld = (V + 63) / 64 * 64;
-    blocks = ceil_div(V, kCeBlock);
+    blocks = ceil_div(V, half ? kCeBlock : kWideBlock);
     int64_t most = std::min(kPieceElems / (half ? 1 : 2) / ld, ((int64_t)1 << 30) / h) / 256 * 256;
     most = std::max<int64_t>(most, 256);
     if (half && T * ld <= kPieceElems + 2 * V * h && T * h <= (int64_t)1 << 30) most = std::max<int64_t>(most, ceil_div(T, 256) * 256);
@@ -479,8 +676,8 @@ struct CeLayout {
     head = take(sizeof(CeHead));
     spans = take((int64_t)sizeof(CeSpan) * pieces);
     rows = take(4 * padded); target = take(4 * padded); slot = take(4 * padded); losses = take(4 * T);
-    at_target = take(4 * piece); lse = take(4 * piece);
-    stats = take(half ? 8 * blocks * piece : 0); totals = take(half ? 4 * blocks * piece : 0);
+    at_target = take(4 * piece); lse = take(4 * piece); inverse = take(half ? 0 : 4 * piece);
+    stats = take(8 * blocks * piece); totals = take(4 * blocks * piece);
     x = take(padded * h * (int64_t)es);
     e = take(grad || !half ? piece * ld * (int64_t)es : 0);
     // Few tiles over a long contraction leave most CUs idle: it is cut until the tiles are about one to a CU, into no less than 1024 k-values.
@@ -578,7 +775,21 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     if (!half) {
       float* Z = (float*)(base + L.e);
       MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc + r0 * h * 4, h, table, h, Z, L.ld, nullptr, live, 1, capacity, 0));
-      rows_f32_kernel<<<grid_for(quota, 8, some), 256, 0, s>>>(p, head, Z, L.ld, grad);
+      if (V <= 256 * 32) {
+        const int grid = grid_for(quota, 8, some);
+        if (V <= 256 * 4) rows_f32_kernel<4><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        else rows_f32_kernel<32><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+      } else {
+        float2* const stats = (float2*)(base + L.stats);
+        float* const totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
+        p.inverse = (float*)(base + L.inverse);
+        const int grid = grid_for(quota, 8, some * L.blocks);
+        wide_f32_kernel<false><<<grid, 256, 0, s>>>(p, head, Z, L.ld, stats, totals, (float*)(base + L.at_target));
+        MOSAIC_LAUNCH_CHECK();
+        lse_kernel<<<grid_for(quota, 2, ceil_div(some, 16)), 1024, 0, s>>>(p, stats, totals, (int)L.blocks);
+        MOSAIC_LAUNCH_CHECK();
+        if (grad) wide_f32_kernel<true><<<grid, 256, 0, s>>>(p, head, Z, L.ld, stats, totals, nullptr);
+      }
       MOSAIC_LAUNCH_CHECK();
       if (dX) {
         MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, live, 1, capacity, 0, L.dx_k, L.dx_splits));
@@ -599,14 +810,25 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     z.tiles_n = (int)ceil_div(V, 256);
     z.rows = target; z.at_target = (float*)(base + L.at_target); z.stats = (float2*)(base + L.stats);
     z.totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
-    MOSAIC_TRY((launch_rows<true, true, W4_SOFTMAX>(s, quota, z, some <= 128)));
-    lse_kernel<<<grid_for(quota, 2, ceil_div(some, 16)), 1024, 0, s>>>(p, z.stats, z.totals, (int)L.blocks);
-    MOSAIC_LAUNCH_CHECK();
+    const bool low = some <= 128;
+    auto w4_tiles = [&](int64_t N) { return (double)(ceil_div(some, low ? 128 : 256) * ceil_div(N, 256)); };
+    switch (few_rows(some, V, h, w4_price(w4_tiles(V), (double)h, low))) {
+      case 1: MOSAIC_TRY((launch_few_rows<1, true>(s, quota, some, z))); break;
+      case 2: MOSAIC_TRY((launch_few_rows<2, true>(s, quota, some, z))); break;
+      case 4: MOSAIC_TRY((launch_few_rows<4, true>(s, quota, some, z))); break;
+      default: MOSAIC_TRY((launch_rows<true, true, W4_SOFTMAX>(s, quota, z, low)));
+    }
+    const bool join = grad && L.blocks <= kJoinBlocks;
+    if (!join) {
+      lse_kernel<<<grid_for(quota, 2, ceil_div(some, 16)), 1024, 0, s>>>(p, z.stats, z.totals, (int)L.blocks);
+      MOSAIC_LAUNCH_CHECK();
+    }
     if (!grad) continue;
     const int64_t left = 2 * some * L.ld;
     const Sweep sweep = sweep_grid(s, quota, ceil_div(some, 16) * ceil_div(L.ld, kStrip), 2 * left);
-    if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true><<<sweep.grid, 256, 0, s>>>(p, z.stats, E, L.ld);
-    else grad_kernel<false><<<sweep.grid, 256, 0, s>>>(p, z.stats, E, L.ld);
+    if (join) grad_kernel<false, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld);
+    else if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
+    else grad_kernel<false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
     MOSAIC_LAUNCH_CHECK();
     if (dX) {
       W4Args d = {};
@@ -618,10 +840,17 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.rows = rows;
       d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
-      const bool low = some <= 128;
-      MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
-      join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
-      MOSAIC_LAUNCH_CHECK();
+      const int blocks = few_rows(some, h, V, 8.0 + w4_cut((int)w4_tiles(h), d.K).us);
+      if (blocks) d.K = (int)V;                  // the rows of E are readable up to ld
+      switch (blocks) {
+        case 1: MOSAIC_TRY((launch_few_rows<1, false>(s, quota, some, d))); break;
+        case 2: MOSAIC_TRY((launch_few_rows<2, false>(s, quota, some, d))); break;
+        case 4: MOSAIC_TRY((launch_few_rows<4, false>(s, quota, some, d))); break;
+        default:
+          MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
+          join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
+          MOSAIC_LAUNCH_CHECK();
+      }
     }
     if (dtable) {
       W4Args w = {};
@@ -633,7 +862,15 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       w.row_block = row_block_for(w.K, V, 256);
       w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
       w.splits = L.dw_splits; w.split_k = L.dw_k;
-      if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
+      const double w4_us = w4_price((double)w.tile_count * L.dw_splits, (double)some / L.dw_splits, false) + (L.dw_splits > 1 ? 5.0 + (double)(V * h) * (4 * L.dw_splits + 2) / 5e6 : 0.0);
+      if (L.pieces == 1 && few_price((double)(ceil_div(V, 64) * ceil_div(h, 64)), (double)some, 4, false) < w4_us) {
+        static std::once_flag once;
+        static hipError_t rc = hipSuccess;
+        constexpr int kLds = few_lds<false, false, 4>();
+        MOSAIC_TRY(few_allow_lds(few_dtable_kernel, kLds, &once, &rc));
+        few_dtable_kernel<<<grid_for(quota, 1, ceil_div(V, 64) * ceil_div(h, 64)), kFewNT, kLds, s>>>(w);
+        MOSAIC_LAUNCH_CHECK();
+      } else if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
       else if (L.dw_splits > 1) {
         w.tile_count *= w.splits;
         MOSAIC_TRY((launch_w4_epi<false, false, W4_PIECES, 8, W4_GROUPED>(s, quota, w)));

@@ -57,7 +57,9 @@ CASES = [  # offsets, k, n, T
     ([0, 1], 64, 64, 1), ([0, 3, 3, 5], 8, 16, 5), ([0, 130, 130, 131, 400], 72, 264, 400), ([0, 256, 512], 128, 256, 512), ([2, 9, 40], 200, 136, 50),
     ([0, 0, 0, 0], 64, 72, 4), ([0, 257, 300, 301, 812], 136, 520, 812), ([0, 700], 320, 96, 700), ([0] + list(range(0, 1024)), 16, 24, 1100),
     # few rows to a group: up to 16, 32, 64 at a time, and groups of many more among them
-    ([0, 16, 33, 33, 40], 1032, 72, 41), ([0, 100, 100, 100, 100, 100, 100, 101], 264, 136, 101), ([0, 30, 70], 520, 200, 80), ([0, 1, 70, 100], 2000, 64, 100), ([0, 50, 130], 136, 1048, 128)]
+    ([0, 16, 33, 33, 40], 1032, 72, 41), ([0, 100, 100, 100, 100, 100, 100, 101], 264, 136, 101), ([0, 30, 70], 520, 200, 80), ([0, 1, 70, 100], 2000, 64, 100), ([0, 50, 130], 136, 1048, 128),
+    # weight gradients of few tiles over many rows, and of many tiles
+    ([0, 3000, 3000, 5100], 104, 136, 5100), ([0, 1, 1000], 72, 8, 1000), ([0, 120, 300], 1100, 1304, 300)]
 
 
 @pytest.mark.parametrize("form", FORMS)
