@@ -630,7 +630,8 @@ mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc,
   auto go = [&](auto t) {
     typedef decltype(t) T;
     const uintptr_t mask = 4 * sizeof(T) - 1;
-    const bool vec = lda % 4 == 0 && ldb % 4 == 0 && ldc % 4 == 0 && N % 4 == 0 && (a_kc ? K : M) % 4 == 0 && (b_kc ? K : N) % 4 == 0 && stride % 4 == 0 &&
+    // four elements per access where rows start on such boundaries; a row that ends between two has room up to the next, zeros in a K-contiguous A
+    const bool vec = lda % 4 == 0 && ldb % 4 == 0 && ldc % 4 == 0 && (b_kc || N % 4 == 0) && stride % 4 == 0 &&
                      (((uintptr_t)A | (uintptr_t)B | (uintptr_t)C | (uintptr_t)R) & mask) == 0;
     if (!a_kc) return vec ? launch_grouped_t<T, false, false, true>(s, quota, p, gr) : launch_grouped_t<T, false, false, false>(s, quota, p, gr);
     if (b_kc) return vec ? launch_grouped_t<T, true, true, true>(s, quota, p, gr) : launch_grouped_t<T, true, true, false>(s, quota, p, gr);

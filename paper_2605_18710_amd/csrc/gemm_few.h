@@ -8,6 +8,8 @@
 namespace {
 
 constexpr int kFewStep = 64, kFewWaves = 8, kFewNT = 64 * kFewWaves;
+// two workgroups to a CU for items of 16 rows: four waves to a SIMD
+constexpr int few_waves(int RB) { return RB == 1 ? 4 : 2; }
 // bytes of LDS: the waves' own 8 KB for every operand whose contraction is the strided index, or then their sums
 template <bool A_KC, bool B_KC, int RB> constexpr int few_lds() {
   return std::max(kFewWaves * 16 * RB * 64 * 4, kFewWaves * 8192 * ((A_KC ? 0 : 1) + (B_KC ? 0 : 1)));

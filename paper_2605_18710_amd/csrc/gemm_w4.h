@@ -113,7 +113,7 @@ struct W4Args {
   const int32_t* offsets;          // [groups + 1], on the device: group g is rows offsets[g] .. offsets[g + 1] - 1 of A (and of B, where A is K-strided)
   int groups, bound;               // offsets are held to 0 .. bound
   int64_t stride;                  // elements between two groups' B (C, where A is K-strided)
-  int splits, split_k;             // W4_PIECES, K-strided A: the contraction in `splits` pieces of split_k k-values, whole K-tiles
+  int splits, split_k;             // W4_PIECES, K-strided A: the contraction in `splits` pieces (K-contiguous: as the kernel cuts it, split_k k-values each)
   const int32_t* rows;             // W4_PIECES, K-contiguous A: where a row of the product goes in C.  W4_SOFTMAX: its target, a column or -1
   float* sums;                     // W4_PIECES: [pieces][rows][N], rows M, or those of the tiles that there are; W4_ADD: what is there already, [M][N]
   const float* scale;              // null, or on the device: a factor of the sums that leave for C
@@ -388,8 +388,9 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
       r.lo = __builtin_amdgcn_readfirstlane(min(max(p.offsets[r.g], 0), p.bound));
       r.hi = __builtin_amdgcn_readfirstlane(max(r.lo, min(max(p.offsets[r.g + 1], 0), p.bound)));
       if constexpr (!A_KC && EPI == W4_PIECES) {
-        r.lo = min(r.lo + r.split * p.split_k, r.hi);
-        r.hi = min(r.lo + p.split_k, r.hi);
+        const int per = ((r.hi - r.lo + p.splits - 1) / p.splits + 63) / 64 * 64;          // the rows that there are, in equal pieces
+        r.lo = min(r.lo + r.split * per, r.hi);
+        r.hi = min(r.lo + per, r.hi);
       }
       if constexpr (!A_KC) r.nk = max(2, (r.hi - r.lo + 63) / 64);
       r.m0 = trow * (32 * MI);

@@ -18,7 +18,22 @@ mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc,
 
 namespace {
 
-// Tiles of 256 rows, or of 128 where the groups have no more on average: an expert's rows seldom fill a tile, and half a tile less is computed for nothing.
+// Tiles of 256, 224, 192 or 160 rows, whichever fill the rounds of 256 CUs best, half a tile more for every group than its rows fill (a round of lower ones takes
+// 0.9, 0.8, 0.73 of the time: they read the weight side's fragments for fewer instructions); of 128 where the groups have no more rows on average.
+// 16384 rows of 16 experts, 2048 x 5632: 338 us by 256 rows (6.2 rounds), 331 by 224 (7.0); 41794 rows of 4, 1840 x 1064 214, 200 by 192.
+inline int tile_rows(int64_t T, int64_t groups, int64_t tiles_n) {
+  if (T <= 128 * groups) return 4;
+  const double with = (double)std::min(groups, T), cost[] = {3.5, 3.15, 2.8, 2.57};
+  double least = 1e30;
+  int best = 8;
+  for (int i = 0; i < 4; ++i) {
+    // uneven ends of the groups: half a tile each on average, give or take sqrt(groups / 12) in all
+    const double per = (double)tiles_n / 256.0, rounds = ((double)T / (32.0 * (8 - i)) + 0.5 * with) * per, spread = std::sqrt(with / 12.0) * per;
+    const double us = (std::ceil(rounds - spread) + std::ceil(rounds) + std::ceil(rounds + spread)) / 3.0 * cost[i];
+    if (us < least - 1e-9) { least = us; best = 8 - i; }
+  }
+  return best;
+}
 template <bool A_KC, bool B_KC>
 mosaic_status launch_rows(hipStream_t s, int quota, W4Args p) {
   auto go = [&](auto mi) -> mosaic_status {
@@ -30,13 +45,19 @@ mosaic_status launch_rows(hipStream_t s, int quota, W4Args p) {
     p.row_block = row_block_for(p.K, p.M, 32 * MI);
     return launch_w4_epi<A_KC, B_KC, W4_PLAIN, MI, W4_GROUPED>(s, quota, p);
   };
-  return p.M <= 128 * (int64_t)p.groups ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 8>{});
+  switch (tile_rows(p.M, p.groups, p.tiles_n)) {
+    case 4: return go(std::integral_constant<int, 4>{});
+    case 5: return go(std::integral_constant<int, 5>{});
+    case 6: return go(std::integral_constant<int, 6>{});
+    case 7: return go(std::integral_constant<int, 7>{});
+    default: return go(std::integral_constant<int, 8>{});
+  }
 }
 
 // Few rows to a group, or few tiles: items of 64 columns and up to 16 RB rows of a group (few_tile).
 // What bounds it: W, read once from memory for up to 16 RB rows.  48 rows of 8 experts, 4096 x 1408 (93 MB): 20 us, four-wave kernel 86.
 template <bool B_KC, int RB>
-__global__ __launch_bounds__(kFewNT) void grouped_few_kernel(const bf16* __restrict__ A, const bf16* __restrict__ W, bf16* __restrict__ C, int T, int groups,
+__global__ __launch_bounds__(kFewNT, few_waves(RB)) void grouped_few_kernel(const bf16* __restrict__ A, const bf16* __restrict__ W, bf16* __restrict__ C, int T, int groups,
                                                              int K, int N, const int32_t* __restrict__ offsets) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int starts[kMaxGroups + 1];
@@ -59,7 +80,7 @@ __global__ __launch_bounds__(kFewNT) void grouped_few_kernel(const bf16* __restr
 }
 
 // Weight gradients of few tiles: items of 64 x 64 of a group's matrix, the group's rows shared by eight waves.
-// 11749 rows of 3 experts, 104 x 136: XXX us, four-wave kernel 106.
+// 11749 rows of 3 experts, 104 x 136: 32 us, four-wave kernel 106.
 __global__ __launch_bounds__(kFewNT) void grouped_few_wgrad_kernel(const bf16* __restrict__ X, const bf16* __restrict__ dY, bf16* __restrict__ dW, int T, int groups, int k,
                                                                    int n, const int32_t* __restrict__ offsets) {
   extern __shared__ __align__(16) unsigned char smem[];
@@ -85,7 +106,7 @@ mosaic_status launch_few(hipStream_t s, int quota, int T, int groups, int K, int
   constexpr int kLds = few_lds<true, B_KC, RB>();
   MOSAIC_TRY(few_allow_lds(grouped_few_kernel<B_KC, RB>, kLds, &once, &rc));
   const int64_t items = (ceil_div(T, 16 * RB) + std::min(groups, T)) * ceil_div(N, 64);
-  grouped_few_kernel<B_KC, RB><<<grid_for(quota, RB <= 2 ? 2 : 1, items), kFewNT, kLds, s>>>((const bf16*)A, (const bf16*)W, (bf16*)C, T, groups, K, N, offsets);
+  grouped_few_kernel<B_KC, RB><<<grid_for(quota, RB == 1 ? 2 : 1, items), kFewNT, kLds, s>>>((const bf16*)A, (const bf16*)W, (bf16*)C, T, groups, K, N, offsets);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -102,7 +123,7 @@ inline int few_blocks(int64_t T, int64_t groups, int64_t K, int64_t N) {
   double least = w4_price(tiles(low ? 128 : 256) * (double)ceil_div(N, 256), (double)K, low);
   int best = 0;
   for (int blocks = 1; blocks <= 4; blocks *= 2) {
-    const double us = few_price(tiles(16.0 * blocks) * (double)ceil_div(N, 64), (double)K, blocks, blocks <= 2);
+    const double us = few_price(tiles(16.0 * blocks) * (double)ceil_div(N, 64), (double)K, blocks, blocks == 1);
     if (us < least) { least = us; best = blocks; }
   }
   return best;

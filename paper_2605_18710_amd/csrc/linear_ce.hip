@@ -100,7 +100,7 @@ __global__ __launch_bounds__(256) void place_kernel(const int32_t* __restrict__ 
 }
 // Both in one launch up to kListMax tokens: every workgroup makes the list for itself (a turn of 1024 tokens takes a microsecond, a launch four),
 // the first one writes it.
-constexpr int kListMax = 4096;
+constexpr int kListMax = 8192;
 template <typename T, int V>
 __global__ __launch_bounds__(kListThreads) void list_place_kernel(CeList l, const T* __restrict__ X, int64_t h, T* __restrict__ Xc, T* __restrict__ dX,
                                                                   float* __restrict__ losses) {
@@ -301,6 +301,7 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* 
     for (int i = 0; i < PER; ++i) {
       const int c = threadIdx.x + 256 * i;
       if (c < p.V) z[c] = g * (c == target ? (v[i] * inverse - 1.f) + (p.smoothing - even) : v[i] * inverse - even);
+      else if (c < (p.V + 3) / 4 * 4) z[c] = 0.f;            // the products read whole 16-byte pieces
     }
   }
 }
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* 
         const int c = 1024 * i + e;
         if (GRAD) {
           const float q = __builtin_amdgcn_exp2f(fmaf(v[i][e], kLog2e, -base)) * inverse;
-          v[i][e] = g * (c == target ? (q - 1.f) + (p.smoothing - even) : q - even);
+          v[i][e] = c0 + c >= p.V ? 0.f : g * (c == target ? (q - 1.f) + (p.smoothing - even) : q - even);      // the products read whole 16-byte pieces
         } else {
           if (c0 + c >= p.V) v[i][e] = -INFINITY;
           else total += v[i][e];
@@ -369,7 +370,7 @@ template <typename F> __device__ __forceinline__ float across_eight(float x, F f
   return f(x, dpp<kDppMirror8>(x));
 }
 template <int RB>
-__global__ __launch_bounds__(kFewNT) void few_logits_kernel(W4Args p) {
+__global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_logits_kernel(W4Args p) {
   extern __shared__ __align__(16) unsigned char smem[];
   auto add = [](float a, float b) { return a + b; };
   auto high = [](float a, float b) { return fmaxf(a, b); };
@@ -409,7 +410,7 @@ __global__ __launch_bounds__(kFewNT) void few_logits_kernel(W4Args p) {
   }
 }
 template <int RB>
-__global__ __launch_bounds__(kFewNT) void few_dx_kernel(W4Args p) {
+__global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_dx_kernel(W4Args p) {
   extern __shared__ __align__(16) unsigned char smem[];
   const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
   const float scale = *p.scale;
@@ -446,7 +447,7 @@ mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& 
   constexpr int kLds = few_lds<true, LOGITS, RB>();
   auto kern = [] { if constexpr (LOGITS) return few_logits_kernel<RB>; else return few_dx_kernel<RB>; }();
   MOSAIC_TRY(few_allow_lds(kern, kLds, &once, &rc));
-  kern<<<grid_for(quota, RB <= 2 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p);
+  kern<<<grid_for(quota, RB == 1 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -454,7 +455,7 @@ mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& 
 inline int few_rows(int64_t most, int64_t N, int64_t K, double other) {
   int best = 0;
   for (int blocks = 1; blocks <= 4; blocks *= 2) {
-    const double us = few_price((double)(ceil_div(most, 16 * blocks) * ceil_div(N, 64)), (double)K, blocks, blocks <= 2);
+    const double us = few_price((double)(ceil_div(most, 16 * blocks) * ceil_div(N, 64)), (double)K, blocks, blocks == 1);
     if (us < other) { other = us; best = blocks; }
   }
   return best;
@@ -627,7 +628,13 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, 
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / pieces, c = (i - row * pieces) * V;
     vec sum = *reinterpret_cast<const vec*>(P + row * N + c);
-    for (int s = 1; s < splits; ++s) sum += *reinterpret_cast<const vec*>(P + (s * M + row) * N + c);
+    for (int s = 1; s < splits; s += 4) {        // four on their way together
+      vec part[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) part[u] = s + u < splits ? *reinterpret_cast<const vec*>(P + ((s + u) * M + row) * N + c) : vec{};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) if (s + u < splits) sum += part[u];
+    }
     typename Pack<T, V>::type o;
 #pragma unroll
     for (int e = 0; e < V; ++e) pack_set<T, V>(o, e, pack_get<float, V>(sum, e) * factor);
@@ -658,7 +665,7 @@ __global__ __launch_bounds__(1024) void loss_kernel(const float* __restrict__ lo
 constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
   int64_t piece, ld, blocks;
-  int pieces, dw_splits, dw_k, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
+  int pieces, dw_splits, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
   size_t head, spans, rows, target, slot, losses, at_target, lse, inverse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
     const bool half = dtype == MOSAIC_BF16;
@@ -681,13 +688,8 @@ struct CeLayout {
     x = take(padded * h * (int64_t)es);
     e = take(grad || !half ? piece * ld * (int64_t)es : 0);
     // Few tiles over a long contraction leave most CUs idle: it is cut until the tiles are about one to a CU, into no less than 1024 k-values.
-    auto cut = [&](int64_t M, int64_t K, int* k) {
-      const int64_t tiles = ceil_div(M, 256) * ceil_div(h, 256);
-      int64_t n = std::max<int64_t>(1, std::min(256 / tiles, K / 1024));
-      *k = (int)(ceil_div(ceil_div(K, n), 64) * 64);
-      return (int)std::max<int64_t>(1, ceil_div(K, *k));
-    };
-    dw_splits = half && grad ? cut(V, piece, &dw_k) : 1;
+    const int64_t tiles = ceil_div(V, 256) * ceil_div(h, 256);
+    dw_splits = half && grad ? (int)std::max<int64_t>(1, std::min(256 / tiles, std::min(piece, T) / 1024)) : 1;
     int64_t n = 0;
     if (half && grad) {
       n = std::min<int64_t>(kMostPieces * ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 128) * ceil_div(h, 256), kMostPieceTiles) * 65536;       // w4_cut
@@ -861,7 +863,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       w.tile_count = w.tiles_m * w.tiles_n;
       w.row_block = row_block_for(w.K, V, 256);
       w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
-      w.splits = L.dw_splits; w.split_k = L.dw_k;
+      w.splits = L.dw_splits;
       const double w4_us = w4_price((double)w.tile_count * L.dw_splits, (double)some / L.dw_splits, false) + (L.dw_splits > 1 ? 5.0 + (double)(V * h) * (4 * L.dw_splits + 2) / 5e6 : 0.0);
       if (L.pieces == 1 && few_price((double)(ceil_div(V, 64) * ceil_div(h, 64)), (double)some, 4, false) < w4_us) {
         static std::once_flag once;
