@@ -266,7 +266,8 @@ struct W4GroupTiles {
 // From 0 to 1, relative to its block's largest: an fp16 number is within 2^-11 of it relative to itself, or within 2^-25 of the largest.  The logits
 // themselves in 16 bits would be off by that share of the logit, which the exponential turns into that much of a probability times the logit.
 // A block whose largest logit is -infinity counts from 0: its sum is 0.  NaN and +infinity make the sum NaN.  m is kept times log2 e.
-// Here for one row of a block, a lane's sixteen values v[j][e], columns col + 16j + 4g + e; the four lanes of a row lie 16 apart (g = 0 .. 3).
+// Here for one row of two blocks side by side, a lane's sixteen values v[h][j][e] of each, columns col + 64h + 16j + 4g + e; the four lanes of a row lie 16 apart
+// (g = 0 .. 3).  Two at once, because a wave is alone on its SIMD and every step waits for the one before (12288 x 4096 x 128000 9790 -> 9450 us).
 constexpr int kCeBlock = 64;
 // what the four lanes of a row make of their values together
 template <typename F> __device__ __forceinline__ float across_rows(float x, F f) {
@@ -275,51 +276,69 @@ template <typename F> __device__ __forceinline__ float across_rows(float x, F f)
   auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);       // the same by 16 lanes
   return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ void w4_softmax(const W4Args& p, f32x4 (&v)[4], int row, int col, int g, int target, bool in) {
+__device__ __forceinline__ void w4_softmax(const W4Args& p, f32x4 (&v)[2][4], int row, int col, int g, int target, bool in) {
   constexpr float kLog2e = 1.44269504088896340736f;
   auto add = [](float a, float b) { return a + b; };
   auto high = [](float a, float b) { return fmaxf(a, b); };
   const int hit = target - col;
-  const bool mine = in && hit >= 0 && hit < kCeBlock && target < p.N && ((hit >> 2) & 3) == g;
+  const bool mine = in && hit >= 0 && hit < 2 * kCeBlock && target < p.N && ((hit >> 2) & 3) == g;
   if (__ballot(mine)) {
     float t = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = hit & 1 ? v[j][1] : v[j][0], b = hit & 1 ? v[j][3] : v[j][2];
+    for (int j = 0; j < 8; ++j) {
+      const f32x4& x = v[j >> 2][j & 3];
+      const float a = hit & 1 ? x[1] : x[0], b = hit & 1 ? x[3] : x[2];
       t = hit >> 4 == j ? (hit & 2 ? b : a) : t;
     }
     if (mine) p.at_target[row] = t;
   }
-  const bool first = g == 0 && in && col < p.N;
+  const bool first = g == 0 && in;
   const int64_t slot = (int64_t)(col / kCeBlock) * p.M + row;
   if (p.totals) {
-    float total = 0.f;                             // rows of the table past its end read zeros
 #pragma unroll
-    for (int j = 0; j < 4; ++j) total += (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
-    total = across_rows(total, add);
-    if (first) p.totals[slot] = total;
+    for (int h = 0; h < 2; ++h) {
+      float total = 0.f;                           // rows of the table past its end read zeros
+#pragma unroll
+      for (int j = 0; j < 4; ++j) total += (v[h][j][0] + v[h][j][1]) + (v[h][j][2] + v[h][j][3]);
+      total = across_rows(total, add);
+      if (first && col + 64 * h < p.N) p.totals[slot + h * p.M] = total;
+    }
   }
-  if (col + kCeBlock > p.N) {
+  if (col + 2 * kCeBlock > p.N) {
+    int left = p.N - col - 4 * g;
+    asm volatile("" : "+v"(left));                 // compared here, for these rows: kept for all of a tile's the masks take more scalar registers than there are
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[j][e] = col + 16 * j + 4 * g + e < p.N ? v[j][e] : -INFINITY;
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[h][j][e] = 64 * h + 16 * j + e < left ? v[h][j][e] : -INFINITY;
   }
-  float m = -INFINITY;
+  float m[2], ref[2], sum[2], part[2][4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fmaxf(v[j][0], v[j][1]), fmaxf(v[j][2], v[j][3])));
-  m = across_rows(m, high);
-  const float ref = m == -INFINITY ? 0.f : m * kLog2e;
-  float sum = 0.f;
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    // fused: the product rounded before the subtraction would cost 2^-24 of the logit
+    for (int h = 0; h < 2; ++h) part[h][j] = fmaxf(fmaxf(v[h][j][0], v[h][j][1]), fmaxf(v[h][j][2], v[h][j][3]));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[j][e] = __builtin_amdgcn_exp2f(fmaf(v[j][e], kLog2e, -ref));
-    sum += (v[j][0] + v[j][1]) + (v[j][2] + v[j][3]);
+  for (int h = 0; h < 2; ++h) m[h] = fmaxf(fmaxf(part[h][0], part[h][1]), fmaxf(part[h][2], part[h][3]));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    m[h] = across_rows(m[h], high);
+    ref[h] = m[h] == -INFINITY ? 0.f : m[h] * kLog2e;
   }
-  sum = across_rows(sum, add);
-  if (first) p.stats[slot] = make_float2(ref, sum);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      // fused: the product rounded before the subtraction would cost 2^-24 of the logit
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[h][j][e] = __builtin_amdgcn_exp2f(fmaf(v[h][j][e], kLog2e, -ref[h]));
+      part[h][j] = (v[h][j][0] + v[h][j][1]) + (v[h][j][2] + v[h][j][3]);
+    }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) sum[h] = across_rows((part[h][0] + part[h][1]) + (part[h][2] + part[h][3]), add);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) if (first && col + 64 * h < p.N) p.stats[slot + h * p.M] = make_float2(ref[h], sum[h]);
 }
 
 template <bool A_KC, bool B_KC, int EPI, int MI, int MAP = W4_WHOLE>
@@ -532,7 +551,17 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
   };
   const __amdgpu_buffer_rsrc_t rc_all = make_rsrc(p.C, p.c_bytes), rc2 = make_rsrc(p.C2, p.C2 ? p.c2_bytes : 0u);
   const __amdgpu_buffer_rsrc_t rr = make_rsrc(p.R, !p.R ? 0u : EPI == W4_TABLE ? (uint32_t)(p.r_rows * p.ldc * 2) : p.c_bytes), rbias = make_rsrc(p.bias, p.bias ? (uint32_t)p.N * 2u : 0u);
+  // W4_PIECES, K-contiguous A: where this lane's rows go; W4_SOFTMAX: their targets.  Requested ahead of the K loop: behind it they would wait for the requests of the
+  // next item's K-tiles, and the epilogue for them (loss of 2450 tokens, 2048 x 50021, 455 -> 431 us).
+  constexpr bool TO_ROWS = EPI == W4_PIECES && A_KC;
+  constexpr int kOfRow = TO_ROWS ? 2 * MI : EPI == W4_SOFTMAX ? MI : 0;
+  int of_row[kOfRow ? kOfRow : 1];
   while (true) {
+#pragma unroll
+    for (int i = 0; i < kOfRow; ++i) {
+      const int row = wm + (EPI == W4_SOFTMAX ? 16 * i + (lane & 15) : 8 * i + (lane >> 3));
+      of_row[i] = row < it.hi - it.lo - it.m0 ? p.rows[start + it.lo + it.m0 + row] : -1;
+    }
     settle();
     for (int n = it.nk - 2; n > 0; --n) step();
     // the last K-tile of this item has been requested: the requests move on to the next item
@@ -594,18 +623,8 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
 #pragma unroll
         for (int b = 0; b < RAHEAD; ++b) request_res(b);
       }
-      // W4_PIECES: where this lane's rows go; W4_SOFTMAX: their targets
-      constexpr bool TO_ROWS = EPI == W4_PIECES && A_KC;
-      int of_row[2 * MI];
-      if constexpr (TO_ROWS || EPI == W4_SOFTMAX) {
-#pragma unroll
-        for (int i = 0; i < (EPI == W4_SOFTMAX ? MI : 2 * MI); ++i) {
-          const int row = wm + (EPI == W4_SOFTMAX ? 16 * i + elr : 8 * i + prow);
-          of_row[i] = row < rows ? p.rows[start + it.lo + it.m0 + row] : -1;
-        }
-      }
-      // Groups of rows, no sums: 16 rows x 64 columns are rounded to bf16 where they are and pass through one of two patches of 2 KB (rows of 128
-      // bytes, 16-byte chunks XOR-swizzled by the row), from which a block is read while the next is worked on and stored behind it.
+      // Groups of rows, no sums: 16 rows x 128 columns are rounded where they are and pass through two patches of 2 KB (64 columns each, rows of 128
+      // bytes, 16-byte chunks XOR-swizzled by the row); they are stored once the next are worked on.
       if constexpr (GROUPED && (EPI == W4_PLAIN || EPI == W4_SOFTMAX || EPI == W4_PIECES)) {
         unsigned char* const half = reinterpret_cast<unsigned char*>(smem + 2 * kW4Stage) + wave * (64 * kW4Pitch);
         u32x4 leaving[2][2];
@@ -624,48 +643,52 @@ __global__ __launch_bounds__(256, 1) void gemm_bf16_w4_kernel(W4Args p, TileQueu
           }
         };
 #pragma unroll
-        for (int b = 0; b < 2 * MI; ++b) {
-          const int i = b >> 1, h = b & 1;
-          f32x4 v[4];
+        for (int i = 0; i < MI; ++i) {
+          f32x4 v[2][4];
 #pragma unroll
-          for (int jj = 0; jj < 4; ++jj) {
+          for (int j = 0; j < 8; ++j) {
             // moved here and not before: left to itself the compiler moves all 256 accumulators at once, to registers that there are not
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float x;
-              asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[i][4 * h + jj][e]));
-              v[jj][e] = x;
+              asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(x) : "a"(acc[i][j][e]));
+              v[j >> 2][j & 3][e] = x;
             }
-            acc[i][4 * h + jj] = f32x4{0.f, 0.f, 0.f, 0.f};
+            acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
           }
           if constexpr (EPI == W4_SOFTMAX) {
             const int row = wm + 16 * i + elr;
-            w4_softmax(p, v, it.m0 + row, it.n0 + wn + 64 * h, eg, of_row[i], row < rows);
+            w4_softmax(p, v, it.m0 + row, it.n0 + wn, eg, of_row[i], row < rows);
           }
           if (EPI == W4_PIECES && p.splits > 1) {        // a piece's sums, in fp32
-            const int row = wm + 16 * i + elr, col = it.n0 + wn + 64 * h + 4 * eg;
+            const int row = wm + 16 * i + elr, col = it.n0 + wn + 4 * eg;
             float* const at = p.sums + ((int64_t)it.split * p.M + (A_KC ? it.lo : 0) + it.m0 + row) * p.N + col;
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) if (row < rows && col + 16 * jj < p.N) *reinterpret_cast<f32x4*>(at + 16 * jj) = v[jj];
+            for (int j = 0; j < 8; ++j) if (row < rows && col + 16 * j < p.N) *reinterpret_cast<f32x4*>(at + 16 * j) = v[j >> 2][j & 3];
           } else if (EPI != W4_SOFTMAX || p.C) {
+            if (i > 0) { leave(2 * i - 2); leave(2 * i - 1); }
 #pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-              typedef typename std::conditional<EPI == W4_SOFTMAX, _Float16, bf16>::type E;
-              typedef __attribute__((ext_vector_type(4))) E vec4;
-              vec4 o;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[e] = (E)(EPI == W4_SOFTMAX ? v[jj][e] : v[jj][e] * scale);
-              *reinterpret_cast<vec4*>(half + 2048 * (b & 1) + elr * 128 + (((2 * jj + (eg >> 1)) ^ (elr & 7)) << 4) + 8 * (eg & 1)) = o;
-            }
+              for (int jj = 0; jj < 4; ++jj) {
+                typedef typename std::conditional<EPI == W4_SOFTMAX, _Float16, bf16>::type E;
+                typedef __attribute__((ext_vector_type(4))) E vec4;
+                vec4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (E)(EPI == W4_SOFTMAX ? v[h][jj][e] : v[h][jj][e] * scale);
+                *reinterpret_cast<vec4*>(half + 2048 * h + elr * 128 + (((2 * jj + (eg >> 1)) ^ (elr & 7)) << 4) + 8 * (eg & 1)) = o;
+              }
             patch_sync();
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
-              leaving[b & 1][q] = *reinterpret_cast<const u32x4*>(half + 2048 * (b & 1) + (prow + 8 * q) * 128 + (((ln & 7) ^ (prow & 7)) << 4));
-            if (b > 0) leave(b - 1);
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int q = 0; q < 2; ++q)
+                leaving[h][q] = *reinterpret_cast<const u32x4*>(half + 2048 * h + (prow + 8 * q) * 128 + (((ln & 7) ^ (prow & 7)) << 4));
+            patch_sync();
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (EPI == W4_PIECES ? p.splits == 1 : EPI != W4_SOFTMAX || p.C) leave(2 * MI - 1);
+        if (EPI == W4_PIECES ? p.splits == 1 : EPI != W4_SOFTMAX || p.C) { leave(2 * MI - 2); leave(2 * MI - 1); }
       } else {
       // W4_ADD: the sums so far, requested a block ahead
       float4 before[EPI == W4_ADD ? 2 : 1][2][2];
