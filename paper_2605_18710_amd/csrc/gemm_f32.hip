@@ -593,7 +593,10 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
 
 template <typename T, bool A_KC, bool B_KC, bool VEC>
 mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
-  const bool large = large_tiles(p.M, p.N);
+  // Half a tile more for every group than its rows fill.  Tiles of 32 / of 64, us: input gradient of 2998 rows of 12 experts, 640 x 1000, 530 tiles of 64, 59 / 71, forward,
+  // 848, 59 / 58; 6000 rows, 640 x 640, 1000, 71 / 57; weight gradients of 4, 1024 x 1024, 1024, 57 / 47; of 8, 256 x 256, 128, 13 / 26.
+  const int64_t t64 = ceil_div(p.M, 64), n64 = ceil_div(p.N, 64);
+  const bool large = (A_KC ? (t64 + std::min<int64_t>(gr.groups, p.M) / 2) * n64 : t64 * n64 * gr.groups) * gr.splits >= 848;
   const int bt = large ? 64 : 32;
   const int64_t tm = ceil_div(p.M, bt), tn = ceil_div(p.N, bt), most = (A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups) * gr.splits;
   if (most > INT32_MAX / 2) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "too many output tiles");

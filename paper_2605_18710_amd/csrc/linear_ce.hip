@@ -409,9 +409,28 @@ __global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_logits_kernel(W4Arg
     });
   }
 }
+// loss = sum of the tokens' / D, by one workgroup of NT threads: every thread its tokens in ascending order, in 64 bits
+struct CeLoss { const float* losses; int T; const CeHead* head; float* loss; };
+template <int NT>
+__device__ __forceinline__ void add_losses(const CeLoss& l, double* part) {
+  double sum = 0.0;
+  for (int t = threadIdx.x; t < l.T; t += NT) sum += (double)l.losses[t];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) sum += part[w];
+    *l.loss = (float)(sum * (double)l.head->per_token);
+  }
+  __syncthreads();
+}
+// the last workgroup also adds the losses, where there are no more pieces (loss not null)
 template <int RB>
-__global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_dx_kernel(W4Args p) {
+__global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l) {
   extern __shared__ __align__(16) unsigned char smem[];
+  if (l.loss && blockIdx.x == gridDim.x - 1) add_losses<kFewNT>(l, reinterpret_cast<double*>(smem));
   const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
   const float scale = *p.scale;
   const int64_t items = (int64_t)tiles_m * ((p.N + 63) / 64);
@@ -440,14 +459,14 @@ __global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p) {
     });
   }
 }
-template <int RB, bool LOGITS>
-mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& p) {
+template <int RB, bool LOGITS, typename... MORE>
+mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& p, MORE... more) {
   static std::once_flag once;
   static hipError_t rc = hipSuccess;
   constexpr int kLds = few_lds<true, LOGITS, RB>();
   auto kern = [] { if constexpr (LOGITS) return few_logits_kernel<RB>; else return few_dx_kernel<RB>; }();
   MOSAIC_TRY(few_allow_lds(kern, kLds, &once, &rc));
-  kern<<<grid_for(quota, RB == 1 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p);
+  kern<<<grid_for(quota, RB == 1 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p, more...);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -642,20 +661,10 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, 
   }
 }
 
-// loss = sum of the tokens' / D: one workgroup, every thread its tokens in ascending order, in 64 bits
-__global__ __launch_bounds__(1024) void loss_kernel(const float* __restrict__ losses, int T, const CeHead* __restrict__ head, float* __restrict__ loss) {
-  __shared__ double part[16];
-  double sum = 0.0;
-  for (int t = threadIdx.x; t < T; t += 1024) sum += (double)losses[t];
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int w = 1; w < 16; ++w) sum += part[w];
-    *loss = (float)(sum * (double)head->per_token);
-  }
+constexpr int kLossThreads = kFewNT;             // the order of the sum is few_dx_kernel's
+__global__ __launch_bounds__(kLossThreads) void loss_kernel(CeLoss l) {
+  __shared__ double part[kLossThreads / 64];
+  add_losses<kLossThreads>(l, part);
 }
 
 // -------------------------------------------------------------------------------- sizes
@@ -766,6 +775,8 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
   if (half) MOSAIC_TRY(wide ? place(bf16(), std::integral_constant<int, 8>()) : place(bf16(), One()));
   else MOSAIC_TRY(wide ? place(float(), std::integral_constant<int, 4>()) : place(float(), One()));
   float* const sums = (float*)(base + L.sums);
+  const CeLoss add = {losses, (int)T, head, loss};
+  bool added = false;
   for (int i = 0; i < L.pieces; ++i) {
     const int64_t r0 = i * L.piece;
     const int capacity = (int)L.piece, some = (int)std::min(L.piece, std::max<int64_t>(T - (half ? 0 : r0), 1));      // at most that many rows
@@ -844,10 +855,13 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
       const int blocks = few_rows(some, h, V, 8.0 + w4_cut((int)w4_tiles(h), d.K).us);
       if (blocks) d.K = (int)V;                  // the rows of E are readable up to ld
+      CeLoss now = add;
+      if (L.pieces > 1) now.loss = nullptr;
+      added = blocks && now.loss;
       switch (blocks) {
-        case 1: MOSAIC_TRY((launch_few_rows<1, false>(s, quota, some, d))); break;
-        case 2: MOSAIC_TRY((launch_few_rows<2, false>(s, quota, some, d))); break;
-        case 4: MOSAIC_TRY((launch_few_rows<4, false>(s, quota, some, d))); break;
+        case 1: MOSAIC_TRY((launch_few_rows<1, false>(s, quota, some, d, now))); break;
+        case 2: MOSAIC_TRY((launch_few_rows<2, false>(s, quota, some, d, now))); break;
+        case 4: MOSAIC_TRY((launch_few_rows<4, false>(s, quota, some, d, now))); break;
         default:
           MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
           join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
@@ -881,7 +895,9 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       } else MOSAIC_TRY((launch_w4_epi<false, false, W4_PLAIN, 8, W4_GROUPED>(s, quota, w)));
     }
   }
-  loss_kernel<<<1, 1024, 0, s>>>(losses, (int)T, head, loss);
-  MOSAIC_LAUNCH_CHECK();
+  if (!added) {
+    loss_kernel<<<1, kLossThreads, 0, s>>>(add);
+    MOSAIC_LAUNCH_CHECK();
+  }
   return MOSAIC_OK;
 }
