@@ -523,7 +523,7 @@ struct F32Groups {
   const int32_t* offsets;
   int groups, bound;
   int64_t stride;            // elements between two groups' B, or C
-  int splits, split_k;       // K-contiguous A, one group: the contraction in pieces of split_k, each with a C of its own, M rows
+  int splits, split_k;       // one group: the contraction in pieces of split_k (K-strided A: as equal ones as whole K-tiles make), each with a C of its own, M rows
 };
 constexpr int kGroupsAtOnce = 256;       // of which the first tiles are kept in LDS, a thread each
 template <typename T, int BT, int KS, bool A_KC, bool B_KC, bool VEC>
@@ -583,6 +583,13 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
         q.B = (const T*)p.B + (int64_t)first * p.ldb;
         q.C = (T*)p.C + (g0 + a) * gr.stride;
         q.K = rows;
+        if (gr.splits > 1) {
+          const int per = ((rows + gr.splits - 1) / gr.splits + KS - 1) / KS * KS, k0 = min(piece * per, rows);
+          q.A = (const T*)q.A + (int64_t)k0 * p.lda;
+          q.B = (const T*)q.B + (int64_t)k0 * p.ldb;
+          q.C = (T*)p.C + (int64_t)piece * p.M * p.ldc;
+          q.K = min(per, rows - k0);
+        }
         if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
       }
       gemm_f32_tile<T, BT, KS, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
@@ -623,7 +630,7 @@ mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const 
 }  // namespace
 
 // M: rows of A for all groups together, the most that there can be (a K-strided A: of each C).  K: the contraction (a K-strided A: the longest).
-// splits > 1 (one group, K-contiguous A, fp32): the contraction in pieces of split_k, C [splits, M, ldc]
+// splits > 1 (one group, fp32): the contraction in pieces (K-contiguous A: of split_k), C [splits, M, ldc]
 mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
                                  int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k, int splits) {
   if (M == 0 || N == 0 || groups == 0) return MOSAIC_OK;

@@ -158,6 +158,8 @@ mosaic_status few_allow_lds(KERN kern, int bytes, std::once_flag* once, hipError
 // 256: 1.5) for 64 k-values while it has its CU to itself.  Workgroups of few_tile read their operands through the caches at 6.3 TB/s together, or wait 1.45
 // for a step of each wave; two of them share a CU where their LDS allows.
 inline double w4_price(double tiles, double K, bool low) { return 4.0 + std::ceil(tiles / 256.0) * std::max(2.0, std::ceil(K / 64.0)) * (low ? 1.3 : 1.5); }
+// items and operands of a group whose rows are its contraction are taken as the average, but the longest chain as 2.5 times that: experts are not chosen evenly
+constexpr double kUneven = 2.5;
 inline double few_price(double items, double K, int blocks, bool twice) {
   const double waits = std::ceil(items / (twice ? 512.0 : 256.0)) * (2.0 + std::ceil(std::ceil(K / 64.0) / kFewWaves) * 1.45);
   return 4.0 + std::max(waits, items * K * 2.0 * (64.0 + 16.0 * blocks) / 6.3e6);

@@ -133,21 +133,36 @@ enum { W4_WHOLE, W4_GROUPED };
 constexpr int kMaxGroups = 1024;
 
 // W4_PIECES, K-contiguous A: into how many pieces the contraction of `tiles` tiles is cut, by the shape alone (256: CUs of the device that the kernels are written
-// for).  Microseconds: 1.45 for 64 k-values of a tile, 8 around them; the pass that adds the pieces at 5 TB/s behind 5.  dz table for 4096, 1280 of 51001: 30 tiles,
-// one round however long; 6144 x 4096 of 128000: 384 tiles, 5600 us in two rounds, 4400 as three rounds of half the length.
-constexpr int kMostPieces = 16, kMostPieceTiles = 2048;
-struct W4Cut { int pieces, k; float us; };
-__device__ __host__ __forceinline__ W4Cut w4_cut(int tiles, int K) {
-  W4Cut best = {1, (K + 63) / 64 * 64, 0.f};
-  best.us = (float)((tiles + 255) / 256) * ((float)(best.k / 64) * 1.45f + 8.f);
-  for (int n = 2; n <= kMostPieces && n * tiles <= kMostPieceTiles; ++n) {
-    const int k = ((K + n - 1) / n + 63) / 64 * 64;
-    if (k < 1024) break;
-    const int pieces = (K + k - 1) / k;
-    const float us = (float)((tiles * pieces + 255) / 256) * ((float)(k / 64) * 1.45f + 8.f) + (float)tiles * (float)(4 * pieces + 2) * 0.0131f + 5.f;
-    if (us < best.us) best = {pieces, k, us};
-  }
-  return best;
+// for).  Nanoseconds: 1450 for 64 k-values of a tile, 8000 around them; the sums of a tile written and read at 5 TB/s, 5000 for the pass that adds them.  Whole
+// numbers, so that the product and that pass come to the same cut.  Measured: 6144 x 4096 of 128000, 384 tiles: 5600 us in two rounds, 4400 as
+// three rounds of half the length; 187 x 216 of 85501, one tile: 106 us in 16 pieces, 29 in 122.
+constexpr int kMostPieces = 128, kMostPieceTiles = 2048, kCuts = 40;
+struct W4Cut { int pieces, k; };
+// candidate i: 1 to 16, then eight of even steps up to every doubling
+__device__ __host__ __forceinline__ int w4_cut_pieces(int i) { return i < 16 ? i + 1 : (18 + 2 * ((i - 16) & 7)) << ((i - 16) >> 3); }
+__device__ __host__ __forceinline__ W4Cut w4_cut_of(int i, int K) {
+  const int n = w4_cut_pieces(i), k = ((K + n - 1) / n + 63) / 64 * 64;
+  return {(K + k - 1) / k, k};
+}
+__device__ __host__ __forceinline__ int64_t w4_cut_ns(int i, int tiles, int K) {
+  const W4Cut cut = w4_cut_of(i, K);
+  if (i && (cut.k < 256 || (int64_t)w4_cut_pieces(i) * tiles > kMostPieceTiles)) return INT64_MAX >> 8;
+  return ((int64_t)tiles * cut.pieces + 255) / 256 * (cut.k / 64 * (int64_t)1450 + 8000) + (i ? (int64_t)tiles * (8 * cut.pieces + 2) * 13 + 5000 : 0);
+}
+inline float w4_cut_us(int tiles, int K) {
+  int64_t best = INT64_MAX;
+  for (int i = 0; i < kCuts; ++i) best = std::min(best, w4_cut_ns(i, tiles, K));
+  return (float)best * 1e-3f;
+}
+// all lanes of a wave together, a candidate to a lane
+__device__ __forceinline__ W4Cut w4_cut(int tiles, int K) {
+  const int lane = threadIdx.x & 63;
+  int64_t best = lane < kCuts ? w4_cut_ns(lane, tiles, K) << 6 | lane : INT64_MAX;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) best = min(best, (int64_t)__shfl_xor((long long)best, o, 64));
+  const int i = __builtin_amdgcn_readfirstlane((int)best & 63);
+  const W4Cut cut = w4_cut_of(i, K);
+  return {__builtin_amdgcn_readfirstlane(cut.pieces), __builtin_amdgcn_readfirstlane(cut.k)};
 }
 constexpr int kW4Stage = 2 * 256 * 64 * 2;                         // both operands of a K-tile
 constexpr int kW4Pitch = 68;                                       // floats per row of the epilogue's patch: 16 rows of 64

@@ -267,25 +267,26 @@ __device__ __forceinline__ float block_reduce(float x, bool max, float* lds) {
   return max ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// fp32 logits, a workgroup to a row of up to 256 PER of them, which it holds: loss and (grad) dz in place
-template <int PER>
-__global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, int grad) {
+// fp32 logits, a workgroup (NT 256) or a wave (64) to a row of up to NT PER of them, which it holds: loss and (grad) dz in place
+template <int NT, int PER>
+__global__ __launch_bounds__(NT) void rows_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, int grad) {
   __shared__ float lds[4];
   const int live = p.span->live, start = p.span->start;
   const float g = head->per_token, even = p.smoothing / (float)p.V;
+  auto reduce = [&](float x, bool max) { return NT == 64 ? (max ? wave_max(x) : wave_sum(x)) : block_reduce(x, max, lds); };
   for (int row = blockIdx.x; row < live; row += gridDim.x) {
     float* z = Z + row * ld;
     const int target = p.target[start + row];
     float v[PER], top = -INFINITY, total = 0.f, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x + 256 * i;
+      const int c = threadIdx.x + NT * i;
       v[i] = c < p.V ? z[c] : -INFINITY;
       top = fmaxf(top, v[i]);
       total += c < p.V ? v[i] : 0.f;
     }
-    top = block_reduce(top, true, lds);
-    if (p.smoothing > 0.f) total = block_reduce(total, false, lds);
+    top = reduce(top, true);
+    if (p.smoothing > 0.f) total = reduce(total, false);
     const float ref = top == -INFINITY ? 0.f : top;
     const float at_target = z[target];
 #pragma unroll
@@ -293,13 +294,14 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(CePiece p, const CeHead* 
       v[i] = expf(v[i] - ref);
       sum += v[i];
     }
-    sum = block_reduce(sum, false, lds);         // behind its barriers the target's logit has been read
+    sum = reduce(sum, false);
+    __syncthreads();                             // the target's logit has been read by all
     if (threadIdx.x == 0) p.losses[p.rows[start + row]] = token_loss((ref + logf(sum)) / kLn2, at_target, total, p.smoothing, p.V);
     if (!grad) continue;
     const float inverse = 1.f / sum;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x + 256 * i;
+      const int c = threadIdx.x + NT * i;
       if (c < p.V) z[c] = g * (c == target ? (v[i] * inverse - 1.f) + (p.smoothing - even) : v[i] * inverse - even);
       else if (c < (p.V + 3) / 4 * 4) z[c] = 0.f;            // the products read whole 16-byte pieces
     }
@@ -647,12 +649,12 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, 
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < items; i += (int64_t)gridDim.x * 256) {
     const int64_t row = i / pieces, c = (i - row * pieces) * V;
     vec sum = *reinterpret_cast<const vec*>(P + row * N + c);
-    for (int s = 1; s < splits; s += 4) {        // four on their way together
-      vec part[4];
+    for (int s = 1; s < splits; s += 8) {        // eight on their way together
+      vec part[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) part[u] = s + u < splits ? *reinterpret_cast<const vec*>(P + ((s + u) * M + row) * N + c) : vec{};
+      for (int u = 0; u < 8; ++u) part[u] = s + u < splits ? *reinterpret_cast<const vec*>(P + ((s + u) * M + row) * N + c) : vec{};
 #pragma unroll
-      for (int u = 0; u < 4; ++u) if (s + u < splits) sum += part[u];
+      for (int u = 0; u < 8; ++u) if (s + u < splits) sum += part[u];
     }
     typename Pack<T, V>::type o;
 #pragma unroll
@@ -701,7 +703,7 @@ struct CeLayout {
     dw_splits = half && grad ? (int)std::max<int64_t>(1, std::min(256 / tiles, std::min(piece, T) / 1024)) : 1;
     int64_t n = 0;
     if (half && grad) {
-      n = std::min<int64_t>(kMostPieces * ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 128) * ceil_div(h, 256), kMostPieceTiles) * 65536;       // w4_cut
+      n = std::min<int64_t>(std::min<int64_t>(kMostPieces, ceil_div(V, 256)) * ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 128) * ceil_div(h, 256), kMostPieceTiles) * 65536;       // w4_cut
       if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
       if (pieces > 1) n += V * h;
     }
@@ -711,6 +713,9 @@ struct CeLayout {
       dx_k = (int)(ceil_div(ceil_div(V, most), 64) * 64);
       dx_splits = (int)ceil_div(V, dx_k);
       n = dx_splits * piece * h;
+      const int64_t of_table = ceil_div(V, 32) * ceil_div(h, 32);
+      if (pieces == 1) dw_splits = (int)std::max<int64_t>(1, std::min(1024 / of_table, T / 256));
+      if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
     }
     sums = take(4 * n);
     bytes = at;
@@ -723,7 +728,7 @@ mosaic_status launch_rows(hipStream_t s, int quota, W4Args p, bool low) {
     constexpr int MI = decltype(mi)::value;
     p.tiles_m = (int)ceil_div(p.M, 32 * MI);
     const int most = p.tiles_m * p.tiles_n;
-    p.tile_count = EPI == W4_PIECES && most <= kMostPieceTiles ? std::min(most * kMostPieces, kMostPieceTiles) : most;
+    p.tile_count = EPI == W4_PIECES && most <= kMostPieceTiles ? std::min((int)std::min<int64_t>(kMostPieces, ceil_div(p.K, 256)) * most, kMostPieceTiles) : most;
     p.row_block = row_block_for(p.K, p.M, 32 * MI);
     return launch_w4_epi<A_KC, B_KC, EPI, MI, W4_GROUPED>(s, quota, p);
   };
@@ -790,8 +795,9 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc + r0 * h * 4, h, table, h, Z, L.ld, nullptr, live, 1, capacity, 0));
       if (V <= 256 * 32) {
         const int grid = grid_for(quota, 8, some);
-        if (V <= 256 * 4) rows_f32_kernel<4><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
-        else rows_f32_kernel<32><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        if (V <= 64 * 2) rows_f32_kernel<64, 2><<<grid_for(quota, 32, some), 64, 0, s>>>(p, head, Z, L.ld, grad);
+        else if (V <= 256 * 4) rows_f32_kernel<256, 4><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        else rows_f32_kernel<256, 32><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
       } else {
         float2* const stats = (float2*)(base + L.stats);
         float* const totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
@@ -811,7 +817,18 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
         else join_kernel<float, true, 1><<<grid_for(quota, 8, ceil_div(words, 256)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX);
         MOSAIC_LAUNCH_CHECK();
       }
-      if (dtable) MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, false, false, (int)V, (int)h, some, Z, L.ld, Xc + r0 * h * 4, h, dtable, h, i ? dtable : nullptr, live, 1, capacity, 0));
+      if (dtable) {
+        const bool cut = L.dw_splits > 1;
+        MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, false, false, (int)V, (int)h, some, Z, L.ld, Xc + r0 * h * 4, h, cut ? sums : (float*)dtable, h, i ? dtable : nullptr, live, 1,
+                                      capacity, 0, 0, L.dw_splits));
+        if (cut) {
+          if (((uintptr_t)dtable & 15) == 0 && h % 4 == 0)
+            join_kernel<float, false, 4><<<grid_for(quota, 8, ceil_div(V * h, 1024)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable);
+          else
+            join_kernel<float, false, 1><<<grid_for(quota, 8, ceil_div(V * h, 256)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable);
+          MOSAIC_LAUNCH_CHECK();
+        }
+      }
       continue;
     }
     bf16* E = grad ? (bf16*)(base + L.e) : nullptr;
@@ -853,7 +870,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.rows = rows;
       d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
-      const int blocks = few_rows(some, h, V, 8.0 + w4_cut((int)w4_tiles(h), d.K).us);
+      const int blocks = few_rows(some, h, V, 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
       if (blocks) d.K = (int)V;                  // the rows of E are readable up to ld
       CeLoss now = add;
       if (L.pieces > 1) now.loss = nullptr;
