@@ -136,7 +136,7 @@ constexpr int kMaxGroups = 1024;
 // for).  Nanoseconds: 1450 for 64 k-values of a tile, 8000 around them; the sums of a tile written and read at 5 TB/s, 5000 for the pass that adds them.  Whole
 // numbers, so that the product and that pass come to the same cut.  Measured: 6144 x 4096 of 128000, 384 tiles: 5600 us in two rounds, 4400 as
 // three rounds of half the length; 187 x 216 of 85501, one tile: 106 us in 16 pieces, 29 in 122.
-constexpr int kMostPieces = 128, kMostPieceTiles = 2048, kCuts = 40;
+constexpr int kMostPieces = 128, kMostPieceTiles = 2048, kLeastPiece = 256, kCuts = 40;
 struct W4Cut { int pieces, k; };
 // candidate i: 1 to 16, then eight of even steps up to every doubling
 __device__ __host__ __forceinline__ int w4_cut_pieces(int i) { return i < 16 ? i + 1 : (18 + 2 * ((i - 16) & 7)) << ((i - 16) >> 3); }
@@ -146,7 +146,7 @@ __device__ __host__ __forceinline__ W4Cut w4_cut_of(int i, int K) {
 }
 __device__ __host__ __forceinline__ int64_t w4_cut_ns(int i, int tiles, int K) {
   const W4Cut cut = w4_cut_of(i, K);
-  if (i && (cut.k < 256 || (int64_t)w4_cut_pieces(i) * tiles > kMostPieceTiles)) return INT64_MAX >> 8;
+  if (i && (cut.k < kLeastPiece || (int64_t)w4_cut_pieces(i) * tiles > kMostPieceTiles)) return INT64_MAX >> 8;
   return ((int64_t)tiles * cut.pieces + 255) / 256 * (cut.k / 64 * (int64_t)1450 + 8000) + (i ? (int64_t)tiles * (8 * cut.pieces + 2) * 13 + 5000 : 0);
 }
 inline float w4_cut_us(int tiles, int K) {
