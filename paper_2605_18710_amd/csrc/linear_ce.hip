@@ -42,20 +42,34 @@ struct CeList {
   int32_t* slot;           // of a token: its place in that order, or -1
 };
 
-// One workgroup: 16 waves in order, lanes in order.  `write`: to memory; each(t, at) for every token a thread looks at, at < 0 where it does not count.
-constexpr int kListThreads = 1024;
+// One workgroup: 16 waves in order, 512 tokens of a turn each, eight to a lane (with one to a lane a barrier for every 1024 tokens: 15 us of 14313, now 7).
+// `write`: to memory; each(t, at) for every token a thread looks at, at < 0 where it does not count.
+constexpr int kListThreads = 1024, kListEach = 8;
 template <typename F>
 __device__ __forceinline__ void list_tokens(const CeList& l, bool write, F each) {
   constexpr int kWaves = kListThreads / 64;
   __shared__ int wave_count[2][kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int run = 0, y = (int)threadIdx.x < l.T ? l.targets[threadIdx.x] : -1;
-  for (int t0 = 0, turn = 0; t0 < l.T; t0 += kListThreads, turn ^= 1) {
-    const int t = t0 + threadIdx.x, here = y;
-    y = t + kListThreads < l.T ? l.targets[t + kListThreads] : -1;       // its latency passes under this turn
-    const bool counts = here >= 0 && here < l.V;
-    const unsigned long long m = __ballot(counts);
-    if (lane == 0) wave_count[turn][wave] = __popcll(m);
+  int run = 0, y[kListEach];
+  auto look = [&](int t0) {
+#pragma unroll
+    for (int j = 0; j < kListEach; ++j) {
+      const int64_t t = (int64_t)t0 + 64 * (kListEach * wave + j) + lane;
+      y[j] = t < l.T ? l.targets[t] : -1;
+    }
+  };
+  look(0);
+  for (int64_t t0 = 0, turn = 0; t0 < l.T; t0 += kListThreads * kListEach, turn ^= 1) {
+    int here[kListEach], mine[kListEach], all = 0;       // tokens of the wave that count: before the lane's own, all
+#pragma unroll
+    for (int j = 0; j < kListEach; ++j) {
+      here[j] = y[j] >= 0 && y[j] < l.V ? y[j] : -1;
+      const unsigned long long m = __ballot(here[j] >= 0);
+      mine[j] = all + __popcll(m & ((1ull << lane) - 1ull));
+      all += __popcll(m);
+    }
+    look((int)min(t0 + kListThreads * kListEach, (int64_t)l.T));         // its latency passes under this turn
+    if (lane == 0) wave_count[turn][wave] = all;
     __syncthreads();                             // the other half of wave_count was read before the barrier of the turn before
     int before = run;
 #pragma unroll
@@ -64,9 +78,13 @@ __device__ __forceinline__ void list_tokens(const CeList& l, bool write, F each)
       if (w < wave) before += n;
       run += n;
     }
-    const int at = counts ? before + __popcll(m & ((1ull << lane) - 1ull)) : -1;
-    if (write && counts) { l.rows[at] = t; l.target[at] = here; }
-    if (t < l.T) each(t, at);
+#pragma unroll
+    for (int j = 0; j < kListEach; ++j) {
+      const int64_t t = t0 + 64 * (kListEach * wave + j) + lane;
+      const int at = here[j] >= 0 ? before + mine[j] : -1;
+      if (write && at >= 0) { l.rows[at] = (int)t; l.target[at] = here[j]; }
+      if (t < l.T) each((int)t, at);
+    }
   }
   if (!write) return;
   const int n = l.balanced ? max(1, (int)(((int64_t)run + l.piece - 1) / l.piece)) : l.pieces;
@@ -98,8 +116,8 @@ __global__ __launch_bounds__(256) void place_kernel(const int32_t* __restrict__ 
                                                     T* __restrict__ dX, float* __restrict__ losses) {
   for (int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); t < tokens; t += (int64_t)gridDim.x * 4) place_row<T, V>(t, slot[t], X, h, Xc, dX, losses);
 }
-// Both in one launch up to kListMax tokens: every workgroup makes the list for itself (a turn of 1024 tokens takes a microsecond, a launch four),
-// the first one writes it.
+// Both in one launch up to kListMax tokens: every workgroup makes the list for itself (one turn, where a launch takes four microseconds), the first one
+// writes it.
 constexpr int kListMax = 8192;
 template <typename T, int V>
 __global__ __launch_bounds__(kListThreads) void list_place_kernel(CeList l, const T* __restrict__ X, int64_t h, T* __restrict__ Xc, T* __restrict__ dX,
@@ -190,7 +208,7 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
 // -1 and not rounded at all): a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
 constexpr int kStrip = 1024;
 template <bool PAST, bool JOIN>
-__global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld) {
+__global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld) {
   // JOIN: every workgroup joins its rows' blocks itself, of which there are at most kJoinBlocks, and no launch does before
   __shared__ float top_of[4][16], sum_of[4][16], total_of[4][16], lse_of[16];
   const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
@@ -211,9 +229,21 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __re
       scale[i] = stats[(int64_t)(col / kCeBlock) * p.capacity + row].x;
       hit[i] = p.target[start + row] - col;
     }
+    float own[8];                                // the target's logit, where a lane has its column: all asked for before the first is waited for
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = r0 + 2 * i + (threadIdx.x >> 7);
+      own[i] = 0.f;
+      if (row < live && col < ld && hit[i] >= 0 && hit[i] < 8) own[i] = p.at_target[row];
+    }
     if constexpr (JOIN) {
       const int r = threadIdx.x & 15, wave = threadIdx.x >> 6, row = r0 + r, blocks = (p.V + kCeBlock - 1) / kCeBlock;
+      const bool tells = c0 == 0 && threadIdx.x < 16 && row < live;        // the rows' losses
+      int token = 0;
+      float at_target = 0.f;
+      if (tells) { token = p.rows[start + row]; at_target = p.at_target[row]; }
       float top = -INFINITY, sum = 0.f, total = 0.f;
+#pragma unroll 4
       for (int b = threadIdx.x >> 4; b < blocks; b += 16) {
         const float2 x = stats[(int64_t)b * p.capacity + row];
         join_sums(top, sum, x.x, x.y);
@@ -232,7 +262,7 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __re
         for (int w = 1; w < 4; ++w) { join_sums(top, sum, top_of[w][r], sum_of[w][r]); total += total_of[w][r]; }
         const float all = top + __builtin_amdgcn_logf(sum);
         lse_of[r] = all;
-        if (c0 == 0 && row < live) p.losses[p.rows[start + row]] = token_loss(all, p.at_target[row], total, p.smoothing, p.V);
+        if (tells) p.losses[token] = token_loss(all, at_target, total, p.smoothing, p.V);
       }
       __syncthreads();
 #pragma unroll
@@ -249,7 +279,7 @@ __global__ __launch_bounds__(256) void grad_kernel(CePiece p, const float2* __re
       for (int e = 0; e < 8; ++e) o.set(e, col + e < p.V ? (float)v[i][e] * f - even : 0.f);
       if (hit[i] >= 0 && hit[i] < 8) {
         // the target's probability from its own logit: 1 - p keeps its digits where p is near 1
-        const float d = (__builtin_amdgcn_exp2f(fmaf(p.at_target[row], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even);
+        const float d = (__builtin_amdgcn_exp2f(fmaf(own[i], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even);
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (e == hit[i]) o.set(e, d);
       }
@@ -416,7 +446,13 @@ struct CeLoss { const float* losses; int T; const CeHead* head; float* loss; };
 template <int NT>
 __device__ __forceinline__ void add_losses(const CeLoss& l, double* part) {
   double sum = 0.0;
-  for (int t = threadIdx.x; t < l.T; t += NT) sum += (double)l.losses[t];
+  for (int64_t t0 = threadIdx.x; t0 < l.T; t0 += 8 * NT) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = t0 + u * NT < l.T ? l.losses[t0 + u * NT] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += (double)v[u];
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
@@ -428,16 +464,33 @@ __device__ __forceinline__ void add_losses(const CeLoss& l, double* part) {
   }
   __syncthreads();
 }
-// the last workgroup also adds the losses, where there are no more pieces (loss not null)
-template <int RB>
-__global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l) {
+// dX, and (TABLE) dtable in the same launch: 375 x 33 of 72: two launches 11.7 us, one 7.6.  The last workgroup also adds the losses, where there are no more
+// pieces (loss not null).
+__device__ __forceinline__ void few_dtable(const W4Args& p, int64_t item, unsigned char* smem) {
+  const int live = p.offsets[1], start = p.piece[0], cols = (p.N + 63) / 64, m0 = (int)(item / cols) * 64, n0 = (int)(item % cols) * 64;
+  const float scale = *p.scale;
+  few_tile<false, false, 4>(p.A, p.lda, m0, p.M, p.B + (int64_t)start * p.ldb, p.ldb, n0, p.N, live, smem, [&](int row, int col, const float (&v)[8]) {
+    bf16x8 o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
+    if (row < p.M && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
+  });
+}
+constexpr int kBothItems = 512;
+__device__ __host__ __forceinline__ int64_t few_dtable_items(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); }
+template <int RB, bool TABLE>
+__global__ __launch_bounds__(kFewNT, TABLE ? 2 : few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l, W4Args w) {
   extern __shared__ __align__(16) unsigned char smem[];
   if (l.loss && blockIdx.x == gridDim.x - 1) add_losses<kFewNT>(l, reinterpret_cast<double*>(smem));
   const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
   const float scale = *p.scale;
-  const int64_t items = (int64_t)tiles_m * ((p.N + 63) / 64);
+  const int64_t first = TABLE ? few_dtable_items(w.M, w.N) : 0, items = first + (int64_t)tiles_m * ((p.N + 63) / 64);
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int n0 = (int)(item / tiles_m) * 64, m0 = (int)(item % tiles_m) * 16 * RB;
+    if (TABLE && item < first) {                 // their contraction is the longer one as a rule
+      few_dtable(w, item, smem);
+      continue;
+    }
+    const int n0 = (int)((item - first) / tiles_m) * 64, m0 = (int)((item - first) % tiles_m) * 16 * RB;
     few_tile<true, false, RB>(p.A, p.lda, m0, live, p.B, p.ldb, n0, p.N, p.K, smem, [&](int row, int col, const float (&v)[8]) {
       bf16x8 o;
 #pragma unroll
@@ -448,27 +501,26 @@ __global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_dx_kernel(W4Args p,
 }
 __global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p) {
   extern __shared__ __align__(16) unsigned char smem[];
-  const int live = p.offsets[1], start = p.piece[0], cols = (p.N + 63) / 64;
-  const float scale = *p.scale;
-  const int64_t items = (int64_t)((p.M + 63) / 64) * cols;
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int m0 = (int)(item / cols) * 64, n0 = (int)(item % cols) * 64;
-    few_tile<false, false, 4>(p.A, p.lda, m0, p.M, p.B + (int64_t)start * p.ldb, p.ldb, n0, p.N, live, smem, [&](int row, int col, const float (&v)[8]) {
-      bf16x8 o;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
-      if (row < p.M && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
-    });
-  }
+  for (int64_t item = blockIdx.x; item < few_dtable_items(p.M, p.N); item += gridDim.x) few_dtable(p, item, smem);
 }
-template <int RB, bool LOGITS, typename... MORE>
-mosaic_status launch_few_rows(hipStream_t s, int quota, int most, const W4Args& p, MORE... more) {
+template <int RB>
+mosaic_status launch_few_logits(hipStream_t s, int quota, int most, const W4Args& p) {
   static std::once_flag once;
   static hipError_t rc = hipSuccess;
-  constexpr int kLds = few_lds<true, LOGITS, RB>();
-  auto kern = [] { if constexpr (LOGITS) return few_logits_kernel<RB>; else return few_dx_kernel<RB>; }();
-  MOSAIC_TRY(few_allow_lds(kern, kLds, &once, &rc));
-  kern<<<grid_for(quota, RB == 1 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p, more...);
+  constexpr int kLds = few_lds<true, true, RB>();
+  MOSAIC_TRY(few_allow_lds(few_logits_kernel<RB>, kLds, &once, &rc));
+  few_logits_kernel<RB><<<grid_for(quota, RB == 1 ? 2 : 1, ceil_div(most, 16 * RB) * ceil_div(p.N, 64)), kFewNT, kLds, s>>>(p);
+  MOSAIC_LAUNCH_CHECK();
+  return MOSAIC_OK;
+}
+template <int RB, bool TABLE>
+mosaic_status launch_few_dx(hipStream_t s, int quota, int most, const W4Args& p, const CeLoss& l, const W4Args& w) {
+  static std::once_flag once;
+  static hipError_t rc = hipSuccess;
+  constexpr int kLds = std::max(few_lds<true, false, RB>(), TABLE ? few_lds<false, false, 4>() : 0);
+  MOSAIC_TRY(few_allow_lds(few_dx_kernel<RB, TABLE>, kLds, &once, &rc));
+  const int64_t items = ceil_div(most, 16 * RB) * ceil_div(p.N, 64) + (TABLE ? few_dtable_items(w.M, w.N) : 0);
+  few_dx_kernel<RB, TABLE><<<grid_for(quota, RB == 1 && !TABLE ? 2 : 1, items), kFewNT, kLds, s>>>(p, l, w);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -633,10 +685,13 @@ __global__ __launch_bounds__(1024) void few_join_kernel(CeFew p) {
 }
 
 // ------------------------------------------------------------------------------- joins
-// out[r] = sum over the pieces in ascending order, rows of N elements; TO_ROWS: those of the span, to the tokens' rows
+// out[r] = sum over the pieces in ascending order, rows of N elements; TO_ROWS: those of the span, to the tokens' rows, and the last workgroup adds
+// the losses (loss not null)
 template <typename T, bool TO_ROWS, int V = 4>
 __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, int splits, int64_t M, int64_t N, const float* __restrict__ scale, int height, int K, const CeSpan* __restrict__ span,
-                                                   const int32_t* __restrict__ to, T* __restrict__ out) {
+                                                   const int32_t* __restrict__ to, T* __restrict__ out, CeLoss l) {
+  __shared__ double part[4];
+  if (TO_ROWS && l.loss && blockIdx.x == gridDim.x - 1) add_losses<256>(l, part);
   const int64_t rows = TO_ROWS ? span->live : M, pieces = N / V, items = rows * pieces, start = TO_ROWS ? span->start : 0;
   if (TO_ROWS && height) {                       // as the product cut itself: in tiles of `height` rows
     const int tiles_m = (int)(rows + height - 1) / height;
@@ -663,7 +718,7 @@ __global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ P, 
   }
 }
 
-constexpr int kLossThreads = kFewNT;             // the order of the sum is few_dx_kernel's
+constexpr int kLossThreads = 1024;
 __global__ __launch_bounds__(kLossThreads) void loss_kernel(CeLoss l) {
   __shared__ double part[kLossThreads / 64];
   add_losses<kLossThreads>(l, part);
@@ -780,6 +835,8 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
   if (half) MOSAIC_TRY(wide ? place(bf16(), std::integral_constant<int, 8>()) : place(bf16(), One()));
   else MOSAIC_TRY(wide ? place(float(), std::integral_constant<int, 4>()) : place(float(), One()));
   float* const sums = (float*)(base + L.sums);
+  // added by a launch that has the time, or by one of its own: up to this many tokens that takes 3 us of the workgroup that does
+  constexpr int kAddMax = 16384;
   const CeLoss add = {losses, (int)T, head, loss};
   bool added = false;
   for (int i = 0; i < L.pieces; ++i) {
@@ -787,6 +844,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     const int capacity = (int)L.piece, some = (int)std::min(L.piece, std::max<int64_t>(T - (half ? 0 : r0), 1));      // at most that many rows
     const char* Xc = base + L.x;                 // of all tokens
     const int32_t* live = &spans[i].zero;        // 0 and how many
+    const CeLoss now = {losses, (int)T, head, i + 1 == L.pieces && T <= kAddMax ? loss : nullptr};
     CePiece p = {};
     p.span = spans + i; p.rows = rows; p.target = target; p.at_target = (float*)(base + L.at_target);
     p.capacity = capacity; p.V = (int)V; p.smoothing = smoothing; p.lse = (float*)(base + L.lse); p.losses = losses;
@@ -813,8 +871,9 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       if (dX) {
         MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, false, some, (int)h, (int)V, Z, L.ld, table, h, sums, h, nullptr, live, 1, capacity, 0, L.dx_k, L.dx_splits));
         const int64_t words = some * h;
-        if (wide) join_kernel<float, true, 4><<<grid_for(quota, 8, ceil_div(words, 1024)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX);
-        else join_kernel<float, true, 1><<<grid_for(quota, 8, ceil_div(words, 256)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX);
+        if (wide) join_kernel<float, true, 4><<<grid_for(quota, 8, ceil_div(words, 1024)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX, now);
+        else join_kernel<float, true, 1><<<grid_for(quota, 8, ceil_div(words, 256)), 256, 0, s>>>(sums, L.dx_splits, some, h, nullptr, 0, 0, p.span, rows, (float*)dX, now);
+        added = now.loss != nullptr;
         MOSAIC_LAUNCH_CHECK();
       }
       if (dtable) {
@@ -823,9 +882,9 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
                                       capacity, 0, 0, L.dw_splits));
         if (cut) {
           if (((uintptr_t)dtable & 15) == 0 && h % 4 == 0)
-            join_kernel<float, false, 4><<<grid_for(quota, 8, ceil_div(V * h, 1024)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable);
+            join_kernel<float, false, 4><<<grid_for(quota, 8, ceil_div(V * h, 1024)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable, {});
           else
-            join_kernel<float, false, 1><<<grid_for(quota, 8, ceil_div(V * h, 256)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable);
+            join_kernel<float, false, 1><<<grid_for(quota, 8, ceil_div(V * h, 256)), 256, 0, s>>>(sums, L.dw_splits, V, h, nullptr, 0, 0, nullptr, nullptr, (float*)dtable, {});
           MOSAIC_LAUNCH_CHECK();
         }
       }
@@ -844,9 +903,9 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     auto w4_tiles = [&](int64_t N) { return (double)(ceil_div(some, low ? 128 : 256) * ceil_div(N, 256)); };
     // 8 us for the epilogue of a round: 375 x 33 of 72, four-wave kernel 20.7 us, few_tile 5.3
     switch (few_rows(some, V, h, w4_price(w4_tiles(V), (double)h, low) + 8.0 * std::ceil(w4_tiles(V) / 256.0))) {
-      case 1: MOSAIC_TRY((launch_few_rows<1, true>(s, quota, some, z))); break;
-      case 2: MOSAIC_TRY((launch_few_rows<2, true>(s, quota, some, z))); break;
-      case 4: MOSAIC_TRY((launch_few_rows<4, true>(s, quota, some, z))); break;
+      case 1: MOSAIC_TRY(launch_few_logits<1>(s, quota, some, z)); break;
+      case 2: MOSAIC_TRY(launch_few_logits<2>(s, quota, some, z)); break;
+      case 4: MOSAIC_TRY(launch_few_logits<4>(s, quota, some, z)); break;
       default: MOSAIC_TRY((launch_rows<true, true, W4_SOFTMAX>(s, quota, z, low)));
     }
     const bool join = grad && L.blocks <= kJoinBlocks;
@@ -861,6 +920,20 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     else if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
     else grad_kernel<false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
     MOSAIC_LAUNCH_CHECK();
+    W4Args w = {};
+    bool few_table = false;
+    if (dtable) {
+      w.A = E; w.B = (const bf16*)Xc; w.C = (bf16*)dtable;
+      w.M = (int)V; w.N = (int)h; w.K = capacity; w.lda = L.ld; w.ldb = h; w.ldc = h;
+      w.offsets = live; w.piece = &spans[i].start; w.groups = 1; w.bound = capacity;
+      w.tiles_m = (int)ceil_div(V, 256); w.tiles_n = (int)ceil_div(h, 256);
+      w.tile_count = w.tiles_m * w.tiles_n;
+      w.row_block = row_block_for(w.K, V, 256);
+      w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
+      w.splits = L.dw_splits;
+      const double w4_us = w4_price((double)w.tile_count * L.dw_splits, (double)some / L.dw_splits, false) + (L.dw_splits > 1 ? 5.0 + (double)(V * h) * (4 * L.dw_splits + 2) / 5e6 : 0.0);
+      few_table = L.pieces == 1 && few_price((double)few_dtable_items(V, h), (double)some, 4, false) < w4_us;
+    }
     if (dX) {
       W4Args d = {};
       d.A = E; d.B = (const bf16*)table; d.C = (bf16*)dX;
@@ -872,48 +945,40 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
       const int blocks = few_rows(some, h, V, 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
-      if (blocks) d.K = (int)V;                  // the rows of E are readable up to ld
-      CeLoss now = add;
-      if (L.pieces > 1) now.loss = nullptr;
-      added = blocks && now.loss;
-      switch (blocks) {
-        case 1: MOSAIC_TRY((launch_few_rows<1, false>(s, quota, some, d, now))); break;
-        case 2: MOSAIC_TRY((launch_few_rows<2, false>(s, quota, some, d, now))); break;
-        case 4: MOSAIC_TRY((launch_few_rows<4, false>(s, quota, some, d, now))); break;
-        default:
-          MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
-          if (d.K > kLeastPiece) {               // or there is one piece, which went where it belongs
-            join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX);
-            MOSAIC_LAUNCH_CHECK();
-          }
+      if (blocks) {
+        d.K = (int)V;                            // the rows of E are readable up to ld
+        const bool both = few_table && ceil_div(some, 16 * blocks) * ceil_div(h, 64) + few_dtable_items(V, h) <= kBothItems;
+        auto go = [&](auto rb) -> mosaic_status {
+          constexpr int RB = decltype(rb)::value;
+          return both ? launch_few_dx<RB, true>(s, quota, some, d, now, w) : launch_few_dx<RB, false>(s, quota, some, d, now, w);
+        };
+        MOSAIC_TRY(blocks == 1 ? go(std::integral_constant<int, 1>{}) : blocks == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{}));
+        added = now.loss != nullptr;
+        if (both) continue;
+      } else {
+        MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
+        if (d.K > kLeastPiece) {                 // or there is one piece, which went where it belongs
+          join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX, now);
+          MOSAIC_LAUNCH_CHECK();
+          added = now.loss != nullptr;
+        }
       }
     }
-    if (dtable) {
-      W4Args w = {};
-      w.A = E; w.B = (const bf16*)Xc; w.C = (bf16*)dtable;
-      w.M = (int)V; w.N = (int)h; w.K = capacity; w.lda = L.ld; w.ldb = h; w.ldc = h;
-      w.offsets = live; w.piece = &spans[i].start; w.groups = 1; w.bound = capacity;
-      w.tiles_m = (int)ceil_div(V, 256); w.tiles_n = (int)ceil_div(h, 256);
-      w.tile_count = w.tiles_m * w.tiles_n;
-      w.row_block = row_block_for(w.K, V, 256);
-      w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
-      w.splits = L.dw_splits;
-      const double w4_us = w4_price((double)w.tile_count * L.dw_splits, (double)some / L.dw_splits, false) + (L.dw_splits > 1 ? 5.0 + (double)(V * h) * (4 * L.dw_splits + 2) / 5e6 : 0.0);
-      if (L.pieces == 1 && few_price((double)(ceil_div(V, 64) * ceil_div(h, 64)), (double)some, 4, false) < w4_us) {
-        static std::once_flag once;
-        static hipError_t rc = hipSuccess;
-        constexpr int kLds = few_lds<false, false, 4>();
-        MOSAIC_TRY(few_allow_lds(few_dtable_kernel, kLds, &once, &rc));
-        few_dtable_kernel<<<grid_for(quota, 1, ceil_div(V, 64) * ceil_div(h, 64)), kFewNT, kLds, s>>>(w);
-        MOSAIC_LAUNCH_CHECK();
-      } else if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
-      else if (L.dw_splits > 1) {
-        w.tile_count *= w.splits;
-        MOSAIC_TRY((launch_w4_epi<false, false, W4_PIECES, 8, W4_GROUPED>(s, quota, w)));
-        join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, w.scale, 0, 0, nullptr, nullptr, (bf16*)dtable);
-        MOSAIC_LAUNCH_CHECK();
-      } else MOSAIC_TRY((launch_w4_epi<false, false, W4_PLAIN, 8, W4_GROUPED>(s, quota, w)));
-    }
+    if (!dtable) continue;
+    if (few_table) {
+      static std::once_flag once;
+      static hipError_t rc = hipSuccess;
+      constexpr int kLds = few_lds<false, false, 4>();
+      MOSAIC_TRY(few_allow_lds(few_dtable_kernel, kLds, &once, &rc));
+      few_dtable_kernel<<<grid_for(quota, 1, few_dtable_items(V, h)), kFewNT, kLds, s>>>(w);
+      MOSAIC_LAUNCH_CHECK();
+    } else if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
+    else if (L.dw_splits > 1) {
+      w.tile_count *= w.splits;
+      MOSAIC_TRY((launch_w4_epi<false, false, W4_PIECES, 8, W4_GROUPED>(s, quota, w)));
+      join_kernel<bf16, false><<<grid_for(quota, 8, ceil_div(V * (h / 4), 256)), 256, 0, s>>>(sums, w.splits, V, h, w.scale, 0, 0, nullptr, nullptr, (bf16*)dtable, {});
+      MOSAIC_LAUNCH_CHECK();
+    } else MOSAIC_TRY((launch_w4_epi<false, false, W4_PLAIN, 8, W4_GROUPED>(s, quota, w)));
   }
   if (!added) {
     loss_kernel<<<1, kLossThreads, 0, s>>>(add);
