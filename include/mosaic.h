@@ -540,8 +540,9 @@ size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t 
  * them may be NULL).  Logits are fp32; bf16: the logits' gradient is rounded to bf16 before the products that dX and dtable are (formed of probabilities kept in fp16 relative to the
  * largest of 64).  What lies between is kept in
  * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
- * it holds the logits' exponentials for as many tokens at a time as 2^30 of them (2 GiB in bf16) belong to.  bf16: h a multiple of 8 and all tensors 16-byte aligned
- * (MOSAIC_EUNSUPPORTED otherwise); the table is smaller than 4 GiB. */
+ * it holds what is left of the logits for as many tokens at a time as 2 GiB hold (bf16: of all tokens, where that wants no more room than several such pieces and the
+ * fp32 sums of dtable that they need).  bf16: h a multiple of 8 and all tensors 16-byte aligned; the table is smaller than 4 GiB, V at most 2^22, h 2^20, T 2^30
+ * (MOSAIC_EUNSUPPORTED otherwise). */
 size_t        mosaic_op_linear_ce_fwd_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
 size_t        mosaic_op_linear_ce_grad_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
 mosaic_status mosaic_op_linear_ce_fwd(void* stream, int32_t quota, int32_t dtype, int64_t T, int64_t h, int64_t V,

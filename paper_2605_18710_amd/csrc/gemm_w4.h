@@ -1,4 +1,4 @@
-// What the matrix-core kernels of gemm.hip and grouped.hip share: the order of a product's tiles, and the four-wave kernel.
+// What the matrix-core kernels of gemm.hip, grouped.hip and linear_ce.hip share: the order of a product's tiles, and the four-wave kernel.
 #pragma once
 #include "activations.h"
 #include "common.h"
