@@ -15,6 +15,7 @@
 // twice the flops per LDS byte (rule and figures in launch_t).
 // A decoder layer of 256 rows, width 128, MLP 384 (forward, loss, backward): 19 launches, 92.8 us -> 14, 62.3.
 #include <algorithm>
+#include <mutex>
 #include <type_traits>
 #include "activations.h"
 #include "kernels.h"
@@ -525,11 +526,170 @@ struct F32Groups {
   int64_t stride;            // elements between two groups' B, or C
   int splits, split_k;       // one group: the contraction in pieces of split_k (K-strided A: as equal ones as whole K-tiles make), each with a C of its own, M rows
 };
+
+// An operand of f32_block: BX rows (KC: K contiguous) or columns, in K-tiles of 32.  Requests are unconditional, through a descriptor that ends
+// with the operand, so that the compiler counts them and waits for each only where it is used.  LDS: [row][k], or [k][column], whose two lane groups'
+// reads touch 32 banks each.
+template <int BX, bool KC>
+struct F32Panel {
+  static constexpr int KS = 32, NCH = BX * KS / 1024, PITCH = KC ? KS + 4 : BX + 8, FLOATS = (KC ? BX : KS) * PITCH;
+  unsigned voff[NCH];
+  int kofs;                                // KC: of the lane's pieces in the K-tile
+  uint64_t base, left;                     // of the next K-tile to be requested: its address, bytes from there to the operand's end
+  uint32_t step;
+  int k_left;
+  __device__ __forceinline__ static uint64_t uniform(uint64_t x) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+  }
+  __device__ __forceinline__ void init(const float* p, int64_t ld, int x0, int X, int K) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int q = threadIdx.x + 256 * i;
+      voff[i] = KC ? (unsigned)(q / (KS / 4) * ld * 4 + q % (KS / 4) * 16) : (unsigned)(q / (BX / 4) * ld * 4 + q % (BX / 4) * 16);
+    }
+    kofs = threadIdx.x % (KS / 4) * 4;
+    // whole 16-byte pieces: a row has them
+    const int64_t all = KC ? (int64_t)(X - 1 - x0) * ld + (K + 3) / 4 * 4 : (int64_t)(K - 1) * ld + (X + 3) / 4 * 4 - x0;
+    base = uniform((uint64_t)(p + (KC ? (int64_t)x0 * ld : x0)));
+    left = uniform(K > 0 ? (uint64_t)all * 4 : 0);
+    step = KC ? KS * 4 : (uint32_t)__builtin_amdgcn_readfirstlane((int)(KS * ld * 4));
+    k_left = __builtin_amdgcn_readfirstlane(K);
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t desc() const {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(uint32_t)(left < 0xFFFFFFF0u ? left : 0xFFFFFFF0u), 0x00020000);
+  }
+  __device__ __forceinline__ f32x4 request(__amdgpu_buffer_rsrc_t d, int i) const {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, KC && kofs >= k_left ? kOutside : (int)voff[i], 0, 0));
+  }
+  __device__ __forceinline__ void advance() {
+    base += step;
+    left = left > step ? left - step : 0;
+    k_left -= KS;
+  }
+  __device__ __forceinline__ static void put(float* lds, int i, f32x4 v) {
+    constexpr int W = (KC ? KS : BX) / 4;
+    const int q = threadIdx.x + 256 * i;
+    *reinterpret_cast<f32x4*>(lds + q / W * PITCH + q % W * 4) = v;
+  }
+  // k-values 8 ks + 4 g .. + 3 of row x
+  __device__ __forceinline__ static f32x4 frag(const float* lds, int x, int ks, int g) {
+    if constexpr (KC) return *reinterpret_cast<const f32x4*>(lds + x * PITCH + 8 * ks + 4 * g);
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = lds[(8 * ks + 4 * g + e) * PITCH + x];
+    return v;
+  }
+};
+
+// A tile of BM x BN, 64 or 128 each, of fp32 tensors in rows of whole 16-byte pieces: four waves, a quarter each in blocks of 32 x 32.
+// What bounds it: the matrix cores, 157 TFLOP/s in fp32, as long as nothing stands in a wave's way between two instructions, of which a SIMD has one or two waves.
+// K-tile t is multiplied from stage t % 2 while t + 1 goes from registers to the other stage and t + 2 comes from memory, every access in a slot behind a
+// matrix instruction (64 cycles), the fragments eight k-values ahead; one barrier a K-tile, ahead of its last eight k-values.  4096 x 1024, K 4096: 259 us
+// (133 TFLOP/s) by 128 x 128, 289 by 64 x 64; with gemm_f32_tile's loop 306 and 330, whose requests stand in branches.  Four K-tiles under way: as fast.
+template <int BM, int BN, bool A_KC, bool B_KC>
+__device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds) {
+  typedef __attribute__((ext_vector_type(16))) float f32x16;
+  typedef F32Panel<BM, A_KC> PA;
+  typedef F32Panel<BN, B_KC> PB;
+  constexpr int WM = BM / 64, WN = BN / 64, KS = PA::KS, STEPS = KS / 8, STAGE = PA::FLOATS + PB::FLOATS, NA = PA::NCH, NP = NA + PB::NCH, NM = 4 * WM * WN;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 31, g = lane >> 5;
+  const int wm = (wave >> 1) * (BM / 2), wn = (wave & 1) * (BN / 2);
+  const int tn = tile / p.tiles_m, tm = tile - tn * p.tiles_m, m0 = tm * BM, n0 = tn * BN, K = __builtin_amdgcn_readfirstlane(p.K);
+  PA pa; PB pb;
+  pa.init((const float*)p.A, p.lda, m0, p.M, K);
+  pb.init((const float*)p.B, p.ldb, n0, p.N, K);
+  f32x4 held[2][NP], fa[2][WM], fb[2][WN];
+  f32x16 acc[WM][WN];
+#pragma unroll
+  for (int i = 0; i < WM; ++i)
+#pragma unroll
+    for (int j = 0; j < WN; ++j) acc[i][j] = f32x16{};
+  auto read = [&](int st, int ks, int u) {             // unit u of the fragments of step ks
+    const float* const a = lds + st * STAGE;
+    if (u < WM) fa[ks & 1][u] = PA::frag(a, wm + 32 * u + lr, ks, g);
+    else fb[ks & 1][u - WM] = PB::frag(a + PA::FLOATS, wn + 32 * (u - WM) + lr, ks, g);
+  };
+  auto put = [&](int st, int u) {
+    if (u < NA) PA::put(lds + st * STAGE, u, held[st][u]);
+    else PB::put(lds + st * STAGE + PA::FLOATS, u - NA, held[st][u]);
+  };
+  auto request_all = [&](int set) {
+    const auto da = pa.desc(), db = pb.desc();
+#pragma unroll
+    for (int u = 0; u < NP; ++u) held[set][u] = u < NA ? pa.request(da, u) : pb.request(db, u - NA);
+    pa.advance();
+    pb.advance();
+  };
+  request_all(0);
+  request_all(1);
+#pragma unroll
+  for (int u = 0; u < NP; ++u) put(0, u);
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < WM + WN; ++u) read(0, 0, u);
+  auto k_tile = [&](auto stage) {
+    constexpr int U = decltype(stage)::value;
+    const auto da = pa.desc(), db = pb.desc();
+#pragma unroll
+    for (int ks = 0; ks < STEPS; ++ks) {
+      if (ks == STEPS - 1) __syncthreads();            // the other stage is written, this one read
+#pragma unroll
+      for (int q = 0; q < NM; ++q) {
+        const int e = q / (WM * WN), i = q / WN % WM, j = q % WN;
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(fb[ks & 1][j][e], fa[ks & 1][i][e], acc[i][j], 0, 0, 0);
+        // what this slot takes: the next fragments in the first half of a step, requests in the first step, stores to LDS in the second and third
+#pragma unroll
+        for (int u = 0; u < WM + WN; ++u)
+          if (q == u * (NM / 2) / (WM + WN)) {
+            if (ks < STEPS - 1) read(U, ks + 1, u);
+            else read(U ^ 1, 0, u);
+          }
+#pragma unroll
+        for (int u = 0; u < NP; ++u) {
+          if (ks == 0 && q == u * NM / NP) held[U][u] = u < NA ? pa.request(da, u) : pb.request(db, u - NA);
+          if (ks >= 1 && ks <= 2 && (ks - 1) * NM + q == u * 2 * NM / NP) put(U ^ 1, u);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    pa.advance();
+    pb.advance();
+  };
+  for (int k0 = 0;;) {
+    k_tile(std::integral_constant<int, 0>{});
+    if ((k0 += KS) >= K) break;
+    k_tile(std::integral_constant<int, 1>{});
+    if ((k0 += KS) >= K) break;
+  }
+  // acc[i][j][4 q + e] is row 32 i + lr, column 32 j + 8 q + 4 g + e
+  const float* R = (const float*)p.R;
+  float* C = (float*)p.C;
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+    const int row = m0 + wm + 32 * i + lr;
+    if (row >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = n0 + wn + 32 * j + 8 * q + 4 * g;
+        if (col >= p.N) continue;
+        f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+        if (R) v += *reinterpret_cast<const f32x4*>(R + (int64_t)row * p.ldc + col);
+        *reinterpret_cast<f32x4*>(C + (int64_t)row * p.ldc + col) = v;
+      }
+    }
+  }
+}
+template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC> constexpr int f32_group_lds() {
+  constexpr int KS = BM == 32 ? 64 : 32;
+  if (std::is_same<T, float>::value && VEC && BM > 32) return 2 * (F32Panel<BM, A_KC>::FLOATS + F32Panel<BN, B_KC>::FLOATS) * 4;
+  return 2 * (F32Tile<T, BM, KS, A_KC, VEC>::FLOATS + F32Tile<T, BN, KS, B_KC, VEC>::FLOATS) * 4;
+}
 constexpr int kGroupsAtOnce = 256;       // of which the first tiles are kept in LDS, a thread each
-template <typename T, int BT, int KS, bool A_KC, bool B_KC, bool VEC>
-__global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Groups gr) {
-  constexpr int STAGE = F32Tile<T, BT, KS, A_KC, VEC>::FLOATS + F32Tile<T, BT, KS, B_KC, VEC>::FLOATS;
-  __shared__ __align__(16) float lds[2 * STAGE];
+template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC>
+__global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_grouped_kernel(F32Gemm p, F32Groups gr) {
+  extern __shared__ __align__(16) float lds[];
   __shared__ int starts[kGroupsAtOnce + 1], wave_total[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // tiles of all groups are dealt out as one list, wherever the batches of groups end
@@ -541,7 +701,7 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
       lo = min(max(gr.offsets[g0 + tid], 0), gr.bound);
       n = max(min(max(gr.offsets[g0 + tid + 1], 0), gr.bound) - lo, 0);
     }
-    const int mine = tid < ng ? (A_KC ? (n + BT - 1) / BT : p.tiles_m) * p.tiles_n : 0;
+    const int mine = tid < ng ? (A_KC ? (n + BM - 1) / BM : p.tiles_m) * p.tiles_n : 0;
     int scan = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -571,7 +731,7 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
         q.B = (const T*)p.B + (g0 + a) * gr.stride;
         q.C = (T*)p.C + (int64_t)first * p.ldc;
         q.M = rows;
-        q.tiles_m = (rows + BT - 1) / BT;
+        q.tiles_m = (rows + BM - 1) / BM;
         if (gr.splits > 1) {
           const int k0 = piece * gr.split_k;
           q.A = (const T*)q.A + (int64_t)k0;
@@ -584,7 +744,7 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
         q.C = (T*)p.C + (g0 + a) * gr.stride;
         q.K = rows;
         if (gr.splits > 1) {
-          const int per = ((rows + gr.splits - 1) / gr.splits + KS - 1) / KS * KS, k0 = min(piece * per, rows);
+          const int per = ((rows + gr.splits - 1) / gr.splits + 63) / 64 * 64, k0 = min(piece * per, rows);
           q.A = (const T*)q.A + (int64_t)k0 * p.lda;
           q.B = (const T*)q.B + (int64_t)k0 * p.ldb;
           q.C = (T*)p.C + (int64_t)piece * p.M * p.ldc;
@@ -592,27 +752,65 @@ __global__ __launch_bounds__(256) void gemm_f32_grouped_kernel(F32Gemm p, F32Gro
         }
         if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
       }
-      gemm_f32_tile<T, BT, KS, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
+      if constexpr (std::is_same<T, float>::value && VEC && BM > 32) f32_block<BM, BN, A_KC, B_KC>(q, (int)(item - starts[a]), lds);
+      else gemm_f32_tile<T, BM, BM == 32 ? 64 : 32, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
     }
     before += all;
   }
 }
 
-template <typename T, bool A_KC, bool B_KC, bool VEC>
-mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
-  // Half a tile more for every group than its rows fill.  Tiles of 32 / of 64, us: input gradient of 2998 rows of 12 experts, 640 x 1000, 530 tiles of 64, 59 / 71, forward,
-  // 848, 59 / 58; 6000 rows, 640 x 640, 1000, 71 / 57; weight gradients of 4, 1024 x 1024, 1024, 57 / 47; of 8, 256 x 256, 128, 13 / 26.
-  const int64_t t64 = ceil_div(p.M, 64), n64 = ceil_div(p.N, 64);
-  const bool large = (A_KC ? (t64 + std::min<int64_t>(gr.groups, p.M) / 2) * n64 : t64 * n64 * gr.groups) * gr.splits >= 848;
-  const int bt = large ? 64 : 32;
-  const int64_t tm = ceil_div(p.M, bt), tn = ceil_div(p.N, bt), most = (A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups) * gr.splits;
+// Tiles of a grouped product and their price in microseconds on the whole device: tiles to a CU times what a tile's operations take of one, divided by the share of the
+// peak that they reach, and 8 around them.  A K-contiguous A: half a tile of rows more for every group than its rows fill, give or take sqrt(groups / 12).  K: of one
+// tile (groups' rows: their mean, the longest 2.5 times that).  Measured, tiles of 32 x 32 / 64 x 64 / 64 x 128 / 128 x 128, us (price):
+//   2998 rows of 12, 640 x 1000, input gradient 57 61 74 71 (56 60 73 61), forward 57 49 48 49 (58 52 50 47);  1038 of 3, 1728 x 4080, input gradient 234 165 161 253
+//   (232 149 141 256), weight gradient 207 137 146 141 (199 134 135 134);  500 x 2048, K 512 19 17 24 39 (20 17 25 39);  6065 of 5, input gradient, 152 columns, K 2192 56 79 78 139
+struct F32Choice { int bm, bn; double us; };
+F32Choice f32_choice(bool a_kc, int64_t M, int64_t N, double K, int64_t groups, int splits) {
+  struct Shape { int bm, bn; double share; };
+  constexpr Shape shapes[] = {{32, 32, 0.56}, {64, 64, 0.77}, {64, 128, 0.82}, {128, 64, 0.82}, {128, 128, 0.88}};
+  F32Choice best = {};
+  for (const Shape& t : shapes) {
+    const double cols = (double)ceil_div(N, t.bn) * splits, with = (double)std::min(groups, M);
+    const double items = cols * (!a_kc ? (double)(ceil_div(M, t.bm) * groups) : groups == 1 ? (double)ceil_div(M, t.bm) : (double)M / t.bm + 0.5 * with);
+    const double spread = a_kc && groups > 1 ? cols * std::sqrt(with / 12.0) : 0.0;
+    const double per = (std::ceil((items - spread) / 256.0) + std::ceil(items / 256.0) + std::ceil((items + spread) / 256.0)) / 3.0;
+    const double us = 8.0 + std::max(per, !a_kc && groups > 1 ? 2.5 : 1.0) * t.bm * t.bn * (K + 32.0) * 2.0 / 614e3 / t.share;
+    if (!best.bm || us < best.us) best = {t.bm, t.bn, us};
+  }
+  return best;
+}
+template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC>
+mosaic_status launch_grouped_tiles(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
+  static std::once_flag once;
+  static hipError_t rc = hipSuccess;
+  constexpr int kLds = f32_group_lds<T, BM, BN, A_KC, B_KC, VEC>();
+  auto kern = gemm_f32_grouped_kernel<T, BM, BN, A_KC, B_KC, VEC>;
+  std::call_once(once, [&] { rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, kLds); });
+  MOSAIC_HIP(rc);
+  const int64_t tm = ceil_div(p.M, BM), tn = ceil_div(p.N, BN), most = (A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups) * gr.splits;
   if (most > INT32_MAX / 2) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "too many output tiles");
   p.tiles_m = (int)tm; p.tiles_n = (int)tn;
-  const int grid = grid_for(quota, 4, most);
-  if (large) gemm_f32_grouped_kernel<T, 64, 32, A_KC, B_KC, VEC><<<grid, 256, 0, s>>>(p, gr);
-  else gemm_f32_grouped_kernel<T, 32, 64, A_KC, B_KC, VEC><<<grid, 256, 0, s>>>(p, gr);
+  kern<<<grid_for(quota, BM * BN > 64 * 64 ? 2 : 4, most), 256, kLds, s>>>(p, gr);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
+}
+template <typename T, bool A_KC, bool B_KC, bool VEC>
+mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
+  if constexpr (std::is_same<T, float>::value && VEC) {
+    const double K = A_KC ? (gr.splits > 1 ? gr.split_k : p.K) : (double)p.K / (gr.groups * gr.splits);
+    const F32Choice c = f32_choice(A_KC, p.M, p.N, K, gr.groups, gr.splits);
+    if (c.bm > 32 && std::max(p.lda, p.ldb) <= 1 << 21) {          // a descriptor's 32 bits reach over the tile's rows
+      if (c.bm == 128) return c.bn == 128 ? launch_grouped_tiles<T, 128, 128, A_KC, B_KC, VEC>(s, quota, p, gr) : launch_grouped_tiles<T, 128, 64, A_KC, B_KC, VEC>(s, quota, p, gr);
+      return c.bn == 128 ? launch_grouped_tiles<T, 64, 128, A_KC, B_KC, VEC>(s, quota, p, gr) : launch_grouped_tiles<T, 64, 64, A_KC, B_KC, VEC>(s, quota, p, gr);
+    }
+  } else {
+    // Other types and alignments.  Half a tile more for every group than its rows fill; forward of 2998 rows of 12, 640 x 1000, fp32 in this loop, 848 tiles of 64: 59 us by 32,
+    // 58 by 64; 6000 rows, 640 x 640, 1000, 71 / 57; weight gradients of 4, 1024 x 1024, 1024, 57 / 47; of 8, 256 x 256, 128, 13 / 26.
+    const int64_t t64 = ceil_div(p.M, 64), n64 = ceil_div(p.N, 64);
+    if ((A_KC ? (t64 + std::min<int64_t>(gr.groups, p.M) / 2) * n64 : t64 * n64 * gr.groups) * gr.splits >= 848)
+      return launch_grouped_tiles<T, 64, 64, A_KC, B_KC, VEC>(s, quota, p, gr);
+  }
+  return launch_grouped_tiles<T, 32, 32, A_KC, B_KC, VEC>(s, quota, p, gr);
 }
 
 template <typename T>
@@ -628,6 +826,8 @@ mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const 
 }
 
 }  // namespace
+
+double grouped_f32_us(bool a_kc, int64_t M, int64_t N, int64_t K, int splits) { return f32_choice(a_kc, M, N, (double)ceil_div(K, splits), 1, splits).us; }
 
 // M: rows of A for all groups together, the most that there can be (a K-strided A: of each C).  K: the contraction (a K-strided A: the longest).
 // splits > 1 (one group, fp32): the contraction in pieces (K-contiguous A: of split_k), C [splits, M, ldc]

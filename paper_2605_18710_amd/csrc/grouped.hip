@@ -13,9 +13,6 @@
 #include "gemm_w4.h"
 #include "kernels.h"
 
-mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
-                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k = 0, int splits = 1);
-
 namespace {
 
 // Tiles of 256, 224, 192 or 160 rows, whichever fill the rounds of 256 CUs best, half a tile more for every group than its rows fill (a round of lower ones takes

@@ -31,6 +31,10 @@ size_t gemm_splitk_scratch_bytes(int64_t M, int64_t N, int64_t K);
 enum GroupedForm { GROUPED_FWD, GROUPED_DGRAD, GROUPED_WGRAD };
 mosaic_status launch_grouped(hipStream_t s, int quota, int dtype, GroupedForm form, int64_t T, int groups, int64_t k, int64_t n, const int32_t* offsets,
                              const void* A, const void* B, void* C);
+// the fp32 kernel of these products (gemm_f32.hip says what the arguments are), and its price in microseconds for one group
+mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
+                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k = 0, int splits = 1);
+double grouped_f32_us(bool a_kc, int64_t M, int64_t N, int64_t K, int splits);
 // Y[b, t, :] = X[b, t, :] W + bias + table[t, :]: B x rows patches of k values, ldx apart (zeros past k), W [k, n].  One rounding
 // where the bf16 matrix-core kernel takes the product and the table in its epilogue, else the product and add_pos.
 mosaic_status launch_embed_fwd(hipStream_t s, int quota, int dtype, int64_t B, int64_t rows, int64_t n, int64_t k, int64_t ldx, const void* X,

@@ -23,9 +23,6 @@
 #include "gemm_w4.h"
 #include "kernels.h"
 
-mosaic_status launch_grouped_f32(hipStream_t s, int quota, int dtype, bool a_kc, bool b_kc, int M, int N, int K, const void* A, int64_t lda, const void* B,
-                                 int64_t ldb, void* C, int64_t ldc, const void* R, const int32_t* offsets, int groups, int bound, int64_t stride, int split_k = 0, int splits = 1);
-
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
@@ -301,7 +298,8 @@ __device__ __forceinline__ float block_reduce(float x, bool max, float* lds) {
   return max ? fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3])) : (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// fp32 logits, a workgroup (NT 256) or a wave (64) to a row of up to NT PER of them, which it holds: loss and (grad) dz in place
+// fp32 logits, a workgroup (NT 256) or a wave (64) to a row of up to 4 NT PER of them, which it holds: loss and (grad) dz in place.  8969 rows of 2667: 46 us (4.1 TB/s);
+// by single words, in registers for 8192, 105.
 template <int NT, int PER>
 __global__ __launch_bounds__(NT) void rows_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, int grad) {
   __shared__ float lds[4];
@@ -309,25 +307,35 @@ __global__ __launch_bounds__(NT) void rows_f32_kernel(CePiece p, const CeHead* _
   const float g = head->per_token, even = p.smoothing / (float)p.V;
   auto reduce = [&](float x, bool max) { return NT == 64 ? (max ? wave_max(x) : wave_sum(x)) : block_reduce(x, max, lds); };
   for (int row = blockIdx.x; row < live; row += gridDim.x) {
-    float* z = Z + row * ld;
-    const int target = p.target[start + row];
-    float v[PER], top = -INFINITY, total = 0.f, sum = 0.f;
+    float* const z = Z + row * ld + 4 * threadIdx.x;           // rows of whole 16-byte pieces, with room up to ld
+    const int target = p.target[start + row], last = p.V - 4 * threadIdx.x;
+    f32x4 v[PER];
+    float top = -INFINITY, total = 0.f, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x + NT * i;
-      v[i] = c < p.V ? z[c] : -INFINITY;
-      top = fmaxf(top, v[i]);
-      total += c < p.V ? v[i] : 0.f;
+      v[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (4 * NT * i < last) v[i] = *reinterpret_cast<const f32x4*>(z + 4 * NT * i);
     }
+    const float at_target = Z[row * ld + target];
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool in = 4 * NT * i + e < last;
+        if (!in) v[i][e] = -INFINITY;
+        top = fmaxf(top, v[i][e]);
+        total += in ? v[i][e] : 0.f;
+      }
     top = reduce(top, true);
     if (p.smoothing > 0.f) total = reduce(total, false);
     const float ref = top == -INFINITY ? 0.f : top;
-    const float at_target = z[target];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      v[i] = expf(v[i] - ref);
-      sum += v[i];
-    }
+    for (int i = 0; i < PER; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[i][e] = expf(v[i][e] - ref);
+        sum += v[i][e];
+      }
     sum = reduce(sum, false);
     __syncthreads();                             // the target's logit has been read by all
     if (threadIdx.x == 0) p.losses[p.rows[start + row]] = token_loss((ref + logf(sum)) / kLn2, at_target, total, p.smoothing, p.V);
@@ -335,14 +343,19 @@ __global__ __launch_bounds__(NT) void rows_f32_kernel(CePiece p, const CeHead* _
     const float inverse = 1.f / sum;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const int c = threadIdx.x + NT * i;
-      if (c < p.V) z[c] = g * (c == target ? (v[i] * inverse - 1.f) + (p.smoothing - even) : v[i] * inverse - even);
-      else if (c < (p.V + 3) / 4 * 4) z[c] = 0.f;            // the products read whole 16-byte pieces
+      if (4 * NT * i >= last) continue;
+      f32x4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float q = v[i][e] * inverse;
+        o[e] = 4 * NT * i + e >= last ? 0.f : g * (4 * (NT * i + (int)threadIdx.x) + e == target ? (q - 1.f) + (p.smoothing - even) : q - even);      // the products read whole pieces
+      }
+      *reinterpret_cast<f32x4*>(z + 4 * NT * i) = o;
     }
   }
 }
 // Longer rows: (m, sum) of blocks of kWideBlock columns, joined by lse_kernel, and dz in place, a workgroup to a block
-constexpr int kWideBlock = 4096;
+constexpr int kWideRow = 8192, kWideBlock = 4096;
 template <bool GRAD>
 __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* __restrict__ head, float* __restrict__ Z, int64_t ld, float2* __restrict__ stats,
                                                        float* __restrict__ totals, float* __restrict__ at_target) {
@@ -767,13 +780,22 @@ struct CeLayout {
       if (pieces > 1) n += V * h;
     }
     dx_splits = 1;
-    if (!half && grad) {                         // dX of the piece: tiles of 32 x 32, four workgroups to a CU, no less than 256 k-values
-      const int64_t tiles = ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 32) * ceil_div(h, 32), most = std::max<int64_t>(1, std::min(1024 / tiles, V / 256));
-      dx_k = (int)(ceil_div(ceil_div(V, most), 64) * 64);
+    if (!half && grad) {                         // the pieces that price least, joined at 5 TB/s; up to 1 GiB of them
+      auto cut = [&](bool a_kc, int64_t M, int64_t N, int64_t K, double join) {
+        int best = 1;
+        double least = grouped_f32_us(a_kc, M, N, K, 1);
+        for (int s = 2; s <= 64 && K / s >= 128 && s * M * N <= (int64_t)1 << 28; ++s) {
+          const double us = grouped_f32_us(a_kc, M, N, K, s) + join + (double)(8 * s) * (double)(M * N) / 5e6;
+          if (us < least) { least = us; best = s; }
+        }
+        return best;
+      };
+      const int64_t some = std::min(piece, std::max<int64_t>(T, 1));
+      const int pieces_of = cut(true, some, h, V, 0.0);        // which pass through a join even if there is one: its rows go to the tokens'
+      dx_k = (int)(ceil_div(ceil_div(V, pieces_of), 64) * 64);
       dx_splits = (int)ceil_div(V, dx_k);
       n = dx_splits * piece * h;
-      const int64_t of_table = ceil_div(V, 32) * ceil_div(h, 32);
-      if (pieces == 1) dw_splits = (int)std::max<int64_t>(1, std::min(1024 / of_table, T / 256));
+      if (pieces == 1) dw_splits = cut(false, V, h, some, 4.0);
       if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
     }
     sums = take(4 * n);
@@ -855,11 +877,12 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     if (!half) {
       float* Z = (float*)(base + L.e);
       MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc + r0 * h * 4, h, table, h, Z, L.ld, nullptr, live, 1, capacity, 0));
-      if (V <= 256 * 32) {
+      if (V <= kWideRow) {
         const int grid = grid_for(quota, 8, some);
-        if (V <= 64 * 2) rows_f32_kernel<64, 2><<<grid_for(quota, 32, some), 64, 0, s>>>(p, head, Z, L.ld, grad);
-        else if (V <= 256 * 4) rows_f32_kernel<256, 4><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
-        else rows_f32_kernel<256, 32><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        if (V <= 256) rows_f32_kernel<64, 1><<<grid_for(quota, 32, some), 64, 0, s>>>(p, head, Z, L.ld, grad);
+        else if (V <= 1024) rows_f32_kernel<256, 1><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        else if (V <= 4096) rows_f32_kernel<256, 4><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
+        else rows_f32_kernel<256, 8><<<grid, 256, 0, s>>>(p, head, Z, L.ld, grad);
       } else {
         float2* const stats = (float2*)(base + L.stats);
         float* const totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
