@@ -295,7 +295,13 @@ __device__ __forceinline__ void gemm_f32_tile(const F32Gemm& p, int tile, float*
         }
       }
     }
-    if constexpr (SHARES) { sum += acc[0][0]; acc[0][0] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+    if constexpr (SHARES) {
+      // the 10 wait states between a matrix instruction and another reader of its result: where a loop of them can be passed by, the compiler
+      // has left them out (the sums of K-strided operands lost their fourth columns)
+      asm volatile("s_nop 15" : "+v"(acc[0][0]));
+      sum += acc[0][0];
+      acc[0][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
   } while (SHARES && k0 < p.K);
   if constexpr (SHARES) acc[0][0] = sum;
   __syncthreads();                       // the next tile writes stage 0
@@ -655,11 +661,41 @@ __device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds
     pa.advance();
     pb.advance();
   };
+  // Sums of kChunk k-values each, added up: a chain of K roundings is off by sqrt(K / kChunk) times as much.  (128 x 128 has no registers for it; its contractions
+  // are short for what they are worth.)
+  constexpr int kChunk = 512;
+  constexpr bool CHUNKS = WM * WN < 4;
+  f32x16 sum[CHUNKS ? WM : 1][CHUNKS ? WN : 1];
+#pragma unroll
+  for (int i = 0; i < (CHUNKS ? WM : 1); ++i)
+#pragma unroll
+    for (int j = 0; j < (CHUNKS ? WN : 1); ++j) sum[i][j] = f32x16{};
+  auto settle = [&] {                                  // as in gemm_f32_tile; 18 wait states
+    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc[0][0]));
+#pragma unroll
+    for (int i = 1; i < WM * WN; ++i) asm volatile("" : "+v"(acc[i / WN][i % WN]));
+  };
   for (int k0 = 0;;) {
     k_tile(std::integral_constant<int, 0>{});
     if ((k0 += KS) >= K) break;
     k_tile(std::integral_constant<int, 1>{});
     if ((k0 += KS) >= K) break;
+    if constexpr (CHUNKS) {
+      if (k0 % kChunk == 0) {
+        settle();
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+#pragma unroll
+          for (int j = 0; j < WN; ++j) { sum[i][j] += acc[i][j]; acc[i][j] = f32x16{}; }
+      }
+    }
+  }
+  settle();
+  if constexpr (CHUNKS) {
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+      for (int j = 0; j < WN; ++j) acc[i][j] += sum[i][j];
   }
   // acc[i][j][4 q + e] is row 32 i + lr, column 32 j + 8 q + 4 g + e
   const float* R = (const float*)p.R;
@@ -753,7 +789,8 @@ __global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_group
         if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
       }
       if constexpr (std::is_same<T, float>::value && VEC && BM > 32) f32_block<BM, BN, A_KC, B_KC>(q, (int)(item - starts[a]), lds);
-      else gemm_f32_tile<T, BM, BM == 32 ? 64 : 32, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
+      else if constexpr (BM == 32) { q.in_shares = true; gemm_f32_tile<T, 32, 64, A_KC, B_KC, VEC, true>(q, (int)(item - starts[a]), lds); }
+      else gemm_f32_tile<T, BM, 32, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
     }
     before += all;
   }

@@ -37,17 +37,17 @@ __device__ __forceinline__ bf16x8 few_get(const lds_byte* area, int j, int half)
 
 // C[m0 .. m0 + 16 RB - 1, n0 .. n0 + 63] of C[M,N] = op(A) op(B): finish(row, col, v) for eight columns v[8] of a row, by eight lanes side by side for a row's 64, rows
 // and columns past M and N too.  A [M, K] (A_KC) or [K, M] (RB 4), B [N, K] (B_KC) or [K, N]; lda, ldb, M or N where they are a row's length rounded up, and K
-// where it is, multiples of 8, zeros or readable up to there.  K = 0: zeros.
+// where it is, multiples of 8, zeros or readable up to there.  K = 0: zeros.  LO: A is the sum of two, the other one a_lo elements behind it, whose product is added.
 // Step i of 64 k-values is wave i % 8's, so the waves read on side by side; a wave has two steps on their way in registers, 16 KB of B.  An operand
 // whose contraction is contiguous goes straight to the matrix instructions: of a row's 128-byte line 32 bytes to a lane where
 // both are, else the k-values that the transposing read gives.  The waves' sums meet in LDS and are added in wave order.
-template <bool A_KC, bool B_KC, int RB, typename FINISH>
+template <bool A_KC, bool B_KC, int RB, bool LO = false, typename FINISH>
 __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda, int m0, int M, const bf16* __restrict__ B, int64_t ldb, int n0, int N, int K,
-                                         unsigned char* smem, FINISH finish) {
+                                         unsigned char* smem, FINISH finish, int64_t a_lo = 0) {
   static_assert(A_KC || RB == 4, "a strided row operand comes in 64 columns");
   constexpr int kRows = 16 * RB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, g = lane >> 4;
-  const int steps = (K + kFewStep - 1) / kFewStep;
+  const int once = (K + kFewStep - 1) / kFewStep, steps = LO ? 2 * once : once;
   lds_byte* const mine_b = (lds_byte*)smem + wave * 8192 * ((A_KC ? 0 : 1) + (B_KC ? 0 : 1));
   lds_byte* const mine_a = mine_b + (B_KC ? 0 : 8192);
   float* const sums = reinterpret_cast<float*>(smem);                    // [wave][row][64]
@@ -58,7 +58,9 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
   bf16x8 a[2][NA], b[2][8];
   auto request = [&](auto buf, int s) {
     constexpr int U = decltype(buf)::value;
-    const int k0 = s * kFewStep;
+    const bool low = LO && s >= once;
+    const int k0 = (low ? s - once : s) * kFewStep;
+    const int64_t lo = low ? a_lo : 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       b[U][i] = bf16x8{};
@@ -75,10 +77,10 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
       a[U][i] = bf16x8{};
       if constexpr (A_KC) {                      // [2i + half]
         const int k = k0 + (B_KC ? 16 * g + 8 * (i & 1) : 32 * (i & 1) + 8 * g);
-        if (k < K) a[U][i] = *reinterpret_cast<const bf16x8*>(a_row[i >> 1] + k);
+        if (k < K) a[U][i] = *reinterpret_cast<const bf16x8*>(a_row[i >> 1] + lo + k);
       } else {
         const int k = k0 + 8 * i + (lane >> 3), c = m0 + 8 * (lane & 7);
-        if (k < K && c < M) a[U][i] = *reinterpret_cast<const bf16x8*>(A + (int64_t)k * lda + c);
+        if (k < K && c < M) a[U][i] = *reinterpret_cast<const bf16x8*>(A + lo + (int64_t)k * lda + c);
       }
     }
   };

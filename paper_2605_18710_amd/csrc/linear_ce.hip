@@ -207,9 +207,12 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
 
 // exp(z - m) in fp16 -> D dz in bf16, in place (the products' results are divided by D: a target of small probability, the largest term of its row, is then
 // -1 and not rounded at all): a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
+// LO: what that rounding leaves goes behind it, `lo` elements on.  The rounding of dz is one error of up to half a step beside the results' own; over many
+// values it makes sqrt(2) of the plain form's error, over the few of a small vocabulary and few tokens up to 2.1 times (1 x 64 to 64 x 3), where it is cheap to take it away.
 constexpr int kStrip = 1024;
-template <bool PAST, bool JOIN>
-__global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld) {
+constexpr int kLowTokens = 512, kLowColumns = 512;
+template <bool PAST, bool JOIN, bool LO>
+__global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld, int64_t lo) {
   // JOIN: every workgroup joins its rows' blocks itself, of which there are at most kJoinBlocks, and no launch does before
   __shared__ float top_of[4][16], sum_of[4][16], total_of[4][16], lse_of[16];
   const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
@@ -275,15 +278,20 @@ __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* _
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
       const float f = __builtin_amdgcn_exp2f(scale[i] - lse[i]);
-      Vec16<bf16> o;
+      Vec16<bf16> o, rest;
+      auto set = [&](int e, float x) {
+        o.set(e, x);
+        if constexpr (LO) rest.set(e, x - o.get(e));
+      };
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o.set(e, col + e < p.V ? (float)v[i][e] * f - even : 0.f);
+      for (int e = 0; e < 8; ++e) set(e, col + e < p.V ? (float)v[i][e] * f - even : 0.f);
       if (hit[i] >= 0 && hit[i] < 8) {
         // the target's probability from its own logit: 1 - p keeps its digits where p is near 1
         const float d = (__builtin_amdgcn_exp2f(fmaf(own[i], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) if (e == hit[i]) o.set(e, d);
+        for (int e = 0; e < 8; ++e) if (e == hit[i]) set(e, d);
       }
+      if constexpr (LO) rest.store<PAST>(E + lo + (int64_t)row * ld + col);
       o.store<PAST>(E + (int64_t)row * ld + col);
     }
   }
@@ -483,20 +491,21 @@ __device__ __forceinline__ void add_losses(const CeLoss& l, double* part) {
 }
 // dX, and (TABLE) dtable in the same launch: 375 x 33 of 72: two launches 11.7 us, one 7.6.  The last workgroup also adds the losses, where there are no more
 // pieces (loss not null).
-__device__ __forceinline__ void few_dtable(const W4Args& p, int64_t item, unsigned char* smem) {
+template <bool LO>
+__device__ __forceinline__ void few_dtable(const W4Args& p, int64_t item, unsigned char* smem, int64_t lo) {
   const int live = p.offsets[1], start = p.piece[0], cols = (p.N + 63) / 64, m0 = (int)(item / cols) * 64, n0 = (int)(item % cols) * 64;
   const float scale = *p.scale;
-  few_tile<false, false, 4>(p.A, p.lda, m0, p.M, p.B + (int64_t)start * p.ldb, p.ldb, n0, p.N, live, smem, [&](int row, int col, const float (&v)[8]) {
+  few_tile<false, false, 4, LO>(p.A, p.lda, m0, p.M, p.B + (int64_t)start * p.ldb, p.ldb, n0, p.N, live, smem, [&](int row, int col, const float (&v)[8]) {
     bf16x8 o;
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
     if (row < p.M && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
-  });
+  }, lo);
 }
 constexpr int kBothItems = 512;
 __device__ __host__ __forceinline__ int64_t few_dtable_items(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); }
-template <int RB, bool TABLE>
-__global__ __launch_bounds__(kFewNT, TABLE ? 2 : few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l, W4Args w) {
+template <int RB, bool TABLE, bool LO>
+__global__ __launch_bounds__(kFewNT, TABLE ? 2 : few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l, W4Args w, int64_t lo) {
   extern __shared__ __align__(16) unsigned char smem[];
   if (l.loss && blockIdx.x == gridDim.x - 1) add_losses<kFewNT>(l, reinterpret_cast<double*>(smem));
   const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
@@ -504,21 +513,22 @@ __global__ __launch_bounds__(kFewNT, TABLE ? 2 : few_waves(RB)) void few_dx_kern
   const int64_t first = TABLE ? few_dtable_items(w.M, w.N) : 0, items = first + (int64_t)tiles_m * ((p.N + 63) / 64);
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     if (TABLE && item < first) {                 // their contraction is the longer one as a rule
-      few_dtable(w, item, smem);
+      few_dtable<LO>(w, item, smem, lo);
       continue;
     }
     const int n0 = (int)((item - first) / tiles_m) * 64, m0 = (int)((item - first) % tiles_m) * 16 * RB;
-    few_tile<true, false, RB>(p.A, p.lda, m0, live, p.B, p.ldb, n0, p.N, p.K, smem, [&](int row, int col, const float (&v)[8]) {
+    few_tile<true, false, RB, LO>(p.A, p.lda, m0, live, p.B, p.ldb, n0, p.N, p.K, smem, [&](int row, int col, const float (&v)[8]) {
       bf16x8 o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = (bf16)(v[e] * scale);
       if (row < live && col < p.N) *reinterpret_cast<bf16x8*>(p.C + (int64_t)p.rows[start + row] * p.ldc + col) = o;
-    });
+    }, lo);
   }
 }
-__global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p) {
+template <bool LO>
+__global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p, int64_t lo) {
   extern __shared__ __align__(16) unsigned char smem[];
-  for (int64_t item = blockIdx.x; item < few_dtable_items(p.M, p.N); item += gridDim.x) few_dtable(p, item, smem);
+  for (int64_t item = blockIdx.x; item < few_dtable_items(p.M, p.N); item += gridDim.x) few_dtable<LO>(p, item, smem, lo);
 }
 template <int RB>
 mosaic_status launch_few_logits(hipStream_t s, int quota, int most, const W4Args& p) {
@@ -530,14 +540,24 @@ mosaic_status launch_few_logits(hipStream_t s, int quota, int most, const W4Args
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
-template <int RB, bool TABLE>
-mosaic_status launch_few_dx(hipStream_t s, int quota, int most, const W4Args& p, const CeLoss& l, const W4Args& w) {
+template <int RB, bool TABLE, bool LO>
+mosaic_status launch_few_dx(hipStream_t s, int quota, int most, const W4Args& p, const CeLoss& l, const W4Args& w, int64_t lo) {
   static std::once_flag once;
   static hipError_t rc = hipSuccess;
   constexpr int kLds = std::max(few_lds<true, false, RB>(), TABLE ? few_lds<false, false, 4>() : 0);
-  MOSAIC_TRY(few_allow_lds(few_dx_kernel<RB, TABLE>, kLds, &once, &rc));
+  MOSAIC_TRY(few_allow_lds(few_dx_kernel<RB, TABLE, LO>, kLds, &once, &rc));
   const int64_t items = ceil_div(most, 16 * RB) * ceil_div(p.N, 64) + (TABLE ? few_dtable_items(w.M, w.N) : 0);
-  few_dx_kernel<RB, TABLE><<<grid_for(quota, RB == 1 && !TABLE ? 2 : 1, items), kFewNT, kLds, s>>>(p, l, w);
+  few_dx_kernel<RB, TABLE, LO><<<grid_for(quota, RB == 1 && !TABLE ? 2 : 1, items), kFewNT, kLds, s>>>(p, l, w, lo);
+  MOSAIC_LAUNCH_CHECK();
+  return MOSAIC_OK;
+}
+template <bool LO>
+mosaic_status launch_few_dtable(hipStream_t s, int quota, const W4Args& w, int64_t lo) {
+  static std::once_flag once;
+  static hipError_t rc = hipSuccess;
+  constexpr int kLds = few_lds<false, false, 4>();
+  MOSAIC_TRY(few_allow_lds(few_dtable_kernel<LO>, kLds, &once, &rc));
+  few_dtable_kernel<LO><<<grid_for(quota, 1, few_dtable_items(w.M, w.N)), kFewNT, kLds, s>>>(w, lo);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -747,7 +767,7 @@ __global__ __launch_bounds__(kLossThreads) void loss_kernel(CeLoss l) {
 // piece of this size do, there is one (12288 tokens that count, h 4096, V 128000, two pieces 30100 us, one 29900).
 constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
-  int64_t piece, ld, blocks;
+  int64_t piece, ld, blocks, lo;               // lo: elements from a dz to what its rounding left, 0 where that is not kept
   int pieces, dw_splits, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
   size_t head, spans, rows, target, slot, losses, at_target, lse, inverse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
@@ -769,7 +789,8 @@ struct CeLayout {
     at_target = take(4 * piece); lse = take(4 * piece); inverse = take(half ? 0 : 4 * piece);
     stats = take(8 * blocks * piece); totals = take(4 * blocks * piece);
     x = take(padded * h * (int64_t)es);
-    e = take(grad || !half ? piece * ld * (int64_t)es : 0);
+    lo = half && grad && T <= kLowTokens && V <= kLowColumns ? piece * ld : 0;
+    e = take(grad || !half ? (lo ? 2 : 1) * piece * ld * (int64_t)es : 0);
     // Few tiles over a long contraction leave most CUs idle: it is cut until the tiles are about one to a CU, into no less than 1024 k-values.
     const int64_t tiles = ceil_div(V, 256) * ceil_div(h, 256);
     dw_splits = half && grad ? (int)std::max<int64_t>(1, std::min(256 / tiles, std::min(piece, T) / 1024)) : 1;
@@ -943,9 +964,10 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     if (!grad) continue;
     const int64_t left = 2 * some * L.ld;
     const Sweep sweep = sweep_grid(s, quota, ceil_div(some, 16) * ceil_div(L.ld, kStrip), 2 * left);
-    if (join) grad_kernel<false, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld);
-    else if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
-    else grad_kernel<false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld);
+    if (L.lo) grad_kernel<false, true, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld, L.lo);
+    else if (join) grad_kernel<false, true, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld, 0);
+    else if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true, false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld, 0);
+    else grad_kernel<false, false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld, 0);
     MOSAIC_LAUNCH_CHECK();
     W4Args w = {};
     bool few_table = false;
@@ -959,7 +981,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       w.sums = sums; w.first = i == 0; w.scale = &head->per_token;
       w.splits = L.dw_splits;
       const double w4_us = w4_price((double)w.tile_count * L.dw_splits, (double)some / L.dw_splits, false) + (L.dw_splits > 1 ? 5.0 + (double)(V * h) * (4 * L.dw_splits + 2) / 5e6 : 0.0);
-      few_table = L.pieces == 1 && few_price((double)few_dtable_items(V, h), (double)some, 4, false) < w4_us;
+      few_table = L.lo || (L.pieces == 1 && few_price((double)few_dtable_items(V, h), (double)some, 4, false) < w4_us);
     }
     if (dX) {
       W4Args d = {};
@@ -971,13 +993,14 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.rows = rows;
       d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
-      const int blocks = few_rows(some, h, V, 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
+      const int blocks = few_rows(some, h, V, L.lo ? HUGE_VAL : 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
       if (blocks) {
         d.K = (int)V;                            // the rows of E are readable up to ld
         const bool both = few_table && ceil_div(some, 16 * blocks) * ceil_div(h, 64) + few_dtable_items(V, h) <= kBothItems;
         auto go = [&](auto rb) -> mosaic_status {
           constexpr int RB = decltype(rb)::value;
-          return both ? launch_few_dx<RB, true>(s, quota, some, d, now, w) : launch_few_dx<RB, false>(s, quota, some, d, now, w);
+          if (L.lo) return both ? launch_few_dx<RB, true, true>(s, quota, some, d, now, w, L.lo) : launch_few_dx<RB, false, true>(s, quota, some, d, now, w, L.lo);
+          return both ? launch_few_dx<RB, true, false>(s, quota, some, d, now, w, 0) : launch_few_dx<RB, false, false>(s, quota, some, d, now, w, 0);
         };
         MOSAIC_TRY(blocks == 1 ? go(std::integral_constant<int, 1>{}) : blocks == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{}));
         added = now.loss != nullptr;
@@ -993,12 +1016,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     }
     if (!dtable) continue;
     if (few_table) {
-      static std::once_flag once;
-      static hipError_t rc = hipSuccess;
-      constexpr int kLds = few_lds<false, false, 4>();
-      MOSAIC_TRY(few_allow_lds(few_dtable_kernel, kLds, &once, &rc));
-      few_dtable_kernel<<<grid_for(quota, 1, few_dtable_items(V, h)), kFewNT, kLds, s>>>(w);
-      MOSAIC_LAUNCH_CHECK();
+      MOSAIC_TRY(L.lo ? launch_few_dtable<true>(s, quota, w, L.lo) : launch_few_dtable<false>(s, quota, w, 0));
     } else if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
     else if (L.dw_splits > 1) {
       w.tile_count *= w.splits;

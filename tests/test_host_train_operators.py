@@ -3,7 +3,7 @@ on a GPU.  Addresses stand for device memory and are never read."""
 import pytest
 
 from paper_2605_18710_amd import binding as mb
-from test_host_wait_states import listings, matrix_too_close  # noqa: F401
+from test_host_wait_states import listings, looking_back, matrix_too_close, vector_registers  # noqa: F401
 
 A, B, C, D, E, F, G, H = (0x100000000 * i for i in range(1, 9))
 
@@ -90,3 +90,22 @@ def test_matrix_instructions_of_the_four_wave_kernel_keep_their_distance(listing
             if seen[-1] > 4:
                 assert not [x for x in ins if x[1] == "v_accvgpr_mov_b32"] and not matrix_too_close(ins), name
     assert set(seen) == {4, 5, 6, 7, 8}
+
+
+def test_sums_wait_for_the_fp32_matrix_instructions(listings):  # noqa: F811
+    """v_mfma_f32_16x16x4_f32 wants 10 wait states before anything else reads its result, v_mfma_f32_32x32x2_f32 18.  The compiler does not see to it
+    where the reader begins a block that can be reached around the loop of matrix instructions as well."""
+    seen, bad = 0, []
+    for name, ins in listings:
+        if not any(x[1].startswith(("v_mfma_f32_16x16x4_f32", "v_mfma_f32_32x32x2_f32")) for x in ins):
+            continue
+        seen += 1
+        found = looking_back(ins)
+        for i, (at, op, operands, _) in enumerate(ins):
+            if op.startswith("v_mfma") or not op.startswith(("v_", "ds_write", "global_store", "buffer_store", "scratch_store")):
+                continue
+            uses = vector_registers(operands)
+            for states, which in ((10, "v_mfma_f32_16x16x4_f32"), (18, "v_mfma_f32_32x32x2_f32")):
+                if found(i, states, lambda x: x[1].startswith(which) and vector_registers(x[2].split(", ")[0]) & uses):  # noqa: B023
+                    bad.append("%s: %x %s %s" % (name[:90], at, op, operands))
+    assert seen > 20 and not bad, (len(bad), bad[:5])
