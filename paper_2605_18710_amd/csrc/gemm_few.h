@@ -37,7 +37,8 @@ __device__ __forceinline__ bf16x8 few_get(const lds_byte* area, int j, int half)
 
 // C[m0 .. m0 + 16 RB - 1, n0 .. n0 + 63] of C[M,N] = op(A) op(B): finish(row, col, v) for eight columns v[8] of a row, by eight lanes side by side for a row's 64, rows
 // and columns past M and N too.  A [M, K] (A_KC) or [K, M] (RB 4), B [N, K] (B_KC) or [K, N]; lda, ldb, M or N where they are a row's length rounded up, and K
-// where it is, multiples of 8, zeros or readable up to there.  K = 0: zeros.  LO: A is the sum of two, the other one a_lo elements behind it, whose product is added.
+// where it is, multiples of 8, zeros or readable up to there.  K = 0: zeros.  LO: A is the sum of two, the other one a_lo elements behind it, whose product is added
+// (16 rows with a contiguous contraction: in the same step, so that B is read once).
 // Step i of 64 k-values is wave i % 8's, so the waves read on side by side; a wave has two steps on their way in registers, 16 KB of B.  An operand
 // whose contraction is contiguous goes straight to the matrix instructions: of a row's 128-byte line 32 bytes to a lane where
 // both are, else the k-values that the transposing read gives.  The waves' sums meet in LDS and are added in wave order.
@@ -47,7 +48,8 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
   static_assert(A_KC || RB == 4, "a strided row operand comes in 64 columns");
   constexpr int kRows = 16 * RB;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, g = lane >> 4;
-  const int once = (K + kFewStep - 1) / kFewStep, steps = LO ? 2 * once : once;
+  constexpr bool BOTH = LO && A_KC && RB == 1;
+  const int once = (K + kFewStep - 1) / kFewStep, steps = LO && !BOTH ? 2 * once : once;
   lds_byte* const mine_b = (lds_byte*)smem + wave * 8192 * ((A_KC ? 0 : 1) + (B_KC ? 0 : 1));
   lds_byte* const mine_a = mine_b + (B_KC ? 0 : 8192);
   float* const sums = reinterpret_cast<float*>(smem);                    // [wave][row][64]
@@ -55,10 +57,10 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
 #pragma unroll
   for (int i = 0; i < RB; ++i) a_row[i] = A + (int64_t)min(m0 + 16 * i + lr, M - 1) * lda;      // A_KC: rows past the last one repeat it
   constexpr int NA = A_KC ? 2 * RB : 8;
-  bf16x8 a[2][NA], b[2][8];
+  bf16x8 a[2][NA], b[2][8], more[2][BOTH ? NA : 1];
   auto request = [&](auto buf, int s) {
     constexpr int U = decltype(buf)::value;
-    const bool low = LO && s >= once;
+    const bool low = LO && !BOTH && s >= once;
     const int k0 = (low ? s - once : s) * kFewStep;
     const int64_t lo = low ? a_lo : 0;
 #pragma unroll
@@ -78,6 +80,10 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
       if constexpr (A_KC) {                      // [2i + half]
         const int k = k0 + (B_KC ? 16 * g + 8 * (i & 1) : 32 * (i & 1) + 8 * g);
         if (k < K) a[U][i] = *reinterpret_cast<const bf16x8*>(a_row[i >> 1] + lo + k);
+        if constexpr (BOTH) {
+          more[U][i] = bf16x8{};
+          if (k < K) more[U][i] = *reinterpret_cast<const bf16x8*>(a_row[i >> 1] + a_lo + k);
+        }
       } else {
         const int k = k0 + 8 * i + (lane >> 3), c = m0 + 8 * (lane & 7);
         if (k < K && c < M) a[U][i] = *reinterpret_cast<const bf16x8*>(A + lo + (int64_t)k * lda + c);
@@ -114,6 +120,7 @@ __device__ __forceinline__ void few_tile(const bf16* __restrict__ A, int64_t lda
         else y = few_get(mine_b, j, half);
 #pragma unroll
         for (int i = 0; i < RB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[i], acc[i][j], 0, 0, 0);
+        if constexpr (BOTH) acc[0][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, more[U][half], acc[0][j], 0, 0, 0);
       }
     }
     if constexpr (!A_KC || !B_KC) meet();        // read before the next step is written

@@ -208,9 +208,10 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
 // exp(z - m) in fp16 -> D dz in bf16, in place (the products' results are divided by D: a target of small probability, the largest term of its row, is then
 // -1 and not rounded at all): a strip of 16 rows and 1024 columns to a workgroup, 16 bytes to a lane and row pair.  PAST: tensors that no cache holds.
 // LO: what that rounding leaves goes behind it, `lo` elements on.  The rounding of dz is one error of up to half a step beside the results' own; over many
-// values it makes sqrt(2) of the plain form's error, over the few of a small vocabulary and few tokens up to 2.1 times (1 x 64 to 64 x 3), where it is cheap to take it away.
+// values it makes sqrt(2) of the plain form's error, over the few of a small vocabulary and few tokens up to 2.1 times (1 x 64 to 64 x 3), and of up to 16 tokens
+// up to 2.2 times whatever the vocabulary, where it is cheap to take it away.
 constexpr int kStrip = 1024;
-constexpr int kLowTokens = 512, kLowColumns = 512;
+constexpr int kLowTokens = 512, kLowColumns = 512, kFewRows = 16;
 template <bool PAST, bool JOIN, bool LO>
 __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld, int64_t lo) {
   // JOIN: every workgroup joins its rows' blocks itself, of which there are at most kJoinBlocks, and no launch does before
@@ -505,7 +506,7 @@ __device__ __forceinline__ void few_dtable(const W4Args& p, int64_t item, unsign
 constexpr int kBothItems = 512;
 __device__ __host__ __forceinline__ int64_t few_dtable_items(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64); }
 template <int RB, bool TABLE, bool LO>
-__global__ __launch_bounds__(kFewNT, TABLE ? 2 : few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l, W4Args w, int64_t lo) {
+__global__ __launch_bounds__(kFewNT, TABLE || LO ? 2 : few_waves(RB)) void few_dx_kernel(W4Args p, CeLoss l, W4Args w, int64_t lo) {
   extern __shared__ __align__(16) unsigned char smem[];
   if (l.loss && blockIdx.x == gridDim.x - 1) add_losses<kFewNT>(l, reinterpret_cast<double*>(smem));
   const int live = p.offsets[1], start = p.piece[0], tiles_m = (live + 16 * RB - 1) / (16 * RB);
@@ -530,6 +531,70 @@ __global__ __launch_bounds__(kFewNT) void few_dtable_kernel(W4Args p, int64_t lo
   extern __shared__ __align__(16) unsigned char smem[];
   for (int64_t item = blockIdx.x; item < few_dtable_items(p.M, p.N); item += gridDim.x) few_dtable<LO>(p, item, smem, lo);
 }
+// Up to 16 tokens: a piece of the vocabulary to a workgroup, sums [pieces][16][N] for join_kernel.  5 x 424, V 117715 (100 MB): 33 us
+__global__ __launch_bounds__(kFewNT) void few_dx_pieces_kernel(W4Args p, int64_t lo, int per) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int live = p.offsets[1], cols = (p.N + 63) / 64, pieces = (p.K + per - 1) / per;
+  if (live == 0) return;
+  for (int item = blockIdx.x; item < pieces * cols; item += gridDim.x) {
+    const int piece = item / cols, n0 = (item - piece * cols) * 64, k0 = piece * per;
+    float* const out = p.sums + (int64_t)piece * kFewRows * p.N;
+    few_tile<true, false, 1, true>(p.A + k0, p.lda, 0, live, p.B + (int64_t)k0 * p.ldb, p.ldb, n0, p.N, min(per, p.K - k0), smem, [&](int row, int col, const float (&v)[8]) {
+      if (col >= p.N) return;
+      *reinterpret_cast<f32x4*>(out + (int64_t)row * p.N + col) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(out + (int64_t)row * p.N + col + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }, lo);
+  }
+}
+// dtable of up to 16 tokens: dz and what its rounding left are the 32 k-values of one matrix instruction for 16 x 16 results, so the stores are the time.  The tokens'
+// rows of X for 1024 columns lie in LDS, [column][token]; a wave takes 16 rows of the table at a time.  16 tokens, 32000 x 4096: 74 us (3.5 TB/s).
+constexpr int kOuterColumns = 1024;
+constexpr int outer_at(int c) { return c * 32 + (c >> 4) * 128; }          // byte of a column in LDS: 16 columns apart means 32 banks apart
+__global__ __launch_bounds__(256) void few_outer_kernel(W4Args p, int64_t lo) {
+  __shared__ __align__(16) unsigned char lds[outer_at(kOuterColumns)];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, g = lane >> 4, live = p.offsets[1];
+  const int chunks = (p.N + kOuterColumns - 1) / kOuterColumns, tiles = (p.M + 15) / 16, grid = (int)gridDim.x;
+  const float scale = *p.scale;
+  for (int chunk = (int)blockIdx.x % chunks; chunk < chunks; chunk += grid) {
+    const int c0 = chunk * kOuterColumns, columns = min(kOuterColumns, p.N - c0);
+    const int first = (int)blockIdx.x / chunks, step = max(1, (grid - chunk + chunks - 1) / chunks);
+    __syncthreads();                               // the chunk before has been read
+    for (int i = threadIdx.x; i < kFewRows * (kOuterColumns / 8); i += 256) {
+      const int t = i / (kOuterColumns / 8), c = i % (kOuterColumns / 8) * 8;
+      bf16x8 v = {};
+      if (t < live && c < columns) v = *reinterpret_cast<const bf16x8*>(p.B + (int64_t)t * p.ldb + c0 + c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *reinterpret_cast<bf16*>(lds + outer_at(c + e) + 2 * t) = v[e];
+    }
+    __syncthreads();
+    for (int tile = first * 4 + wave; tile < tiles; tile += step * 4) {
+      const int row = 16 * tile + lr;
+      bf16x8 x;                                    // k-values 8 g ..: tokens 8 (g % 2) .. of dz (g < 2) or of the rest
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int t = 8 * (g & 1) + e;
+        x[e] = (bf16)0.f;
+        if (t < live && row < p.M) x[e] = p.A[(g >> 1) * lo + (int64_t)t * p.lda + row];
+      }
+      for (int c = 0; c < columns; c += 64) {
+        f32x4 acc[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {              // columns 16 i / 4 + 4 j + i % 4, i = 0 .. 15: a lane's results are sixteen columns side by side
+          const bf16x8 y = *reinterpret_cast<const bf16x8*>(lds + outer_at(c + 16 * (lr >> 2) + 4 * j + (lr & 3)) + 16 * (g & 1));
+          acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const int col = c + 16 * g + 8 * half;
+          bf16x8 o;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = (bf16)(acc[2 * half + (e >> 2)][e & 3] * scale);
+          if (row < p.M && col < columns) *reinterpret_cast<bf16x8*>(p.C + (int64_t)row * p.ldc + c0 + col) = o;
+        }
+      }
+    }
+  }
+}
 template <int RB>
 mosaic_status launch_few_logits(hipStream_t s, int quota, int most, const W4Args& p) {
   static std::once_flag once;
@@ -547,7 +612,7 @@ mosaic_status launch_few_dx(hipStream_t s, int quota, int most, const W4Args& p,
   constexpr int kLds = std::max(few_lds<true, false, RB>(), TABLE ? few_lds<false, false, 4>() : 0);
   MOSAIC_TRY(few_allow_lds(few_dx_kernel<RB, TABLE, LO>, kLds, &once, &rc));
   const int64_t items = ceil_div(most, 16 * RB) * ceil_div(p.N, 64) + (TABLE ? few_dtable_items(w.M, w.N) : 0);
-  few_dx_kernel<RB, TABLE, LO><<<grid_for(quota, RB == 1 && !TABLE ? 2 : 1, items), kFewNT, kLds, s>>>(p, l, w, lo);
+  few_dx_kernel<RB, TABLE, LO><<<grid_for(quota, RB == 1 && !TABLE && !LO ? 2 : 1, items), kFewNT, kLds, s>>>(p, l, w, lo);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -767,6 +832,8 @@ __global__ __launch_bounds__(kLossThreads) void loss_kernel(CeLoss l) {
 // piece of this size do, there is one (12288 tokens that count, h 4096, V 128000, two pieces 30100 us, one 29900).
 constexpr int64_t kPieceElems = (int64_t)1 << 30;
 struct CeLayout {
+  bool few;                                    // bf16 gradients of up to 16 tokens and more of a table than one launch takes
+  int few_k;
   int64_t piece, ld, blocks, lo;               // lo: elements from a dz to what its rounding left, 0 where that is not kept
   int pieces, dw_splits, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
   size_t head, spans, rows, target, slot, losses, at_target, lse, inverse, stats, totals, x, e, sums, bytes;
@@ -789,8 +856,11 @@ struct CeLayout {
     at_target = take(4 * piece); lse = take(4 * piece); inverse = take(half ? 0 : 4 * piece);
     stats = take(8 * blocks * piece); totals = take(4 * blocks * piece);
     x = take(padded * h * (int64_t)es);
-    lo = half && grad && T <= kLowTokens && V <= kLowColumns ? piece * ld : 0;
-    e = take(grad || !half ? (lo ? 2 : 1) * piece * ld * (int64_t)es : 0);
+    lo = !half || !grad ? 0 : T <= kFewRows ? kFewRows * ld : T <= kLowTokens && V <= kLowColumns ? piece * ld : 0;
+    e = take(grad || !half ? (lo == piece * ld ? 2 : 1) * piece * ld * (int64_t)es : 0);
+    // the input gradient of up to 16 tokens: a workgroup to a CU, no less than two steps to a wave
+    few_k = (int)std::max<int64_t>(2 * kFewStep * kFewWaves, ceil_div(ceil_div(V, std::max<int64_t>(1, 256 / ceil_div(h, 64))), kFewStep) * kFewStep);
+    few = lo && T <= kFewRows && V > kLowColumns;
     // Few tiles over a long contraction leave most CUs idle: it is cut until the tiles are about one to a CU, into no less than 1024 k-values.
     const int64_t tiles = ceil_div(V, 256) * ceil_div(h, 256);
     dw_splits = half && grad ? (int)std::max<int64_t>(1, std::min(256 / tiles, std::min(piece, T) / 1024)) : 1;
@@ -799,6 +869,7 @@ struct CeLayout {
       n = std::min<int64_t>(std::min<int64_t>(kMostPieces, ceil_div(V, kLeastPiece)) * ceil_div(std::min(piece, std::max<int64_t>(T, 1)), 128) * ceil_div(h, 256), kMostPieceTiles) * 65536;       // w4_cut
       if (dw_splits > 1) n = std::max(n, dw_splits * V * h);
       if (pieces > 1) n += V * h;
+      if (few) n = std::max(n, ceil_div(V, few_k) * kFewRows * h);
     }
     dx_splits = 1;
     if (!half && grad) {                         // the pieces that price least, joined at 5 TB/s; up to 1 GiB of them
@@ -964,7 +1035,8 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     if (!grad) continue;
     const int64_t left = 2 * some * L.ld;
     const Sweep sweep = sweep_grid(s, quota, ceil_div(some, 16) * ceil_div(L.ld, kStrip), 2 * left);
-    if (L.lo) grad_kernel<false, true, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld, L.lo);
+    if (L.lo && !join) grad_kernel<false, false, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld, L.lo);
+    else if (L.lo) grad_kernel<false, true, true><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld, L.lo);
     else if (join) grad_kernel<false, true, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, z.totals, E, L.ld, 0);
     else if (sweep.in_order && left > kPastCacheBytes) grad_kernel<true, false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld, 0);
     else grad_kernel<false, false, false><<<sweep.grid, 256, 0, s>>>(p, z.stats, nullptr, E, L.ld, 0);
@@ -993,7 +1065,21 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       d.rows = rows;
       d.scale = &head->per_token;
       d.sums = sums + (L.pieces > 1 ? V * h : 0);
-      const int blocks = few_rows(some, h, V, L.lo ? HUGE_VAL : 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
+      if (L.few) {
+        d.K = (int)V;
+        static std::once_flag once;
+        static hipError_t rc = hipSuccess;
+        constexpr int kLds = few_lds<true, false, 1>();
+        MOSAIC_TRY(few_allow_lds(few_dx_pieces_kernel, kLds, &once, &rc));
+        const int64_t pieces = ceil_div(V, L.few_k);
+        few_dx_pieces_kernel<<<grid_for(quota, 1, pieces * ceil_div(h, 64)), kFewNT, kLds, s>>>(d, L.lo, L.few_k);
+        MOSAIC_LAUNCH_CHECK();
+        join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, (int)pieces, kFewRows, h, d.scale, 0, 0, p.span, rows, (bf16*)dX, now);
+        MOSAIC_LAUNCH_CHECK();
+        added = now.loss != nullptr;
+        if (!dtable) continue;
+      }
+      const int blocks = L.few ? 0 : few_rows(some, h, V, L.lo ? HUGE_VAL : 8.0 + w4_cut_us((int)w4_tiles(h), d.K));
       if (blocks) {
         d.K = (int)V;                            // the rows of E are readable up to ld
         const bool both = few_table && ceil_div(some, 16 * blocks) * ceil_div(h, 64) + few_dtable_items(V, h) <= kBothItems;
@@ -1005,7 +1091,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
         MOSAIC_TRY(blocks == 1 ? go(std::integral_constant<int, 1>{}) : blocks == 2 ? go(std::integral_constant<int, 2>{}) : go(std::integral_constant<int, 4>{}));
         added = now.loss != nullptr;
         if (both) continue;
-      } else {
+      } else if (!L.few) {
         MOSAIC_TRY((launch_rows<true, false, W4_PIECES>(s, quota, d, low)));
         if (d.K > kLeastPiece) {                 // or there is one piece, which went where it belongs
           join_kernel<bf16, true><<<grid_for(quota, 8, ceil_div((int64_t)some * (h / 4), 256)), 256, 0, s>>>(d.sums, 0, 0, h, d.scale, low ? 128 : 256, d.K, p.span, rows, (bf16*)dX, now);
@@ -1015,7 +1101,10 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       }
     }
     if (!dtable) continue;
-    if (few_table) {
+    if (L.few) {
+      few_outer_kernel<<<grid_for(quota, 3, ceil_div(V, 64) * ceil_div(h, kOuterColumns)), 256, 0, s>>>(w, L.lo);
+      MOSAIC_LAUNCH_CHECK();
+    } else if (few_table) {
       MOSAIC_TRY(L.lo ? launch_few_dtable<true>(s, quota, w, L.lo) : launch_few_dtable<false>(s, quota, w, 0));
     } else if (L.pieces > 1) MOSAIC_TRY((launch_w4_epi<false, false, W4_ADD, 8, W4_GROUPED>(s, quota, w)));
     else if (L.dw_splits > 1) {

@@ -91,7 +91,8 @@ CASES = [  # T, h, V, smoothing, share ignored
     (1, 8, 1, 0.0, 0.0), (1, 64, 2, 0.1, 0.0), (3, 72, 27, 0.1, 0.0), (130, 128, 1000, 0.0, 0.5), (257, 200, 515, 0.1, 0.3), (64, 136, 4099, 0.0, 0.0),
     (520, 320, 257, 0.0, 0.9), (129, 64, 20011, 0.2, 0.1), (1500, 64, 64, 0.0, 0.2), (2100, 264, 130, 0.1, 0.0), (40, 512, 2000, 0.0, 1.0), (1030, 256, 300, 0.0, 0.02),
     # by large tiles, of 256 rows and of 128, with the contraction over the vocabulary, or the tokens, cut; fp32 rows past what a workgroup holds
-    (3000, 512, 6000, 0.1, 0.3), (100, 256, 60000, 0.0, 0.1), (5000, 256, 600, 0.0, 0.1), (33, 40, 9001, 0.1, 0.2), (187, 72, 30001, 0.0, 0.0), (1000, 40, 100, 0.1, 0.3), (1500, 104, 2301, 0.1, 0.1), (600, 520, 2050, 0.0, 0.0)]
+    (3000, 512, 6000, 0.1, 0.3), (100, 256, 60000, 0.0, 0.1), (5000, 256, 600, 0.0, 0.1), (33, 40, 9001, 0.1, 0.2), (187, 72, 30001, 0.0, 0.0), (1000, 40, 100, 0.1, 0.3), (1500, 104, 2301, 0.1, 0.1), (600, 520, 2050, 0.0, 0.0), (1, 8, 513, 0.0, 0.0), (5, 256, 1582, 0.1, 0.0),
+         (16, 1032, 2051, 0.1, 0.2), (7, 2056, 700, 0.0, 0.3), (3, 4680, 9001, 0.0, 0.0), (16, 64, 70001, 0.0, 0.0)]
 
 
 @pytest.mark.parametrize("T,h,V,smoothing,ignored", CASES)
