@@ -719,14 +719,15 @@ __device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds
 }
 template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC> constexpr int f32_group_lds() {
   constexpr int KS = BM == 32 ? 64 : 32;
+  if (BM == 16) return kShareFloats * 4;
   if (std::is_same<T, float>::value && VEC && BM > 32) return 2 * (F32Panel<BM, A_KC>::FLOATS + F32Panel<BN, B_KC>::FLOATS) * 4;
   return 2 * (F32Tile<T, BM, KS, A_KC, VEC>::FLOATS + F32Tile<T, BN, KS, B_KC, VEC>::FLOATS) * 4;
 }
 constexpr int kGroupsAtOnce = 256;       // of which the first tiles are kept in LDS, a thread each
 template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC>
-__global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_grouped_kernel(F32Gemm p, F32Groups gr) {
+__global__ __launch_bounds__(BM == 16 ? 64 * kShares : 256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_grouped_kernel(F32Gemm p, F32Groups gr) {
   extern __shared__ __align__(16) float lds[];
-  __shared__ int starts[kGroupsAtOnce + 1], wave_total[4];
+  __shared__ int starts[kGroupsAtOnce + 1], wave_total[kShares];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   // tiles of all groups are dealt out as one list, wherever the batches of groups end
   int64_t before = 0;
@@ -759,6 +760,8 @@ __global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_group
       item = listed - (int64_t)piece * starts[ng];
       int a = 0, b = ng;                           // the last group that starts at or before the tile
       while (b - a > 1) { const int mid = (a + b) >> 1; if (starts[mid] <= item) a = mid; else b = mid; }
+      a = __builtin_amdgcn_readfirstlane(a);
+      const int tile = __builtin_amdgcn_readfirstlane((int)(item - starts[a]));
       const int first = min(max(gr.offsets[g0 + a], 0), gr.bound);
       const int rows = max(min(max(gr.offsets[g0 + a + 1], 0), gr.bound) - first, 0);
       F32Gemm q = p;
@@ -788,9 +791,10 @@ __global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_group
         }
         if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
       }
-      if constexpr (std::is_same<T, float>::value && VEC && BM > 32) f32_block<BM, BN, A_KC, B_KC>(q, (int)(item - starts[a]), lds);
-      else if constexpr (BM == 32) { q.in_shares = true; gemm_f32_tile<T, 32, 64, A_KC, B_KC, VEC, true>(q, (int)(item - starts[a]), lds); }
-      else gemm_f32_tile<T, BM, 32, A_KC, B_KC, VEC, false>(q, (int)(item - starts[a]), lds);
+      if constexpr (BM == 16) gemm_f32_share_tile<A_KC, B_KC, F32_PLAIN>(q, tile, lds);
+      else if constexpr (std::is_same<T, float>::value && VEC && BM > 32) f32_block<BM, BN, A_KC, B_KC>(q, tile, lds);
+      else if constexpr (BM == 32) { q.in_shares = true; gemm_f32_tile<T, 32, 64, A_KC, B_KC, VEC, true>(q, tile, lds); }
+      else gemm_f32_tile<T, BM, 32, A_KC, B_KC, VEC, false>(q, tile, lds);
     }
     before += all;
   }
@@ -801,8 +805,11 @@ __global__ __launch_bounds__(256, BM * BN > 64 * 64 ? 2 : 4) void gemm_f32_group
 // tile (groups' rows: their mean, the longest 2.5 times that).  Measured, tiles of 32 x 32 / 64 x 64 / 64 x 128 / 128 x 128, us (price):
 //   2998 rows of 12, 640 x 1000, input gradient 57 61 74 71 (56 60 73 61), forward 57 49 48 49 (58 52 50 47);  1038 of 3, 1728 x 4080, input gradient 234 165 161 253
 //   (232 149 141 256), weight gradient 207 137 146 141 (199 134 135 134);  500 x 2048, K 512 19 17 24 39 (20 17 25 39);  6065 of 5, input gradient, 152 columns, K 2192 56 79 78 139
+// Few rows over a long contraction are one chain of K-tiles: 16 x 16 with a share of the contraction to each of eight waves (gemm_f32_share_tile), two workgroups to a CU, a
+// microsecond and 0.85 for 256 k-values a round, or what they read through the caches at 11 TB/s (strided, by single words, 6).  32 x 32 / shares, us: input gradient of 18 rows
+// of 2, 1592 x 4168, 42 15; of 1000 of 4, 64 columns, K 4096, 41 20; forward 128 of 2, 512 columns, K 2048, 23 15; 64 rows, 2048 x 2048, forward 24 34, input gradient 24 20.
 struct F32Choice { int bm, bn; double us; };
-F32Choice f32_choice(bool a_kc, int64_t M, int64_t N, double K, int64_t groups, int splits) {
+F32Choice f32_choice(bool a_kc, bool b_kc, int64_t M, int64_t N, double K, int64_t groups, int splits, bool shares) {
   struct Shape { int bm, bn; double share; };
   constexpr Shape shapes[] = {{32, 32, 0.56}, {64, 64, 0.77}, {64, 128, 0.82}, {128, 64, 0.82}, {128, 128, 0.88}};
   F32Choice best = {};
@@ -813,6 +820,11 @@ F32Choice f32_choice(bool a_kc, int64_t M, int64_t N, double K, int64_t groups, 
     const double per = (std::ceil((items - spread) / 256.0) + std::ceil(items / 256.0) + std::ceil((items + spread) / 256.0)) / 3.0;
     const double us = 8.0 + std::max(per, !a_kc && groups > 1 ? 2.5 : 1.0) * t.bm * t.bn * (K + 32.0) * 2.0 / 614e3 / t.share;
     if (!best.bm || us < best.us) best = {t.bm, t.bn, us};
+  }
+  if (a_kc && shares && splits == 1) {
+    const double items = (double)ceil_div(N, 16) * (groups == 1 ? (double)ceil_div(M, 16) : (double)M / 16.0 + 0.5 * (double)std::min(groups, M));
+    const double us = 7.0 + std::max(std::ceil(items / 512.0) * (1.0 + 0.85 * K / 256.0), items * K * 128.0 / (b_kc ? 11e6 : 6e6));
+    if (us < best.us) best = {16, 16, us};
   }
   return best;
 }
@@ -827,7 +839,7 @@ mosaic_status launch_grouped_tiles(hipStream_t s, int quota, F32Gemm p, const F3
   const int64_t tm = ceil_div(p.M, BM), tn = ceil_div(p.N, BN), most = (A_KC ? (tm + gr.groups) * tn : tm * tn * gr.groups) * gr.splits;
   if (most > INT32_MAX / 2) MOSAIC_FAIL(MOSAIC_EUNSUPPORTED, "too many output tiles");
   p.tiles_m = (int)tm; p.tiles_n = (int)tn;
-  kern<<<grid_for(quota, BM * BN > 64 * 64 ? 2 : 4, most), 256, kLds, s>>>(p, gr);
+  kern<<<grid_for(quota, BM * BN > 64 * 64 || BM == 16 ? 2 : 4, most), BM == 16 ? 64 * kShares : 256, kLds, s>>>(p, gr);
   MOSAIC_LAUNCH_CHECK();
   return MOSAIC_OK;
 }
@@ -835,7 +847,11 @@ template <typename T, bool A_KC, bool B_KC, bool VEC>
 mosaic_status launch_grouped_t(hipStream_t s, int quota, F32Gemm p, const F32Groups& gr) {
   if constexpr (std::is_same<T, float>::value && VEC) {
     const double K = A_KC ? (gr.splits > 1 ? gr.split_k : p.K) : (double)p.K / (gr.groups * gr.splits);
-    const F32Choice c = f32_choice(A_KC, p.M, p.N, K, gr.groups, gr.splits);
+    // operands that the 32-bit offsets of the tiles of 16 reach
+    const bool near = ((int64_t)p.M + 32) * p.lda + p.K < (int64_t)1 << 29 && ((int64_t)std::max(p.N, p.K) + 32) * p.ldb + p.K < (int64_t)1 << 29;
+    const F32Choice c = f32_choice(A_KC, B_KC, p.M, p.N, K, gr.groups, gr.splits, near);
+    if constexpr (A_KC)
+      if (c.bm == 16) return launch_grouped_tiles<T, 16, 16, A_KC, B_KC, VEC>(s, quota, p, gr);
     if (c.bm > 32 && std::max(p.lda, p.ldb) <= 1 << 21) {          // a descriptor's 32 bits reach over the tile's rows
       if (c.bm == 128) return c.bn == 128 ? launch_grouped_tiles<T, 128, 128, A_KC, B_KC, VEC>(s, quota, p, gr) : launch_grouped_tiles<T, 128, 64, A_KC, B_KC, VEC>(s, quota, p, gr);
       return c.bn == 128 ? launch_grouped_tiles<T, 64, 128, A_KC, B_KC, VEC>(s, quota, p, gr) : launch_grouped_tiles<T, 64, 64, A_KC, B_KC, VEC>(s, quota, p, gr);
@@ -864,7 +880,7 @@ mosaic_status launch_form(hipStream_t s, int quota, bool a_kc, bool b_kc, const 
 
 }  // namespace
 
-double grouped_f32_us(bool a_kc, int64_t M, int64_t N, int64_t K, int splits) { return f32_choice(a_kc, M, N, (double)ceil_div(K, splits), 1, splits).us; }
+double grouped_f32_us(bool a_kc, int64_t M, int64_t N, int64_t K, int splits) { return f32_choice(a_kc, false, M, N, (double)ceil_div(K, splits), 1, splits, true).us; }
 
 // M: rows of A for all groups together, the most that there can be (a K-strided A: of each C).  K: the contraction (a K-strided A: the longest).
 // splits > 1 (one group, fp32): the contraction in pieces (K-contiguous A: of split_k), C [splits, M, ldc]

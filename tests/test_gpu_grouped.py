@@ -76,9 +76,10 @@ def test_odd_sizes_and_alignments(form, dtype):
     check(form, [0, 33, 33, 70], 40, 24, dtype, 70, off=1)
 
 
-# rows, columns and contraction of a product that take tiles of 64 x 64, 64 x 128, 128 x 64 and 128 x 128 in fp32, with ragged ends of each; a contraction of one piece
+# rows, columns and contraction of a product that take tiles of 64 x 64, 64 x 128, 128 x 64 and 128 x 128 in fp32, with ragged ends of each; a contraction of one piece;
+# few rows over a long one
 @pytest.mark.parametrize("form", FORMS)
-@pytest.mark.parametrize("rows,columns,depth", [(300, 1800, 100), (1500, 900, 100), (2100, 900, 100), (1500, 2300, 100), (1500, 2300, 4), (516, 2052, 516), (2108, 908, 164)])
+@pytest.mark.parametrize("rows,columns,depth", [(300, 1800, 100), (1500, 900, 100), (2100, 900, 100), (1500, 2300, 100), (1500, 2300, 4), (516, 2052, 516), (2108, 908, 164), (18, 404, 4168), (100, 72, 3004)])
 def test_fp32_tiles(form, rows, columns, depth):
     T, k, n = {"fwd": (rows, depth, columns), "dgrad": (rows, columns, depth), "wgrad": (depth, rows, columns)}[form]
     check(form, [0, T], k, n, "f32", T)
