@@ -538,7 +538,7 @@ size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t 
  * losses[t] = 0 for the others (device float [T], may be NULL), and *loss (device float) = sum of the losses / D with D = denom, or, denom = 0, the number of tokens that
  * count (no such token: loss 0, gradients 0).  mosaic_op_linear_ce_grad also writes the gradients of *loss: dX [T,h] and dtable [V,h] (overwritten; one of
  * them may be NULL).  Logits are fp32; bf16: the logits' gradient is rounded to bf16 before the products that dX and dtable are (formed of probabilities kept in fp16 relative to the
- * largest of 64).  What lies between is kept in
+ * largest of 64; of up to 16 tokens, or 512 tokens and V up to 512, what that rounding leaves takes part too).  What lies between is kept in
  * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
  * it holds what is left of the logits for as many tokens at a time as 2 GiB hold (bf16: of all tokens, where that wants no more room than several such pieces and the
  * fp32 sums of dtable that they need).  bf16: h a multiple of 8 and all tensors 16-byte aligned; the table is smaller than 4 GiB, V at most 2^22, h 2^20, T 2^30

@@ -87,6 +87,16 @@ def test_fp32_tiles(form, rows, columns, depth):
 
 
 @pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("rows,columns,depth", [(1500, 2300, 100), (300, 1800, 100), (18, 404, 4168)])
+def test_bits_of_fp32_tiles_do_not_depend_on_the_quota(form, rows, columns, depth):
+    T, k, n = {"fwd": (rows, depth, columns), "dgrad": (rows, columns, depth), "wgrad": (depth, rows, columns)}[form]
+    a, b = operands(form, T, 2, k, n, "f32")
+    want = call(form, [0, T // 3, T], k, n, a, b, "f32")
+    for quota in (1, 40, 200):
+        assert torch.equal(call(form, [0, T // 3, T], k, n, a, b, "f32", quota), want)
+
+
+@pytest.mark.parametrize("form", FORMS)
 def test_no_group_reads_another(form):
     """NaN in rows of no group and in one group's rows or matrix: the other groups' results have the bits that they have without."""
     k, n, offsets, T = 72, 104, [3, 60, 60, 200, 330], 340

@@ -224,6 +224,15 @@ def test_bits_do_not_depend_on_the_quota_or_the_stream(dtype):
         assert got["loss"] == want["loss"] and all(torch.equal(got[k], want[k]) for k in ("losses", "dx", "dtable"))
 
 
+@pytest.mark.parametrize("T,h,V,dtype", [(5, 256, 1582, "bf16"), (300, 72, 100, "bf16"), (40, 1104, 2000, "bf16"), (1500, 104, 2301, "f32"), (3, 520, 9001, "f32"), (2000, 64, 90, "f32")])
+def test_bits_of_small_workloads_do_not_depend_on_the_quota(T, h, V, dtype):
+    x, table, target = inputs(T, h, V, 0.2, dtype)
+    want = call(x, table, target, 0.1, 0.0, dtype)
+    for quota in (1, 24, 200):
+        got = call(x, table, target, 0.1, 0.0, dtype, quota=quota)
+        assert got["loss"] == want["loss"] and all(torch.equal(got[k], want[k]) for k in ("losses", "dx", "dtable"))
+
+
 def test_pieces_of_tokens():
     """More tokens than a piece holds: the table's gradient is summed over pieces in fp32; two of one size, one, and one of few tokens.
     dz in bf16 is off by 2^-7 relative to a probability, so the whole in the 2-norm by that at most and by 2^-8 for the last rounding."""
