@@ -280,7 +280,8 @@ struct W4GroupTiles {
 // exp(z - m) rounded to fp16 (0 past the last column, up to ldc).
 // From 0 to 1, relative to its block's largest: an fp16 number is within 2^-11 of it relative to itself, or within 2^-25 of the largest.  The logits
 // themselves in 16 bits would be off by that share of the logit, which the exponential turns into that much of a probability times the logit.
-// A block whose largest logit is -infinity counts from 0: its sum is 0.  NaN and +infinity make the sum NaN.  m is kept times log2 e.
+// A block whose largest logit is -infinity has a sum of 0, or NaN where it holds one, and m stays -infinity: a 0 in its place would be the largest of a row whose
+// logits all lie below.  +infinity makes the sum NaN.  m is kept times log2 e.
 // Here for one row of two blocks side by side, a lane's sixteen values v[h][j][e] of each, columns col + 64h + 16j + 4g + e; the four lanes of a row lie 16 apart
 // (g = 0 .. 3).  Two at once, because a wave is alone on its SIMD and every step waits for the one before (12288 x 4096 x 128000 9790 -> 9450 us).
 constexpr int kCeBlock = 64;
@@ -353,7 +354,7 @@ __device__ __forceinline__ void w4_softmax(const W4Args& p, f32x4 (&v)[2][4], in
 #pragma unroll
   for (int h = 0; h < 2; ++h) sum[h] = across_rows((part[h][0] + part[h][1]) + (part[h][2] + part[h][3]), add);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) if (first && col + 64 * h < p.N) p.stats[slot + h * p.M] = make_float2(ref[h], sum[h]);
+  for (int h = 0; h < 2; ++h) if (first && col + 64 * h < p.N) p.stats[slot + h * p.M] = make_float2(m[h] * kLog2e, sum[h]);
 }
 
 template <bool A_KC, bool B_KC, int EPI, int MI, int MAP = W4_WHOLE>

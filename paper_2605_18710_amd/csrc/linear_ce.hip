@@ -141,11 +141,14 @@ struct CePiece {
   float* losses;
 };
 
-// (m, sum) of two sets of columns; where nothing has come yet there is nothing to scale; infinities and NaN go into the sum as they are
+// (m, sum) of two sets of columns.  One of which nothing has come, or nothing but -infinity, has m = -infinity and adds its sum, 0 or NaN; infinities and NaN go into the
+// sum as they are
+__device__ __forceinline__ float reference(float top) { return top == -INFINITY ? 0.f : top; }
 __device__ __forceinline__ void join_sums(float& top, float& sum, float m, float s) {
-  const float high = fmaxf(top, m);
-  sum = (top == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f(top - high)) + (m == -INFINITY ? 0.f : s * __builtin_amdgcn_exp2f(m - high));
-  top = high;
+  const float before = top;
+  top = fmaxf(top, m);
+  const float ref = reference(top);
+  sum = sum * __builtin_amdgcn_exp2f(before - ref) + s * __builtin_amdgcn_exp2f(m - ref);
 }
 // A row's (m, sum) and totals over its blocks, by 64 groups of 16 lanes, a lane to a row; in the first group on return.
 struct RowSums { float (*top)[16], (*sum)[16], (*total)[16]; };       // [16][16] each, in LDS
@@ -159,9 +162,10 @@ __device__ __forceinline__ void row_sums(const float2* stats, const float* total
     float high = top;
 #pragma unroll
     for (int u = 0; u < 8; ++u) high = fmaxf(high, v[u].x);
-    if (high != top) { sum = top == -INFINITY ? 0.f : sum * __builtin_amdgcn_exp2f(top - high); top = high; }
+    if (high != top) { sum *= __builtin_amdgcn_exp2f(top - high); top = high; }
+    const float ref = reference(top);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) sum = fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - top), sum);
+    for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) sum = fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - ref), sum);
     if (totals) {
 #pragma unroll
       for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) total += totals[(b0 + 64 * u) * pitch + row];
@@ -411,7 +415,7 @@ __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* 
       sum = block_reduce(sum, false, lds);
       if (totals) total = block_reduce(total, false, lds);
       if (threadIdx.x == 0) {
-        stats[(int64_t)block * p.capacity + row] = make_float2(ref, sum);
+        stats[(int64_t)block * p.capacity + row] = make_float2(top * kLog2e, sum);
         if (totals) totals[(int64_t)block * p.capacity + row] = total;
       }
     }
@@ -462,7 +466,7 @@ __global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_logits_kernel(W4Arg
         o[e] = (_Float16)x;
       }
       sum = across_eight(sum, add);
-      if (first) p.stats[slot] = make_float2(ref, sum);
+      if (first) p.stats[slot] = make_float2(m * kLog2e, sum);
       if (p.C && in && col < p.ldc) *reinterpret_cast<f16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
     });
   }
@@ -742,7 +746,7 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(CeFew p) {
     sum = across_rows(sum, [](float a, float b) { return a + b; });
     if (p.totals) total = across_rows(total, [](float a, float b) { return a + b; });
     if (in && g == 0) {
-      p.stats[(int64_t)lr * tiles + tile] = make_float2(ref, sum);
+      p.stats[(int64_t)lr * tiles + tile] = make_float2(m * kLog2e, sum);
       if (p.totals) p.totals[(int64_t)lr * tiles + tile] = total;
     }
   }
