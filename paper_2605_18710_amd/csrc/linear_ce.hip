@@ -8,7 +8,7 @@
 //      stays on the device, where the products' workgroups read it.
 //   2. In pieces of tokens (kPieceElems): the product with the table, whose epilogue leaves exp(z - m) in fp16 and, for each row and 64 columns, the
 //      largest logit m and the sum (w4_softmax in gemm_w4.h); or only these, when the loss alone is asked for.
-//   3. lse_kernel joins a row's blocks to the logarithm of the sum and the loss; grad_kernel turns what lies there into dz, in place (and joins short rows itself).
+//   3. lse_kernel joins a row's blocks to the largest logit, the sum and the loss; grad_kernel turns what lies there into dz, in place (and joins short rows itself).
 //   4. dX = dz table, into the rows of X that the tokens came from; dtable = dz^T X, summed in fp32 over the pieces.
 // So the gradients take three products of 2 T h V operations, where pieces of the vocabulary would want the logits twice: their softmax needs the whole
 // row.  Few tokens or a small table: the products by few_tile.  fp32: the same on fp32 logits, in rows that a workgroup or a wave holds (rows_f32_kernel), or in blocks
@@ -26,7 +26,8 @@
 namespace {
 
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-constexpr float kLn2 = 0.69314718055994530942f, kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f;
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // ------------------------------------------------------------------------- the tokens that count
 struct CeHead { int count; float per_token; };      // their number, and 1 / D
@@ -136,8 +137,7 @@ struct CePiece {
   const float* at_target;
   int capacity, V;
   float smoothing;
-  float* lse;                  // of each row, to the base of 2; where `inverse` is given, what the sum's exponentials are relative to, and 1 / the sum
-  float* inverse;
+  float *top, *inverse;        // of each row: the largest logit, which the sum's exponentials are relative to, and 1 / the sum
   float* losses;
 };
 
@@ -148,7 +148,7 @@ __device__ __forceinline__ void join_sums(float& top, float& sum, float m, float
   const float before = top;
   top = fmaxf(top, m);
   const float ref = reference(top);
-  sum = sum * __builtin_amdgcn_exp2f(before - ref) + s * __builtin_amdgcn_exp2f(m - ref);
+  sum = sum * exp_of(before - ref) + s * exp_of(m - ref);
 }
 // A row's (m, sum) and totals over its blocks, by 64 groups of 16 lanes, a lane to a row; in the first group on return.
 struct RowSums { float (*top)[16], (*sum)[16], (*total)[16]; };       // [16][16] each, in LDS
@@ -162,10 +162,10 @@ __device__ __forceinline__ void row_sums(const float2* stats, const float* total
     float high = top;
 #pragma unroll
     for (int u = 0; u < 8; ++u) high = fmaxf(high, v[u].x);
-    if (high != top) { sum *= __builtin_amdgcn_exp2f(top - high); top = high; }
+    if (high != top) { sum *= exp_of(top - high); top = high; }
     const float ref = reference(top);
 #pragma unroll
-    for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) sum = fmaf(v[u].y, __builtin_amdgcn_exp2f(v[u].x - ref), sum);
+    for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) sum = fmaf(v[u].y, exp_of(v[u].x - ref), sum);
     if (totals) {
 #pragma unroll
       for (int u = 0; u < 8; ++u) if (b0 + 64 * u < blocks) total += totals[(b0 + 64 * u) * pitch + row];
@@ -187,9 +187,11 @@ __device__ __forceinline__ void row_sums(const float2* stats, const float* total
   }
   __syncthreads();
 }
-__device__ __forceinline__ float token_loss(float lse, float at_target, float total, float smoothing, int V) {
-  const float loss = lse * kLn2 - (1.f - smoothing) * at_target;
-  return smoothing > 0.f ? loss - smoothing * (total / (float)V) : loss;
+// differences of logits first: next to them the logarithm keeps its digits
+__device__ __forceinline__ float token_loss(float top, float sum, float at_target, float total, float smoothing, int V) {
+  float ahead = fmaf(-(1.f - smoothing), at_target, top);
+  if (smoothing > 0.f) ahead -= smoothing * (total / (float)V);
+  return ahead + logf(sum);
 }
 
 // 16 rows to a workgroup: their statistics lie side by side.
@@ -201,10 +203,9 @@ __global__ __launch_bounds__(1024) void lse_kernel(CePiece p, const float2* __re
     float top, sum, total;
     row_sums(stats, totals, blocks, p.capacity, row, {top_of, sum_of, total_of}, top, sum, total);
     if (threadIdx.x < 16 && row < live) {
-      const float lse = top + __builtin_amdgcn_logf(sum);      // to the base of 2
-      p.lse[row] = p.inverse ? top : lse;
-      if (p.inverse) p.inverse[row] = 1.f / sum;
-      p.losses[p.rows[start + row]] = token_loss(lse, p.at_target[row], total, p.smoothing, p.V);
+      p.top[row] = top;
+      p.inverse[row] = 1.f / sum;
+      p.losses[p.rows[start + row]] = token_loss(top, sum, p.at_target[row], total, p.smoothing, p.V);
     }
   }
 }
@@ -219,7 +220,7 @@ constexpr int kLowTokens = 512, kLowColumns = 512, kFewRows = 16;
 template <bool PAST, bool JOIN, bool LO>
 __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* __restrict__ stats, const float* __restrict__ totals, bf16* __restrict__ E, int64_t ld, int64_t lo) {
   // JOIN: every workgroup joins its rows' blocks itself, of which there are at most kJoinBlocks, and no launch does before
-  __shared__ float top_of[4][16], sum_of[4][16], total_of[4][16], lse_of[16];
+  __shared__ float top_of[4][16], sum_of[4][16], total_of[4][16], row_top[16], row_inverse[16];
   const int live = p.span->live, start = p.span->start, strips = (int)((ld + kStrip - 1) / kStrip);
   const float even = p.smoothing / (float)p.V;
   const int64_t items = (int64_t)((live + 15) / 16) * strips;
@@ -227,14 +228,14 @@ __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* _
     const int r0 = (int)(item / strips) * 16, c0 = (int)(item % strips) * kStrip;
     const int col = c0 + 8 * (threadIdx.x & 127);
     f16x8 v[8];
-    float scale[8], lse[8];
+    float scale[8], top_of_row[8], inverse[8];
     int hit[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
       v[i] = load_from<PAST>(reinterpret_cast<const f16x8*>(E + (int64_t)row * ld + col));
-      if constexpr (!JOIN) lse[i] = p.lse[row];
+      if constexpr (!JOIN) { top_of_row[i] = p.top[row]; inverse[i] = p.inverse[row]; }
       scale[i] = stats[(int64_t)(col / kCeBlock) * p.capacity + row].x;
       hit[i] = p.target[start + row] - col;
     }
@@ -269,20 +270,20 @@ __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* _
       if (threadIdx.x < 16) {
 #pragma unroll
         for (int w = 1; w < 4; ++w) { join_sums(top, sum, top_of[w][r], sum_of[w][r]); total += total_of[w][r]; }
-        const float all = top + __builtin_amdgcn_logf(sum);
-        lse_of[r] = all;
-        if (tells) p.losses[token] = token_loss(all, at_target, total, p.smoothing, p.V);
+        row_top[r] = top;
+        row_inverse[r] = 1.f / sum;
+        if (tells) p.losses[token] = token_loss(top, sum, at_target, total, p.smoothing, p.V);
       }
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) lse[i] = lse_of[2 * i + (threadIdx.x >> 7)];
+      for (int i = 0; i < 8; ++i) { top_of_row[i] = row_top[2 * i + (threadIdx.x >> 7)]; inverse[i] = row_inverse[2 * i + (threadIdx.x >> 7)]; }
       __syncthreads();                           // read before the next strip's rows are joined
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int row = r0 + 2 * i + (threadIdx.x >> 7);
       if (row >= live || col >= ld) continue;
-      const float f = __builtin_amdgcn_exp2f(scale[i] - lse[i]);
+      const float f = exp_of(scale[i] - top_of_row[i]) * inverse[i];
       Vec16<bf16> o, rest;
       auto set = [&](int e, float x) {
         o.set(e, x);
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(256, 4) void grad_kernel(CePiece p, const float2* _
       for (int e = 0; e < 8; ++e) set(e, col + e < p.V ? (float)v[i][e] * f - even : 0.f);
       if (hit[i] >= 0 && hit[i] < 8) {
         // the target's probability from its own logit: 1 - p keeps its digits where p is near 1
-        const float d = (__builtin_amdgcn_exp2f(fmaf(own[i], kLog2e, -lse[i])) - 1.f) + (p.smoothing - even);
+        const float d = (exp_of(own[i] - top_of_row[i]) * inverse[i] - 1.f) + (p.smoothing - even);
 #pragma unroll
         for (int e = 0; e < 8; ++e) if (e == hit[i]) set(e, d);
       }
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(NT) void rows_f32_kernel(CePiece p, const CeHead* _
       }
     sum = reduce(sum, false);
     __syncthreads();                             // the target's logit has been read by all
-    if (threadIdx.x == 0) p.losses[p.rows[start + row]] = token_loss((ref + logf(sum)) / kLn2, at_target, total, p.smoothing, p.V);
+    if (threadIdx.x == 0) p.losses[p.rows[start + row]] = token_loss(ref, sum, at_target, total, p.smoothing, p.V);
     if (!grad) continue;
     const float inverse = 1.f / sum;
 #pragma unroll
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* 
       v[i] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       if (c0 + 1024 * i < p.V) v[i] = *reinterpret_cast<const f32x4*>(z + 1024 * i);
     }
-    const float base = GRAD ? p.lse[row] : 0.f, inverse = GRAD ? p.inverse[row] : 0.f;
+    const float base = GRAD ? p.top[row] : 0.f, inverse = GRAD ? p.inverse[row] : 0.f;
     float top = -INFINITY, total = 0.f, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -394,7 +395,7 @@ __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* 
       for (int e = 0; e < 4; ++e) {
         const int c = 1024 * i + e;
         if (GRAD) {
-          const float q = __builtin_amdgcn_exp2f(fmaf(v[i][e], kLog2e, -base)) * inverse;
+          const float q = exp_of(v[i][e] - base) * inverse;
           v[i][e] = c0 + c >= p.V ? 0.f : g * (c == target ? (q - 1.f) + (p.smoothing - even) : q - even);      // the products read whole 16-byte pieces
         } else {
           if (c0 + c >= p.V) v[i][e] = -INFINITY;
@@ -407,15 +408,15 @@ __global__ __launch_bounds__(256) void wide_f32_kernel(CePiece p, const CeHead* 
     }
     if constexpr (!GRAD) {
       top = block_reduce(top, true, lds);
-      const float ref = top == -INFINITY ? 0.f : top * kLog2e;
+      const float ref = reference(top);
 #pragma unroll
       for (int i = 0; i < PER; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(v[i][e], kLog2e, -ref));
+        for (int e = 0; e < 4; ++e) sum += exp_of(v[i][e] - ref);
       sum = block_reduce(sum, false, lds);
       if (totals) total = block_reduce(total, false, lds);
       if (threadIdx.x == 0) {
-        stats[(int64_t)block * p.capacity + row] = make_float2(top * kLog2e, sum);
+        stats[(int64_t)block * p.capacity + row] = make_float2(top, sum);
         if (totals) totals[(int64_t)block * p.capacity + row] = total;
       }
     }
@@ -457,16 +458,16 @@ __global__ __launch_bounds__(kFewNT, few_waves(RB)) void few_logits_kernel(W4Arg
         if (first) p.totals[slot] = total;
       }
       m = across_eight(m, high);
-      const float ref = m == -INFINITY ? 0.f : m * kLog2e;
+      const float ref = reference(m);
       f16x8 o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(v[e], kLog2e, -ref));
+        const float x = exp_of(v[e] - ref);
         sum += x;
         o[e] = (_Float16)x;
       }
       sum = across_eight(sum, add);
-      if (first) p.stats[slot] = make_float2(m * kLog2e, sum);
+      if (first) p.stats[slot] = make_float2(m, sum);
       if (p.C && in && col < p.ldc) *reinterpret_cast<f16x8*>(p.C + (int64_t)row * p.ldc + col) = o;
     });
   }
@@ -739,14 +740,14 @@ __global__ __launch_bounds__(kFewThreads) void few_kernel(CeFew p) {
       m = fmaxf(m, acc[e]);
     }
     m = across_rows(m, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = m == -INFINITY ? 0.f : m * kLog2e;
+    const float ref = reference(m);
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(fmaf(acc[e], kLog2e, -ref));
+    for (int e = 0; e < 4; ++e) sum += exp_of(acc[e] - ref);
     sum = across_rows(sum, [](float a, float b) { return a + b; });
     if (p.totals) total = across_rows(total, [](float a, float b) { return a + b; });
     if (in && g == 0) {
-      p.stats[(int64_t)lr * tiles + tile] = make_float2(m * kLog2e, sum);
+      p.stats[(int64_t)lr * tiles + tile] = make_float2(m, sum);
       if (p.totals) p.totals[(int64_t)lr * tiles + tile] = total;
     }
   }
@@ -778,7 +779,7 @@ __global__ __launch_bounds__(1024) void few_join_kernel(CeFew p) {
       join_sums(top, sum, m, s);                 // a lane of its own and its partner differ in the order, and in a last bit: lane 0's is taken
       total += __shfl_xor(total, o, 64);
     }
-    if (lane == 0) loss_of[row] = token_loss(top + __builtin_amdgcn_logf(sum), p.at_target[row], total, p.smoothing, p.V);
+    if (lane == 0) loss_of[row] = token_loss(top, sum, p.at_target[row], total, p.smoothing, p.V);
   }
   __syncthreads();
   if (row == 0 && lane < p.T) p.losses[lane] = at >= 0 ? loss_of[at] : 0.f;
@@ -840,7 +841,7 @@ struct CeLayout {
   int few_k;
   int64_t piece, ld, blocks, lo;               // lo: elements from a dz to what its rounding left, 0 where that is not kept
   int pieces, dw_splits, dx_splits, dx_k;      // dx: fp32 (bf16: w4_cut)
-  size_t head, spans, rows, target, slot, losses, at_target, lse, inverse, stats, totals, x, e, sums, bytes;
+  size_t head, spans, rows, target, slot, losses, at_target, top, inverse, stats, totals, x, e, sums, bytes;
   CeLayout(int dtype, int64_t T, int64_t h, int64_t V, bool grad) {
     const bool half = dtype == MOSAIC_BF16;
     const size_t es = dtype_size(dtype);
@@ -857,7 +858,7 @@ struct CeLayout {
     head = take(sizeof(CeHead));
     spans = take((int64_t)sizeof(CeSpan) * pieces);
     rows = take(4 * padded); target = take(4 * padded); slot = take(4 * padded); losses = take(4 * T);
-    at_target = take(4 * piece); lse = take(4 * piece); inverse = take(half ? 0 : 4 * piece);
+    at_target = take(4 * piece); top = take(4 * piece); inverse = take(4 * piece);
     stats = take(8 * blocks * piece); totals = take(4 * blocks * piece);
     x = take(padded * h * (int64_t)es);
     lo = !half || !grad ? 0 : T <= kFewRows ? kFewRows * ld : T <= kLowTokens && V <= kLowColumns ? piece * ld : 0;
@@ -969,7 +970,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     const CeLoss now = {losses, (int)T, head, i + 1 == L.pieces && T <= kAddMax ? loss : nullptr};
     CePiece p = {};
     p.span = spans + i; p.rows = rows; p.target = target; p.at_target = (float*)(base + L.at_target);
-    p.capacity = capacity; p.V = (int)V; p.smoothing = smoothing; p.lse = (float*)(base + L.lse); p.losses = losses;
+    p.capacity = capacity; p.V = (int)V; p.smoothing = smoothing; p.top = (float*)(base + L.top); p.inverse = (float*)(base + L.inverse); p.losses = losses;
     if (!half) {
       float* Z = (float*)(base + L.e);
       MOSAIC_TRY(launch_grouped_f32(s, quota, dtype, true, true, some, (int)V, (int)h, Xc + r0 * h * 4, h, table, h, Z, L.ld, nullptr, live, 1, capacity, 0));
@@ -982,7 +983,6 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
       } else {
         float2* const stats = (float2*)(base + L.stats);
         float* const totals = smoothing > 0.f ? (float*)(base + L.totals) : nullptr;
-        p.inverse = (float*)(base + L.inverse);
         const int grid = grid_for(quota, 8, some * L.blocks);
         wide_f32_kernel<false><<<grid, 256, 0, s>>>(p, head, Z, L.ld, stats, totals, (float*)(base + L.at_target));
         MOSAIC_LAUNCH_CHECK();

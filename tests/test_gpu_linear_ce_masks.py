@@ -11,7 +11,8 @@ from helpers import from_dev, quantize
 from test_gpu_linear_ce import U, bounds, call, close
 
 pytestmark = pytest.mark.gpu
-MASKS = [-np.inf]
+LOWEST = float(torch.finfo(torch.bfloat16).min)          # finite in either type
+MASKS = [-np.inf, -1e9, -1e30, LOWEST]
 
 
 def masked_inputs(T, h, V, level, value, dtype, seed=11):
@@ -60,6 +61,25 @@ def test_masked_rows_of_the_table(T, h, V, level, value, dtype):
     close(alone["loss"], loss, bl.sum() / n + 4 * U * abs(loss), "loss alone")
 
 
+@pytest.mark.parametrize("value", MASKS[1:])
+@pytest.mark.parametrize("T,V", [(5, 3000), (40, 3000), (40, 6001), (300, 9001)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_row_masked_by_the_same_finite_value(T, V, value, dtype):
+    """All logits are equal, so every probability is 1 / V and every loss log V: off by a logarithm's rounding, a sum's of V ones, and what bf16 makes of D dz."""
+    x, table = np.zeros((T, 64)), np.zeros((V, 64))
+    x[:, 0] = 1.0
+    table[:, 0] = value
+    x[np.arange(T), 1 + np.arange(T) % 63] = 1.0           # which the gradient of a row of the table shows
+    target = synth.integers(4, (T,), 0, V).astype(np.int32)
+    got = call(quantize(x, dtype), quantize(table, dtype), target, 0.0, 0.0, dtype)
+    assert np.abs(from_dev(got["losses"]) - np.log(V)).max() <= (64 + V / 512) * 2 * U + 8 * U * np.log(V)
+    dz = np.full((T, V), 1.0 / V)
+    dz[np.arange(T), target] -= 1.0
+    dtable = dz.T @ x / T
+    bound = (2.0 ** -7 if dtype == "bf16" else 0.0) * (np.abs(dz).T @ x / T) + (64 + V / 512 + T) * 2 * U * (np.abs(dz).T @ x / T)
+    close(from_dev(got["dtable"]), dtable, bound, "dtable")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,V", [(5, 3000), (40, 3000), (40, 6001), (40, 9001)])
 def test_every_row_masked_by_infinity(T, V, dtype):
@@ -71,3 +91,35 @@ def test_every_row_masked_by_infinity(T, V, dtype):
     bad = call(x, table, target, 0.0, 10.0, dtype)
     keep = [t for t in range(T) if t != 3]
     assert torch.isnan(bad["losses"][3]) and torch.isfinite(bad["losses"][keep]).all() and torch.equal(bad["losses"][keep], base["losses"][keep])
+
+
+@pytest.mark.parametrize("T,V,dtype", [(12, 1000, "bf16"), (60, 400, "bf16"), (60, 1000, "bf16"), (60, 5000, "bf16"), (60, 1000, "f32"), (60, 9001, "f32")])
+def test_probabilities_next_to_one_keep_their_digits(T, V, dtype):
+    """Whole logits around 200, the target's 16 and more ahead: they are exact, so 1 - p is off by what the sums and the exponential leave: a sum next to 1 by half a step at each of
+    fewer than 64 + V / 512 additions, probabilities by 2^-23 |argument| of themselves, in bf16 by 2^-11 or 2^-25 of their block's largest, and dz by its roundings.  Every token has a column of X of
+    its own, so the table's gradient shows each dz."""
+    h = 64
+    x = np.zeros((T, h))
+    x[np.arange(T), np.arange(T)] = 1.0
+    target = synth.integers(7, (T,), 0, V)
+    table = np.floor(synth.uniform(8, (V, h), 150.0, 181.0))
+    table[target, np.arange(T)] = 196.0 + np.arange(T) % 37
+    x, table = quantize(x, dtype), quantize(table, dtype)
+    assert (table == np.floor(table)).all() and table.max() < 256
+    _, losses, _, dtable = O.linear_ce(x, table, target.astype(np.int32))
+    got = call(x, table, target.astype(np.int32), 0.0, 1.0, dtype)
+    z = x @ table.T
+    p = np.exp(z - z.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    hit = np.zeros(p.shape, dtype=bool)
+    hit[np.arange(T), target] = True
+    rest = np.where(hit, 0.0, p)
+    dz = np.where(hit, -rest.sum(1, keepdims=True), p)
+    sums = (64 + V / 512) * U
+    block = np.repeat(np.stack([p[:, b:b + 64].max(1) for b in range(0, V, 64)], 1), 64, axis=1)[:, :V]
+    exponential = 2 * U * 100 * rest + sums * p
+    kept = 2.0 ** -11 * rest + 2.0 ** -25 * block if dtype == "bf16" else 0.0
+    off = np.where(hit, sums + 4 * U + exponential, exponential + kept)
+    want = dz.T @ x
+    last = 2.0 ** -7 if dtype == "bf16" else 2 * U
+    close(from_dev(got["dtable"]), want, off.T @ x * (1 + last) + last * np.abs(want), "dtable")
