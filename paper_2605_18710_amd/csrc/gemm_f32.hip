@@ -362,7 +362,8 @@ struct ShareOperand {
   int step;                      // bytes per k-value
   int k4;
   __device__ __forceinline__ void init(const float* base, int64_t ld, int x0, int X, int K, int lr, int g) {
-    const int64_t skip = KC ? (int64_t)x0 * ld : x0, all = KC ? (int64_t)(X - 1) * ld + K : (int64_t)(K - 1) * ld + X;
+    // KC: whole 16-byte pieces, which a row has (ld is a multiple of 4, and what lies past K in a row is zero)
+    const int64_t skip = KC ? (int64_t)x0 * ld : x0, all = KC ? (int64_t)(X - 1) * ld + (K + 3) / 4 * 4 : (int64_t)(K - 1) * ld + X;
     rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base) + skip, 0, (int)(uint32_t)((all - skip) * 4), 0x00020000);
     step = KC ? 4 : (int)(ld * 4);
     k4 = 4 * g;
