@@ -31,6 +31,7 @@ struct F32Gemm {
   int64_t lda, ldb, ldc;
   int tiles_m, tiles_n;
   bool in_shares;            // the order of the sums (share_order)
+  int chain;                 // > 0: shares are no longer than that
   // what the epilogues and the norm in front take (fp32 tensors, rows of whole 16-byte pieces)
   const float* Z;            // the stored input of the activation whose derivative is applied
   float* C2;                 // the activation, or the gradient behind the derivative
@@ -227,7 +228,7 @@ __device__ __host__ __forceinline__ int share_length(int K) { return (K + 64 * k
 
 template <typename T, int BT, int KS, bool A_KC, bool B_KC, bool VEC, bool SHARES, int EPI = F32_PLAIN, int NORM = 0>
 __device__ __forceinline__ void gemm_f32_tile(const F32Gemm& p, int tile, float* lds) {
-  static_assert((EPI == F32_PLAIN && !SHARES) || BT == 32, "shares and the other epilogues exist for 32 x 32 tiles");
+  static_assert(EPI == F32_PLAIN || BT == 32, "the other epilogues exist for 32 x 32 tiles");
   constexpr bool GU = EPI == F32_SWIGLU;
   constexpr int TW = BT / 32;                                      // 16-wide blocks per wave and direction
   typedef F32Tile<T, BT, KS, A_KC, VEC> TA;
@@ -242,12 +243,12 @@ __device__ __forceinline__ void gemm_f32_tile(const F32Gemm& p, int tile, float*
   const int m0 = tm * BT, n0 = tn * (GU ? 16 : BT);
   TA ta; TB tb;
   // SHARES: the sum of gemm_f32_share_tile, a share of the contraction at a time
-  const int share = p.in_shares ? share_length(p.K) : 0;
-  f32x4 acc[TW][TW], sum = {-0.f, -0.f, -0.f, -0.f};        // -0 + x is x for every x
+  const int all = p.in_shares ? share_length(p.K) : 0, share = p.chain ? min(all, p.chain) : all;
+  f32x4 acc[TW][TW], sum[TW][TW];
 #pragma unroll
   for (int i = 0; i < TW; ++i)
 #pragma unroll
-    for (int j = 0; j < TW; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < TW; ++j) { acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f}; sum[i][j] = f32x4{-0.f, -0.f, -0.f, -0.f}; }      // -0 + x is x for every x
   if constexpr (!NORM) ta.request(A, p.lda, m0, p.M, 0, p.K);
   tb.request(B, p.ldb, n0, p.N, 0, p.K, GU ? p.f : 0);
   if constexpr (NORM != 0) f32_norm_panel<NORM>(p, m0, tn == 0, panel);
@@ -299,11 +300,20 @@ __device__ __forceinline__ void gemm_f32_tile(const F32Gemm& p, int tile, float*
       // the 10 wait states between a matrix instruction and another reader of its result: where a loop of them can be passed by, the compiler
       // has left them out (the sums of K-strided operands lost their fourth columns)
       asm volatile("s_nop 15" : "+v"(acc[0][0]));
-      sum += acc[0][0];
-      acc[0][0] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 1; i < TW * TW; ++i) asm volatile("" : "+v"(acc[i / TW][i % TW]));
+#pragma unroll
+      for (int i = 0; i < TW; ++i)
+#pragma unroll
+        for (int j = 0; j < TW; ++j) { sum[i][j] += acc[i][j]; acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f}; }
     }
   } while (SHARES && k0 < p.K);
-  if constexpr (SHARES) acc[0][0] = sum;
+  if constexpr (SHARES) {
+#pragma unroll
+    for (int i = 0; i < TW; ++i)
+#pragma unroll
+      for (int j = 0; j < TW; ++j) acc[i][j] = sum[i][j];
+  }
   __syncthreads();                       // the next tile writes stage 0
   // acc[i][j][e] is output (row m0+wm+16i+lr, column n0+wn+16j+4g+e)
   if constexpr (EPI != F32_PLAIN) {
@@ -382,7 +392,9 @@ struct ShareOperand {
 // A tile is one block of 16 x 16 outputs; each of eight waves takes an eighth of the contraction (share_length), its fragments straight from
 // memory, and the eight sums meet in LDS, added in wave order.  For long contractions over few tiles, which are one chain of
 // latencies: 128 x 256 outputs, K 768 (384): tiles of 32 x 32 8.8 us (5.6), this 5.3 (4.1); 100 x 64, K 1500 16.3 -> 5.7.
-template <bool A_KC, bool B_KC, int EPI>
+// CHAINS: a wave's sum in chains of kChain k-values, added in turn
+constexpr int kChain = 512;
+template <bool A_KC, bool B_KC, int EPI, bool CHAINS = false>
 __device__ __forceinline__ void gemm_f32_share_tile(const F32Gemm& p, int tile, float* lds) {
   constexpr int STEPS = 2;                     // k-steps of 16 requested together
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -394,7 +406,7 @@ __device__ __forceinline__ void gemm_f32_share_tile(const F32Gemm& p, int tile, 
   ShareOperand<B_KC> B;
   A.init((const float*)p.A, p.lda, m0, p.M, p.K, lr, g);
   B.init((const float*)p.B, p.ldb, n0, p.N, p.K, lr, g);
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f}, sum = acc;
   f32x4 fa[2][STEPS], fb[2][STEPS];            // [buffer][step]
   auto request = [&](auto buf_, int k0) {
     constexpr int buf = decltype(buf_)::value;
@@ -418,6 +430,17 @@ __device__ __forceinline__ void gemm_f32_share_tile(const F32Gemm& p, int tile, 
     multiply(B0{}, k0);
     request(B0{}, k0 + 32 * STEPS);
     multiply(B1{}, k0 + 16 * STEPS);
+    if constexpr (CHAINS) {
+      if ((k0 - kb) % kChain == kChain - 32 * STEPS) {
+        asm volatile("s_nop 15" : "+v"(acc));    // as in gemm_f32_tile
+        sum += acc;
+        acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+  }
+  if constexpr (CHAINS) {
+    asm volatile("s_nop 15" : "+v"(acc));
+    acc += sum;
   }
   // acc[e] is output (row lr, column 4g + e)
   *reinterpret_cast<f32x4*>(lds + (wave * 16 + lr) * kSharePitch + 4 * g) = acc;
@@ -662,9 +685,7 @@ __device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds
     pa.advance();
     pb.advance();
   };
-  // Sums of kChunk k-values each, added up: a chain of K roundings is off by sqrt(K / kChunk) times as much.  (128 x 128 has no registers for it; its contractions
-  // are short for what they are worth.)
-  constexpr int kChunk = 512;
+  // Sums of kChain k-values each, added up: a chain of K roundings is off by sqrt(K / kChain) times as much.  (128 x 128 has no registers for them: kLongChain.)
   constexpr bool CHUNKS = WM * WN < 4;
   f32x16 sum[CHUNKS ? WM : 1][CHUNKS ? WN : 1];
 #pragma unroll
@@ -682,7 +703,7 @@ __device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds
     k_tile(std::integral_constant<int, 1>{});
     if ((k0 += KS) >= K) break;
     if constexpr (CHUNKS) {
-      if (k0 % kChunk == 0) {
+      if (k0 % kChain == 0) {
         settle();
 #pragma unroll
         for (int i = 0; i < WM; ++i)
@@ -716,6 +737,20 @@ __device__ __forceinline__ void f32_block(const F32Gemm& p, int tile, float* lds
         *reinterpret_cast<f32x4*>(C + (int64_t)row * p.ldc + col) = v;
       }
     }
+  }
+}
+// 128 x 128: a chain of kLongChain k-values at a time, added to C, where a lane finds its own values again.  (Inside f32_block's loop the second epilogue cost its K-tiles registers,
+// and 5 to 40 % of their time.)  Weight gradient of 65536 rows, 2048 x 2048, 3950 us in one chain, this 4130; of 500000 rows one chain is off by 1.3e-5 of the result, this by 9e-7.
+constexpr int kLongChain = 2048;
+template <bool A_KC, bool B_KC>
+__device__ __forceinline__ void f32_block_long(F32Gemm p, int tile, float* lds) {
+  for (int left = p.K;; left -= kLongChain) {
+    p.K = min(left, kLongChain);
+    f32_block<128, 128, A_KC, B_KC>(p, tile, lds);
+    if (left <= kLongChain) break;
+    p.A = (const float*)p.A + (A_KC ? (int64_t)kLongChain : kLongChain * p.lda);
+    p.B = (const float*)p.B + (B_KC ? (int64_t)kLongChain : kLongChain * p.ldb);
+    p.R = p.C;
   }
 }
 template <typename T, int BM, int BN, bool A_KC, bool B_KC, bool VEC> constexpr int f32_group_lds() {
@@ -792,10 +827,12 @@ __global__ __launch_bounds__(BM == 16 ? 64 * kShares : 256, BM * BN > 64 * 64 ? 
         }
         if (p.R) q.R = (const T*)p.R + (g0 + a) * gr.stride;
       }
-      if constexpr (BM == 16) gemm_f32_share_tile<A_KC, B_KC, F32_PLAIN>(q, tile, lds);
+      q.in_shares = true;
+      q.chain = kChain;
+      if constexpr (BM == 16) gemm_f32_share_tile<A_KC, B_KC, F32_PLAIN, true>(q, tile, lds);
+      else if constexpr (std::is_same<T, float>::value && VEC && BM * BN > 64 * 128) f32_block_long<A_KC, B_KC>(q, tile, lds);
       else if constexpr (std::is_same<T, float>::value && VEC && BM > 32) f32_block<BM, BN, A_KC, B_KC>(q, tile, lds);
-      else if constexpr (BM == 32) { q.in_shares = true; gemm_f32_tile<T, 32, 64, A_KC, B_KC, VEC, true>(q, tile, lds); }
-      else gemm_f32_tile<T, BM, 32, A_KC, B_KC, VEC, false>(q, tile, lds);
+      else gemm_f32_tile<T, BM, BM == 32 ? 64 : 32, A_KC, B_KC, VEC, true>(q, tile, lds);
     }
     before += all;
   }
