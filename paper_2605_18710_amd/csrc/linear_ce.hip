@@ -940,7 +940,7 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
   int32_t *rows = (int32_t*)(base + L.rows), *target = (int32_t*)(base + L.target), *slot = (int32_t*)(base + L.slot);
   if (!losses) losses = (float*)(base + L.losses);
   const CeList list = {targets, (int)T, (int)V, (int)L.piece, L.pieces, denom, half, head, spans, rows, target, slot};
-  const bool wide = h % (half ? 8 : 4) == 0 && (((uintptr_t)X | (uintptr_t)dX) & 15) == 0;
+  const bool wide = half || (h % 4 == 0 && (((uintptr_t)X | (uintptr_t)dX) & 15) == 0);       // bf16 rows are whole 16-byte pieces
   auto place = [&](auto t, auto v) -> mosaic_status {
     typedef decltype(t) E;
     constexpr int N = decltype(v)::value;
@@ -954,9 +954,8 @@ mosaic_status launch_linear_ce(hipStream_t s, int quota, int dtype, int64_t T, i
     MOSAIC_LAUNCH_CHECK();
     return MOSAIC_OK;
   };
-  typedef std::integral_constant<int, 1> One;
-  if (half) MOSAIC_TRY(wide ? place(bf16(), std::integral_constant<int, 8>()) : place(bf16(), One()));
-  else MOSAIC_TRY(wide ? place(float(), std::integral_constant<int, 4>()) : place(float(), One()));
+  if (half) MOSAIC_TRY(place(bf16(), std::integral_constant<int, 8>()));
+  else MOSAIC_TRY(wide ? place(float(), std::integral_constant<int, 4>()) : place(float(), std::integral_constant<int, 1>()));
   float* const sums = (float*)(base + L.sums);
   // added by a launch that has the time, or by one of its own: up to this many tokens that takes 3 us of the workgroup that does
   constexpr int kAddMax = 16384;
