@@ -56,3 +56,40 @@ def test_products_over_many_columns(form, T, columns, odd):
     off = rms(C[rows].double() - ref) / math.sqrt(K)
     print("off by %.3g of the result, %.2f of the limit" % (off, off / limit(K)))
     assert off <= limit(K)
+
+
+@pytest.mark.parametrize("form", ["fwd", "dgrad", "wgrad"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_that_are_no_whole_pieces(form, dtype):
+    """Enough of them for tiles of 64 x 64.  Element by element: (K + 2) u sum |a b|, and bf16's last rounding."""
+    T, k, n, ends = 2600, 1023, 1025, [3, 700, 700, 2001, 2597]
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(6)
+    make = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(dt)
+    A = make(T, n if form == "dgrad" else k)
+    B = make(T, n) if form == "wgrad" else make(4, k, n)
+    at = torch.tensor(ends, dtype=torch.int32, device="cuda")
+    C = torch.full({"fwd": (T, n), "dgrad": (T, k), "wgrad": (4, k, n)}[form], 7.0, device="cuda", dtype=dt)
+    getattr(mb, "op_grouped_linear_" + form)(torch.cuda.current_stream().cuda_stream, 256, dtype, T, 4, k, n, at, A, B, C)
+    for e, (lo, hi) in enumerate(zip(ends, ends[1:])):
+        a = A[lo:hi].double()
+        if form == "wgrad":
+            left, right, got = a.t().contiguous(), B[lo:hi].double(), C[e]
+        else:
+            w = B[e].double()
+            left, right, got = a, w if form == "fwd" else w.t().contiguous(), C[lo:hi]
+        ref = left @ right
+        bound = (left.shape[1] + 2) * U * (left.abs() @ right.abs()) + (2.0 ** -8 * ref.abs() if dtype == "bf16" else 0.0)
+        assert ((got.double() - ref).abs() <= bound).all()
+    if form != "wgrad":
+        assert (C[:3] == 7).all() and (C[2597:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype,k,n", [("bf16", 64, 72), ("bf16", 2048, 1024), ("f32", 64, 72), ("f32", 33, 51), ("f32", 2048, 2048)])
+def test_weight_gradient_of_no_rows(dtype, k, n):
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    at = torch.zeros(4, dtype=torch.int32, device="cuda")
+    none = torch.empty((0, k), device="cuda", dtype=dt), torch.empty((0, n), device="cuda", dtype=dt)
+    dW = torch.full((3, k, n), 7.0, device="cuda", dtype=dt)
+    mb.op_grouped_linear_wgrad(torch.cuda.current_stream().cuda_stream, 256, dtype, 0, 3, k, n, at, *none, dW)
+    assert not dW.any()
