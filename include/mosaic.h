@@ -540,8 +540,9 @@ size_t        mosaic_op_linear_wgrad_pack8_scratch_bytes(int32_t dtype, int64_t 
  * them may be NULL).  Logits are fp32; bf16: the logits' gradient is rounded to bf16 before the products that dX and dtable are (formed of probabilities kept in fp16 relative to the
  * largest of 64; of up to 16 tokens, or 512 tokens and V up to 512, what that rounding leaves takes part too).  What lies between is kept in
  * scratch, a 256-byte aligned device buffer of the size that the _scratch_bytes calls give, apart from all other buffers and not shared by calls that overlap in time;
- * it holds what is left of the logits for as many tokens at a time as 2 GiB hold (bf16: of all tokens, where that wants no more room than several such pieces and the
- * fp32 sums of dtable that they need).  bf16: h a multiple of 8 and all tensors 16-byte aligned; the table is smaller than 4 GiB, V at most 2^22, h 2^20, T 2^30
+ * it holds what is left of the logits for as many tokens at a time as 2 GiB hold (bf16: of all tokens, where that wants no more than 2 GiB + 4 V h bytes, the room of several
+ * such pieces and the fp32 sums of dtable that they need).  Logits may be -infinity or of any finite size (rows of the table that are masked): they have a probability of 0 beside others, and
+ * a token of whose logits none is finite has NaN.  bf16: h a multiple of 8 and all tensors 16-byte aligned; the table is smaller than 4 GiB, V at most 2^22, h 2^20, T 2^30
  * (MOSAIC_EUNSUPPORTED otherwise). */
 size_t        mosaic_op_linear_ce_fwd_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);
 size_t        mosaic_op_linear_ce_grad_scratch_bytes(int32_t dtype, int64_t T, int64_t h, int64_t V);

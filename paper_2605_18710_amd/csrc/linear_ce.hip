@@ -15,7 +15,7 @@
 // of columns that lse_kernel joins (wide_f32_kernel).
 //
 // What bounds it: the matrix cores.  12288 tokens that count of 16384, h 4096, V 128000, bf16: 29.5 ms, 1.31 PFLOP/s over all; the pass over the logits in
-// step 3 takes 1.1 ms of it at 5.7 TB/s.  Of one token or a few: the table's bytes (few_kernel).  Of small workloads: four to seven launches.
+// step 3 takes 1.35 ms of it at 4.7 TB/s.  Of one token or a few: the table's bytes (few_kernel).  Of small workloads: four to seven launches.
 //
 // All sums have an order that the sizes and the targets fix.
 #include "gemm_few.h"
